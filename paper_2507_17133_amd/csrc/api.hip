@@ -1,5 +1,6 @@
 // C ABI of libbrownout_moe.so: argument validation, workspace carving, kernel sequencing, profiling.
 #include "internal.h"
+#include "layer.h"
 #include "tiles.h"
 
 #include <algorithm>
@@ -60,6 +61,8 @@ hipError_t ensure_device_init(DeviceInfo* info)
         if ((e = init_ffn_kernels()) != hipSuccess) return e;
         if ((e = init_route_kernels()) != hipSuccess) return e;
         if ((e = init_distill_kernels()) != hipSuccess) return e;
+        if ((e = init_attention_kernels()) != hipSuccess) return e;
+        if ((e = init_linear_kernels()) != hipSuccess) return e;
         int n_cu = 0;
         if ((e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev)) != hipSuccess) return e;
         void* sp = nullptr;
@@ -81,7 +84,7 @@ static void* static_scratch_of_current_device()
 
 static thread_local std::string g_hip_error;
 
-static moe_status hip_fail(hipError_t e, const char* where)
+moe_status hip_fail(hipError_t e, const char* where)
 {
     g_hip_error = std::string(where) + ": " + hipGetErrorString(e);
     (void)hipGetLastError();

@@ -1,0 +1,53 @@
+// Internal declarations of the operators around the MoE layer (norm.hip, rope.hip, attention.hip, linear8.hip, layer_api.hip).
+#pragma once
+#include "../../include/brownout_layer.h"
+#include "internal.h"
+
+namespace bmoe {
+
+moe_status hip_fail(hipError_t e, const char* where);      // api.hip: keeps the error's text for moe_last_hip_error
+
+constexpr int kScaleGroup = 128;                  // columns (and, of a weight, rows) under one e4m3 scale
+constexpr float kE4m3Max = 448.0f;
+constexpr float kLeastMagnitude = 7.888609052210118e-31f;  // 2^-100: keeps 448 / magnitude finite
+
+// Four floats -> four e4m3 in one 32-bit word, first value in the low byte.  Values within +-448 only (or NaN).
+__device__ __forceinline__ unsigned pack_e4m3(float a, float b, float c, float d)
+{
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// Eight bf16 of one 16-byte load as floats.
+__device__ __forceinline__ void unpack_bf16(const uint4 w, float* f)
+{
+    const unsigned u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __uint_as_float(u[i] << 16);
+        f[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ uint4 pack_bf16x8(const float* f)
+{
+    return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+
+hipError_t launch_norm(const moe_norm_args& a, bool norm, hipStream_t s);
+hipError_t launch_quantize_weight(const bf16_t* w, int N, int K, uint8_t* w8, float* w_scale, hipStream_t s);
+
+hipError_t launch_rope(const moe_kv_cache& c, const moe_block_table& t, const moe_rope& r, const bf16_t* q, int64_t q_stride,
+                       const bf16_t* k, int64_t k_stride, const bf16_t* v, int64_t v_stride, int n_heads, int T,
+                       const int32_t* positions, bf16_t* q_out, int64_t q_out_stride, hipStream_t s);
+
+hipError_t init_attention_kernels();
+size_t attention_workspace_bytes(const moe_kv_cache& c, int T, int n_heads);
+hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, const bf16_t* q, int64_t q_stride, int n_heads, int T,
+                            const int32_t* lengths, float scale, int window, bf16_t* out, int64_t out_stride, float* lse, void* ws,
+                            hipStream_t s);
+
+hipError_t init_linear_kernels();
+size_t linear_workspace_bytes(int M, int N, int K);
+hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s);
+
+}  // namespace bmoe

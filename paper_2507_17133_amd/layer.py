@@ -1,0 +1,318 @@
+"""Thin ctypes binding of the operators around the MoE layer (see include/brownout_layer.h): the norm with its residual and
+8-bit output, the 8-bit linear layer, rotary positions with the append to a paged key-value cache, attention over it.
+
+Like `binding`: argument marshalling only, no fallback path.  Tensors are on the current device; work goes to the
+current stream, or to `stream`.
+"""
+from __future__ import annotations
+
+import ctypes as C
+from dataclasses import dataclass
+from typing import NamedTuple, Optional, Tuple
+
+import torch
+
+from .binding import _check, _ptr, _stream, lib
+
+E4M3 = torch.float8_e4m3fn
+MOE_KV_BF16, MOE_KV_E4M3 = 0, 1
+ROPE_SCALINGS = ("none", "linear", "ntk", "yarn")
+EXPORTS = ("moe_rms_norm", "moe_quantize_rows", "moe_quantize_weight", "moe_linear_workspace_size", "moe_linear_e4m3",
+           "moe_rope_frequencies", "moe_rope_append", "moe_attention_workspace_size", "moe_paged_attention")
+
+
+class moe_norm_args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_stride", C.c_int64), ("residual", C.c_void_p), ("residual_stride", C.c_int64),
+                ("weight", C.c_void_p), ("residual_out", C.c_void_p), ("residual_out_stride", C.c_int64),
+                ("y", C.c_void_p), ("y_stride", C.c_int64), ("y8", C.c_void_p), ("y8_stride", C.c_int64),
+                ("scale", C.c_void_p), ("scale_stride", C.c_int64), ("T", C.c_int32), ("d", C.c_int32), ("eps", C.c_float)]
+
+
+class moe_linear_args(C.Structure):
+    _fields_ = [("x8", C.c_void_p), ("x_stride", C.c_int64), ("x_scale", C.c_void_p), ("x_scale_stride", C.c_int64),
+                ("w8", C.c_void_p), ("w_scale", C.c_void_p), ("out", C.c_void_p), ("out_stride", C.c_int64),
+                ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32)]
+
+
+class moe_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("type", C.c_int32),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class moe_block_table(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("row_stride", C.c_int64), ("token_row", C.c_void_p), ("n_rows", C.c_int32),
+                ("max_pages", C.c_int32)]
+
+
+class moe_rope(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32), ("factor", C.c_float)]
+
+
+class moe_rope_scaling(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("factor", C.c_double), ("original_length", C.c_double), ("beta_fast", C.c_double),
+                ("beta_slow", C.c_double)]
+
+
+_ready = None
+
+
+def _lib():
+    global _ready
+    if _ready is None:
+        L, p, i32, i64 = lib(), C.c_void_p, C.c_int32, C.c_int64
+        size = C.POINTER(C.c_size_t)
+        for name, args in {
+            "moe_rms_norm": [C.POINTER(moe_norm_args), p],
+            "moe_quantize_rows": [C.POINTER(moe_norm_args), p],
+            "moe_quantize_weight": [p, i32, i32, p, p, p],
+            "moe_linear_workspace_size": [i32, i32, i32, size],
+            "moe_linear_e4m3": [C.POINTER(moe_linear_args), p, C.c_size_t, p],
+            "moe_rope_frequencies": [i32, C.c_double, C.POINTER(moe_rope_scaling), C.POINTER(C.c_double), C.POINTER(C.c_float)],
+            "moe_rope_append": [C.POINTER(moe_kv_cache), C.POINTER(moe_block_table), C.POINTER(moe_rope), p, i64, p, i64, p, i64,
+                                i32, i32, p, p, i64, p],
+            "moe_attention_workspace_size": [C.POINTER(moe_kv_cache), i32, i32, size],
+            "moe_paged_attention": [C.POINTER(moe_kv_cache), C.POINTER(moe_block_table), p, i64, i32, i32, p, C.c_float, i32, p,
+                                    i64, p, p, C.c_size_t, p],
+        }.items():
+            f = getattr(L, name)
+            f.restype, f.argtypes = i32, args
+        _ready = L
+    return _ready
+
+
+def _rows(t: torch.Tensor, dtype, cols: int):
+    """A [rows, cols] tensor whose rows are contiguous; returns its row stride."""
+    assert t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[1] == cols and (cols == 1 or t.stride(1) == 1)
+    return t.stride(0)
+
+
+def _groups(d: int) -> int:
+    return (d + 127) // 128
+
+
+# ---------------------------------------------------------------- norm, 8-bit rows and weights
+
+class NormOut(NamedTuple):
+    y: Optional[torch.Tensor] = None          # [T][d] bf16
+    y8: Optional[torch.Tensor] = None         # [T][d] e4m3
+    scale: Optional[torch.Tensor] = None      # [ceil(d/128)][T] fp32
+    residual: Optional[torch.Tensor] = None   # [T][d] bf16
+
+
+def alloc_norm_out(T: int, d: int, want=("y",), residual: bool = False, device="cuda") -> NormOut:
+    bf = dict(dtype=torch.bfloat16, device=device)
+    q = "y8" in want
+    return NormOut(torch.empty((T, d), **bf) if "y" in want else None, torch.empty((T, d), dtype=E4M3, device=device) if q else None,
+                   torch.empty((_groups(d), T), dtype=torch.float32, device=device) if q else None,
+                   torch.empty((T, d), **bf) if residual else None)
+
+
+def _norm_args(x, out: NormOut) -> moe_norm_args:
+    T, d = x.shape
+    a = moe_norm_args(x=x.data_ptr(), x_stride=_rows(x, torch.bfloat16, d), T=T, d=d)
+    if out.y is not None:
+        assert out.y.shape[0] == T
+        a.y, a.y_stride = out.y.data_ptr(), _rows(out.y, torch.bfloat16, d)
+    if out.y8 is not None:
+        assert out.y8.shape[0] == T and out.scale.shape[0] == _groups(d)
+        a.y8, a.y8_stride = out.y8.data_ptr(), _rows(out.y8, E4M3, d)
+        a.scale, a.scale_stride = out.scale.data_ptr(), _rows(out.scale, torch.float32, T)
+    return a
+
+
+def moe_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
+                 want=("y",), out: Optional[NormOut] = None, stream=None) -> NormOut:
+    """Norm of x + residual; `want`: "y" (bf16), "y8" (e4m3 with scales), or both.  The sum comes back as `residual` if one was given."""
+    T, d = x.shape
+    if out is None:
+        out = alloc_norm_out(T, d, want, residual is not None, x.device)
+    a = _norm_args(x, out)
+    a.eps = eps
+    if residual is not None:
+        assert residual.shape[0] == T
+        a.residual, a.residual_stride = residual.data_ptr(), _rows(residual, torch.bfloat16, d)
+    if weight is not None:
+        assert weight.is_cuda and weight.dtype == torch.bfloat16 and weight.shape == (d,) and weight.is_contiguous()
+        a.weight = weight.data_ptr()
+    if out.residual is not None:
+        assert out.residual.shape[0] == T
+        a.residual_out, a.residual_out_stride = out.residual.data_ptr(), _rows(out.residual, torch.bfloat16, d)
+    _check(_lib().moe_rms_norm(C.byref(a), _stream(stream)), "moe_rms_norm")
+    return out
+
+
+def moe_quantize_rows(x: torch.Tensor, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None):
+    """(x8 [T][d] e4m3, scale [ceil(d/128)][T])."""
+    T, d = x.shape
+    o = alloc_norm_out(T, d, ("y8",), device=x.device) if out is None else NormOut(y8=out[0], scale=out[1])
+    _check(_lib().moe_quantize_rows(C.byref(_norm_args(x, o)), _stream(stream)), "moe_quantize_rows")
+    return o.y8, o.scale
+
+
+def moe_quantize_weight(w: torch.Tensor, stream=None):
+    """(w8 [N][K] e4m3, w_scale [ceil(N/128)][ceil(K/128)]) of a bf16 weight [N][K]."""
+    N, K = w.shape
+    assert w.is_cuda and w.dtype == torch.bfloat16 and w.is_contiguous()
+    w8 = torch.empty((N, K), dtype=E4M3, device=w.device)
+    scale = torch.empty((_groups(N), _groups(K)), dtype=torch.float32, device=w.device)
+    _check(_lib().moe_quantize_weight(_ptr(w), N, K, _ptr(w8), _ptr(scale), _stream(stream)), "moe_quantize_weight")
+    return w8, scale
+
+
+def linear_workspace_size(M: int, N: int, K: int) -> int:
+    n = C.c_size_t(0)
+    _check(_lib().moe_linear_workspace_size(M, N, K, C.byref(n)), "moe_linear_workspace_size")
+    return n.value
+
+
+def alloc_linear_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:
+    return torch.empty(linear_workspace_size(M, N, K), dtype=torch.uint8, device=device)
+
+
+def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w_scale: torch.Tensor, out: Optional[torch.Tensor] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    M, K = x8.shape
+    N = w8.shape[0]
+    assert w8.is_cuda and w8.dtype == E4M3 and w8.shape == (N, K) and w8.is_contiguous()
+    assert w_scale.is_cuda and w_scale.dtype == torch.float32 and w_scale.shape == (_groups(N), _groups(K)) and w_scale.is_contiguous()
+    assert x_scale.shape[0] == _groups(K)
+    if out is None:
+        out = torch.empty((M, N), dtype=torch.bfloat16, device=x8.device)
+    assert out.shape[0] == M
+    if workspace is None:
+        workspace = alloc_linear_workspace(M, N, K, x8.device)
+    a = moe_linear_args(x8.data_ptr(), _rows(x8, E4M3, K), x_scale.data_ptr(), _rows(x_scale, torch.float32, M), w8.data_ptr(),
+                        w_scale.data_ptr(), out.data_ptr(), _rows(out, torch.bfloat16, N), M, N, K)
+    _check(_lib().moe_linear_e4m3(C.byref(a), workspace.data_ptr(), workspace.numel(), _stream(stream)), "moe_linear_e4m3")
+    return out
+
+
+# ---------------------------------------------------------------- paged cache, rotary positions, attention
+
+class KvCache:
+    """k and v of a paged cache as [page, token, head, head_dim] tensors or views of one (head by head pages: a transposed view)
+    with equal strides, bf16 or e4m3 (then with k_scale and v_scale [head] fp32)."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        e4m3 = k.dtype == E4M3
+        assert k.is_cuda and v.is_cuda and k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
+        assert k.stride(3) == 1 and (e4m3 or k.dtype == torch.bfloat16)
+        for s in (k_scale, v_scale):
+            assert (s is not None) == e4m3, "scales belong to an e4m3 cache, and only to one"
+            assert s is None or (s.is_cuda and s.dtype == torch.float32 and s.shape == (k.shape[2],) and s.is_contiguous())
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        n, page, heads, dim = k.shape
+        self.struct = moe_kv_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
+                                   None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr(),
+                                   MOE_KV_E4M3 if e4m3 else MOE_KV_BF16, n, page, heads, dim)
+
+
+def alloc_kv_cache(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, k_scale=None, v_scale=None, heads_first: bool = False,
+                   device="cuda") -> KvCache:
+    """An empty cache; e4m3 if scales are given.  heads_first: pages are stored head by head."""
+    dtype = torch.bfloat16 if k_scale is None else E4M3
+    shape = (n_pages, n_kv_heads, page_size, head_dim) if heads_first else (n_pages, page_size, n_kv_heads, head_dim)
+    k, v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
+    return KvCache(k.transpose(1, 2), v.transpose(1, 2), k_scale, v_scale) if heads_first else KvCache(k, v, k_scale, v_scale)
+
+
+def _table(block_table: torch.Tensor, token_row: Optional[torch.Tensor], T: int) -> moe_block_table:
+    assert block_table.is_cuda and block_table.dtype == torch.int32 and block_table.dim() == 2
+    assert block_table.shape[1] <= 1 or block_table.stride(1) == 1
+    if token_row is not None:
+        assert token_row.is_cuda and token_row.dtype == torch.int32 and token_row.shape == (T,) and token_row.is_contiguous()
+    return moe_block_table(block_table.data_ptr(), block_table.stride(0), None if token_row is None else token_row.data_ptr(),
+                           block_table.shape[0], block_table.shape[1])
+
+
+def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: float = 0.0,
+                     beta_fast: float = 32.0, beta_slow: float = 1.0) -> Tuple[torch.Tensor, float]:
+    """Whole turns per position of each pair (CPU, fp64 [rotary_dim/2]) and the factor on cos and sin."""
+    turns = (C.c_double * max(rotary_dim // 2, 1))()
+    f = C.c_float(0.0)
+    s = moe_rope_scaling(ROPE_SCALINGS.index(scaling), factor, original_length, beta_fast, beta_slow)
+    _check(_lib().moe_rope_frequencies(rotary_dim, base, C.byref(s), turns, C.byref(f)), "moe_rope_frequencies")
+    return torch.tensor(list(turns), dtype=torch.float64), float(f.value)
+
+
+@dataclass
+class Rope:
+    """Rotary positions of a model: turns on the device, as rope_frequencies gives them."""
+    turns: Optional[torch.Tensor]
+    rotary_dim: int
+    interleaved: bool = False
+    factor: float = 1.0
+
+    def __post_init__(self):
+        if self.rotary_dim:
+            assert self.turns.is_cuda and self.turns.dtype == torch.float64 and self.turns.shape == (self.rotary_dim // 2,)
+            assert self.turns.is_contiguous()
+        self.struct = moe_rope(self.turns.data_ptr() if self.rotary_dim else None, self.rotary_dim, 1 if self.interleaved else 0, self.factor)
+
+
+def make_rope(rotary_dim: int, interleaved: bool = False, device="cuda", **frequencies) -> Rope:
+    """Rope of rope_frequencies(rotary_dim, **frequencies)."""
+    turns, factor = rope_frequencies(rotary_dim, **frequencies)
+    return Rope(turns.to(device), rotary_dim, interleaved, factor)
+
+
+def _heads(t: torch.Tensor, T: int, dim: int) -> int:
+    """A [T, heads, dim] tensor whose heads are next to each other; returns its token stride."""
+    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and t.shape[0] == T and t.shape[2] == dim
+    assert t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == dim)
+    return t.stride(0)
+
+
+def _ints(t: torch.Tensor, T: int):
+    assert t.is_cuda and t.dtype == torch.int32 and t.shape == (T,) and t.is_contiguous()
+    return t.data_ptr()
+
+
+def moe_rope_append(cache: KvCache, rope: Rope, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor,
+                    block_table: torch.Tensor, table_row: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """Rotates q [T, heads, dim] and k [T, kv heads, dim] (views of one projection's output as they are), writes k and v to the cache at
+    `positions` of the tokens' rows of block_table (table_row; None: row t), and returns the rotated q (`out`; may be q)."""
+    T, c = q.shape[0], cache.struct
+    qs, ks, vs = (_heads(t, T, c.head_dim) for t in (q, k, v))
+    assert k.shape[1] == v.shape[1] == c.n_kv_heads
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    assert out.shape == q.shape
+    tab = _table(block_table, table_row, T)
+    _check(_lib().moe_rope_append(C.byref(c), C.byref(tab), C.byref(rope.struct), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
+                                  q.shape[1], T, _ints(positions, T), out.data_ptr(), _heads(out, T, c.head_dim), _stream(stream)),
+           "moe_rope_append")
+    return out
+
+
+def attention_workspace_size(cache: KvCache, T_max: int, n_heads: int) -> int:
+    n = C.c_size_t(0)
+    _check(_lib().moe_attention_workspace_size(C.byref(cache.struct), T_max, n_heads, C.byref(n)), "moe_attention_workspace_size")
+    return n.value
+
+
+def alloc_attention_workspace(cache: KvCache, T_max: int, n_heads: int) -> torch.Tensor:
+    return torch.empty(attention_workspace_size(cache, T_max, n_heads), dtype=torch.uint8, device=cache.k.device)
+
+
+def moe_paged_attention(cache: KvCache, q: torch.Tensor, block_table: torch.Tensor, lengths: torch.Tensor,
+                        table_row: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0,
+                        out: Optional[torch.Tensor] = None, want_lse: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
+    """Attention of q [T, heads, dim] over the first `lengths` positions of the tokens' sequences (the last `window` of them if that
+    is not 0); scale None: 1 / sqrt(dim).  Returns out, or (out, lse [T, heads]) with want_lse."""
+    T, H = q.shape[:2]
+    c = cache.struct
+    qs = _heads(q, T, c.head_dim)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    assert out.shape == q.shape
+    lse = torch.empty((T, H), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        workspace = alloc_attention_workspace(cache, T, H)
+    tab = _table(block_table, table_row, T)
+    _check(_lib().moe_paged_attention(C.byref(c), C.byref(tab), q.data_ptr(), qs, H, T, _ints(lengths, T),
+                                      c.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), _heads(out, T, c.head_dim),
+                                      _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream(stream)), "moe_paged_attention")
+    return (out, lse) if want_lse else out
