@@ -28,9 +28,6 @@ struct LinearArgs {
     int vec;                                              // out rows take 8-byte stores
 };
 
-// What lies beyond K is read from here.
-static __device__ __align__(16) const uint4 zero16 = {0, 0, 0, 0};
-
 __device__ __forceinline__ f32x4 mfma_block(i32x8 w, i32x8 x)
 {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);   // scales of 1
@@ -136,6 +133,18 @@ __global__ void __launch_bounds__(kRowWaves * 64) linear_rows_kernel(LinearArgs 
 // 16-byte chunks; chunk c of row r is stored in slot c ^ (r / 2 & 7), so the 16 lanes that the LDS serves together (16 rows, one
 // chunk) fall on 16 different bank groups.
 // ------------------------------------------------------------------------------------------------
+// Direct loads to LDS, 16 or 4 bytes per lane: base (wave-uniform) + off -> lds + 16 (4) lane.  Written as instructions because the compiler puts a
+// wait for every such load in flight before each LDS read (it cannot tell their targets apart).  They have no result register; the kernel
+// waits for them by count before the barrier that hands their stage over.  Nothing else in the kernel uses m0.
+__device__ __forceinline__ void load_lds16(const uint8_t* base, unsigned off, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base));
+}
+__device__ __forceinline__ void load_lds4(const uint8_t* base, unsigned off, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base));
+}
+
 template <int BM, int BN, int WM, int WN, int NST>
 __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
 {
@@ -144,6 +153,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
     constexpr int TILE = (BM + BN) * 128, STAGE = TILE + BM * 4;
     static_assert(NW % 2 == 0 && LA >= 1 && LB >= 1 && TN <= kScaleGroup && BM % 64 == 0 && NST * STAGE <= 160 * 1024, "shape");
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
 
     // Block -> tile: each XCD (block id mod 8) gets a contiguous range of tiles; group_m M tiles x all N tiles follow each other, M
@@ -158,61 +168,106 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
     const int m0 = mt * BM, n0 = nt * BN;
     const int k_per = (p.nk + p.ksplit - 1) / p.ksplit, kb0 = min(p.nk, slice * k_per), nk = min(p.nk, kb0 + k_per) - kb0;
 
+    // A load is a wave-uniform base plus a lane's offset.  Rows past the end are the last one again (never stored); chunks past K, in the last
+    // block, are the row's last one again and are cleared in LDS.
     const int r8 = lane >> 3, chunk_at = ((lane & 7) ^ ((4 * (wave & 1) + (r8 >> 1)) & 7)) * 16;
-    const uint8_t *ga[LA], *gb[LB];
+    const int k_tail = p.K & 127, last = (k_tail != 0 && kb0 + nk == p.nk) ? nk - 1 : -1;       // the block that K ends in
+    const int back = max(0, chunk_at - (k_tail - 16));
+    unsigned oa[LA], ob[LB];
 #pragma unroll
-    for (int i = 0; i < LA; ++i) ga[i] = p.x + (int64_t)min(m0 + (wave + i * NW) * 8 + r8, p.M - 1) * p.x_stride + chunk_at + (int64_t)kb0 * 128;
+    for (int i = 0; i < LA; ++i) oa[i] = (unsigned)min((wave + i * NW) * 8 + r8, p.M - 1 - m0) * (unsigned)p.x_stride + chunk_at;
 #pragma unroll
-    for (int i = 0; i < LB; ++i) gb[i] = p.w + (int64_t)min(n0 + (wave + i * NW) * 8 + r8, p.N - 1) * p.K + chunk_at + (int64_t)kb0 * 128;
+    for (int i = 0; i < LB; ++i) ob[i] = (unsigned)min((wave + i * NW) * 8 + r8, p.N - 1 - n0) * (unsigned)p.K + chunk_at;
+    const uint8_t* xbase = p.x + (int64_t)m0 * p.x_stride + (int64_t)kb0 * 128;
+    const uint8_t* wbase = p.w + (int64_t)n0 * p.K + (int64_t)kb0 * 128;
     const int piece = wave & (BM / 64 - 1);               // 64 rows' scales
-    const float* gs = p.xs + (int64_t)kb0 * p.xs_stride + min(m0 + piece * 64 + lane, p.M - 1);
-    auto issue = [&](int kt) {
-        char* St = smem + (kt % NST) * STAGE;
-        const bool in_k = (kb0 + kt) * 128 + chunk_at < p.K;
+    const unsigned os = (unsigned)min(piece * 64 + lane, p.M - 1 - m0) * 4;
+    const uint8_t* sbase = reinterpret_cast<const uint8_t*>(p.xs + (int64_t)kb0 * p.xs_stride + m0);
+    // part of FM of the loads of block kt into stage st
+    auto issue = [&](int kt, int st, int part) {
+        const unsigned to = lds0 + st * STAGE, less = kt == last ? back : 0;
+        const uint8_t *wk = wbase + (int64_t)kt * 128, *xk = xbase + (int64_t)kt * 128;
 #pragma unroll
-        for (int i = 0; i < LB; ++i)
-            load_lds(in_k ? (const void*)(gb[i] + (int64_t)kt * 128) : (const void*)&zero16, St + BM * 128 + (wave + i * NW) * 1024);
-#pragma unroll
-        for (int i = 0; i < LA; ++i)
-            load_lds(in_k ? (const void*)(ga[i] + (int64_t)kt * 128) : (const void*)&zero16, St + (wave + i * NW) * 1024);
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(gs + (int64_t)kt * p.xs_stride),
-                                         (__attribute__((address_space(3))) void*)(St + TILE + piece * 256), 4, 0, 0);
+        for (int i = 0; i < LD; ++i) {
+            if (i * FM / LD != part) continue;
+            if (i < LB) load_lds16(wk, ob[i < LB ? i : 0] - less, to + BM * 128 + (wave + i * NW) * 1024);
+            else if (i < LB + LA) load_lds16(xk, oa[i < LB ? 0 : i < LB + LA ? i - LB : 0] - less, to + (wave + (i - LB) * NW) * 1024);
+            else load_lds4(sbase + (int64_t)kt * p.xs_stride * 4, os, to + TILE + piece * 256);
+        }
     };
 
     const int wm = wave / WN, wn = wave % WN;
     const int swz = (c >> 1) & 7, s0 = (g ^ swz) << 4, s1 = ((4 + g) ^ swz) << 4;
     const int a_off = (wm * TM + c) * 128, b_off = (BM + wn * TN + c) * 128;
     const float* wscale = p.ws + (int64_t)(min(n0 + wn * TN, p.N - 1) / kScaleGroup) * p.nk + kb0;
-    f32x4 acc[FM][FN];
+    f32x4 acc[FM][FN], prod[2][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    for (int kt = 0; kt < NST - 1 && kt < nk; ++kt) issue(kt);
-    for (int kt = 0; kt < nk; ++kt) {
-        if (nk - kt - 1 >= NST - 2) __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm((NST - 2) * LD));
-        else __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm(0));
-        lds_barrier();                                    // block kt is there; everyone has read block kt - 1
-        if (kt + NST - 1 < nk) issue(kt + NST - 1);
-        const char* St = smem + (kt % NST) * STAGE;
-        const float sw = wscale[kt];
-        i32x8 fb[FN];
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-            fb[j] = operand(*reinterpret_cast<const uint4*>(St + b_off + j * 2048 + s0), *reinterpret_cast<const uint4*>(St + b_off + j * 2048 + s1));
+    for (int j = 0; j < FN; ++j) prod[0][j] = prod[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float s[FM], s_last = 0.0f;                           // scales of the rows; of the last 16 rows of the block before
+
+    // A block of K: step i multiplies 16 rows by the wave's columns.  Behind each MFMA stand the multiply-adds of the step before, and in the
+    // steps the reads of the next step's rows and the loads of the block after next, one at a time.  The compiler would rather have all
+    // MFMAs first, which leaves the matrix pipe idle for as long as the multiply-adds take.
+    static_assert(FM % 2 == 0, "the last step's products are in the second set");
+#pragma unroll
+    for (int st = 0; st < NST - 1; ++st)
+#pragma unroll
+        for (int i = 0; i < FM; ++i) issue(min(st, nk - 1), st, i);
+    int stage = 0;
+    for (int kt = 0; kt < nk; ++kt) {
+        const float sw = wscale[kt];
+        __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm((NST - 2) * LD));
+        lds_barrier();                                    // block kt is there; everyone has read block kt - 1
+        const char* St = smem + stage * STAGE;
+        const int free = stage == 0 ? NST - 1 : stage - 1;
+        if (kt == last) {                                 // what was loaded in place of columns past K
+            char* mine = smem + stage * STAGE + wave * 1024 + lane * 16;
+            if (chunk_at >= k_tail) {
+#pragma unroll
+                for (int i = 0; i < LA + LB; ++i) *reinterpret_cast<uint4*>(mine + i * NW * 1024) = make_uint4(0, 0, 0, 0);
+            }
+            __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0)
+            lds_barrier();
+        }
+        const int next = min(kt + NST - 1, nk - 1);       // past the end: the last block again, never read
+        i32x8 fb[FN], fa[2];
+        auto frag = [&](int at) {
+            return operand(*reinterpret_cast<const uint4*>(St + at + s0), *reinterpret_cast<const uint4*>(St + at + s1));
+        };
+        fa[0] = frag(a_off);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fb[j] = frag(b_off + j * 2048);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) s[i] = *reinterpret_cast<const float*>(St + TILE + (wm * TM + i * 16 + c) * 4);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const i32x8 fa = operand(*reinterpret_cast<const uint4*>(St + a_off + i * 2048 + s0), *reinterpret_cast<const uint4*>(St + a_off + i * 2048 + s1));
-            const float s = sw * *reinterpret_cast<const float*>(St + TILE + (wm * TM + i * 16 + c) * 4);
+            const float sp = i == 0 ? s_last : s[i - 1];
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                const f32x4 t = mfma_block(fb[j], fa);
+                prod[i & 1][j] = mfma_block(fb[j], fa[i & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (j == 0 && i + 1 < FM) fa[(i + 1) & 1] = frag(a_off + (i + 1) * 2048);
+                if (j == FN / 2) issue(next, free, i);
+                f32x4& into = acc[i == 0 ? FM - 1 : i - 1][j];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] += t[e] * s;
+                for (int e = 0; e < 4; ++e) into[e] += prod[(i + 1) & 1][j][e] * sp;
+                __builtin_amdgcn_sched_barrier(0);
             }
+            s[i] *= sw;
         }
+        s_last = s[FM - 1];
+        stage = stage == NST - 1 ? 0 : stage + 1;
     }
+    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));             // nothing is on its way to LDS when the block ends
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[FM - 1][j][e] += prod[1][j][e] * s_last;
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
         const int m = m0 + wm * TM + i * 16 + c;
@@ -256,6 +311,7 @@ static LinearPlan linear_plan(int M, int N, int K)
     else {
         const int tiles = ceil_div(M, 128) * ceil_div(N, 128), nk = ceil_div(K, 128);
         while (L.ksplit < 8 && tiles * L.ksplit * 2 <= 256 && nk / (L.ksplit * 2) >= 4) L.ksplit *= 2;
+        L.ksplit = ceil_div(nk, ceil_div(nk, L.ksplit));  // no slice is empty
     }
     return L;
 }
