@@ -74,7 +74,7 @@ moe_status moe_quantize_weight(const void *w, int32_t N, int32_t K, void *w8, fl
  *   x8 [M][K] e4m3, rows x_stride apart (a multiple of 16); x_scale [ceil(K/128)][x_scale_stride >= M] (as moe_rms_norm
  *   and moe_quantize_rows write them); w8 [N][K] e4m3 dense; w_scale [ceil(N/128)][ceil(K/128)];
  *   out [M][N] bf16, rows out_stride apart (any; 2-byte aligned).
- * K a multiple of 16 (MOE_ERR_SHAPE).  The workspace holds partial sums where the work is split along K:
+ * K a multiple of 16 (MOE_ERR_SHAPE); M <= 2^21, N, K <= 2^20, x_stride <= 2^23 (MOE_ERR_UNSUPPORTED).  The workspace holds partial sums where the work is split along K:
  * moe_linear_workspace_size bytes (0 for many shapes) for exactly this M, N, K, 256-byte aligned.
  */
 typedef struct moe_linear_args {

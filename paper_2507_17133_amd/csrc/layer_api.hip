@@ -6,7 +6,8 @@
 namespace bmoe {
 namespace {
 
-constexpr int64_t kMaxDim = (int64_t)1 << 24;     // rows, and 2^20 columns: tile counts stay in 32 bits
+constexpr int32_t kMaxRows = 1 << 21, kMaxColumns = 1 << 20;     // tile counts and grids stay within what launches take
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 23;               // a tile's offsets stay in 32 bits
 
 bool off(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
@@ -67,7 +68,7 @@ moe_status check_linear(int32_t M, int32_t N, int32_t K)
 {
     if (M < 0) return MOE_ERR_INVALID_ARG;
     if (N < 1 || K < 16 || K % 16 != 0) return MOE_ERR_SHAPE;
-    if (M > kMaxDim || N > (1 << 20) || K > (1 << 20)) return MOE_ERR_UNSUPPORTED;
+    if (M > kMaxRows || N > kMaxColumns || K > kMaxColumns) return MOE_ERR_UNSUPPORTED;
     return MOE_OK;
 }
 
@@ -137,6 +138,7 @@ moe_status moe_linear_e4m3(const moe_linear_args* a, void* workspace, size_t wor
     if (off(a->x8, 16) || off(a->w8, 16) || off(a->x_scale, 4) || off(a->w_scale, 4) || off(a->out, 2) || bad_stride(a->x_stride, 16))
         return MOE_ERR_ALIGNMENT;
     if (a->x_scale_stride < a->M || a->out_stride < 0 || (a->M > 1 && a->out_stride < a->N)) return MOE_ERR_SHAPE;
+    if (a->x_stride > kMaxRowBytes) return MOE_ERR_UNSUPPORTED;
     const size_t need = linear_workspace_bytes(a->M, a->N, a->K);
     if (need > 0 && (!workspace || workspace_bytes < need)) return MOE_ERR_WORKSPACE;
     if (need > 0 && off(workspace, 256)) return MOE_ERR_ALIGNMENT;

@@ -10,6 +10,7 @@
 #include "layer.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace bmoe {
 
@@ -21,10 +22,11 @@ struct LinearArgs {
     const uint8_t *x, *w;
     const float *xs, *ws;
     bf16_t* out;
-    float* part;                                          // [ksplit][M][N] where K is cut
+    float* part;                                          // [ksplit][M][part_stride] where K is cut
     int64_t x_stride, xs_stride, out_stride;
     int M, N, K, nk;                                      // nk: blocks of K
     int tiles_m, tiles_n, group_m, ksplit;
+    int part_stride;                                      // N in whole quads
     int vec;                                              // out rows take 8-byte stores
 };
 
@@ -52,90 +54,143 @@ __device__ __forceinline__ void store4(const LinearArgs& p, int m, int n, const 
 }
 
 // ------------------------------------------------------------------------------------------------
-// Few rows (at most 64), or short K: every block takes 16 columns and 16 MT rows, its eight waves take the blocks of K by turns and are
-// summed through LDS in wave order.  Operands come straight from memory into registers and are widened to bf16 (exact) on the way to
-// four 16x16x32 bf16 MFMAs per block of K, which add up in fp32.  (The 8-bit MFMA drops what lies below 2^-13 of the largest product it
-// adds up at a time; over whole blocks of 128 that averages out, over a few k's it does not.)  Bound by the weights' stream.
+// Few rows (at most 64), or short K: a block takes 16 NT columns and 16 MT rows, its eight waves take the blocks of K by turns and are
+// summed through LDS in wave order.  Operands come straight from memory into registers, DEPTH blocks of K ahead.  Bound by the weights'
+// stream, and for few columns by the latency of a wave's few trips to memory.
+// WIDE (K up to kShortK): operands are widened to bf16 (exact) for four 16x16x32 bf16 MFMAs per block of K, which add up in fp32.  The 8-bit
+// MFMA drops what lies below 2^-13 of the largest product it adds up at a time: over many k's that is 1/100 of the result's rounding to
+// bf16, over a few it is not.
 // ------------------------------------------------------------------------------------------------
 constexpr int kRowWaves = 8;
-constexpr int kShortK = 256;                              // up to here every shape goes this way
+constexpr int kShortK = 256;
 
-__device__ __forceinline__ unsigned widen_lo(unsigned w) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)); }
-__device__ __forceinline__ unsigned widen_hi(unsigned w) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)); }
-__device__ __forceinline__ bf16x8 widen8(unsigned a, unsigned b)
+__device__ __forceinline__ bf16x8 widen8(int a, int b)
 {
-    return __builtin_bit_cast(bf16x8, make_uint4(widen_lo(a), widen_hi(a), widen_lo(b), widen_hi(b)));
+    auto two = [](int w, auto high) {
+        return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)w, 1.0f, decltype(high)::value));
+    };
+    return __builtin_bit_cast(bf16x8, make_uint4(two(a, std::false_type{}), two(a, std::true_type{}), two(b, std::false_type{}), two(b, std::true_type{})));
 }
 
-template <int MT>
+template <bool WIDE>
+__device__ __forceinline__ f32x4 block_product(const i32x8 w, const i32x8 x)
+{
+    if constexpr (!WIDE) return mfma_block(w, x);
+    f32x4 t = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[2 * q], w[2 * q + 1]), widen8(x[2 * q], x[2 * q + 1]), t, 0, 0, 0);
+    return t;
+}
+
+template <int MT, int NT, int DEPTH, bool WIDE>
 __global__ void __launch_bounds__(kRowWaves * 64) linear_rows_kernel(LinearArgs p)
 {
-    __shared__ f32x4 sums[kRowWaves][MT][64];
+    __shared__ f32x4 sums[kRowWaves][MT * NT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * MT;
-    const uint8_t* wrow = p.w + (int64_t)min(n0 + c, p.N - 1) * p.K;
-    const uint8_t* xrow[MT];
+    const int n0 = blockIdx.x * 16 * NT, m0 = blockIdx.y * 16 * MT;
+    const uint8_t *wrow[NT], *xrow[MT];
     const float* srow[MT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) wrow[j] = p.w + (int64_t)min(n0 + 16 * j + c, p.N - 1) * p.K;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
         const int m = min(m0 + 16 * i + c, p.M - 1);
         xrow[i] = p.x + (int64_t)m * p.x_stride;
         srow[i] = p.xs + m;
     }
-    const float* wscale = p.ws + (int64_t)(n0 / kScaleGroup) * p.nk;
-    f32x4 acc[MT];
+    const float* wscale = p.ws + (int64_t)(n0 / kScaleGroup) * p.nk;          // 16 NT columns are in one block of 128
+    f32x4 acc[MT][NT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int b = wave; b < p.nk; b += kRowWaves) {
-        const int k0 = b * 128 + 16 * g, k1 = k0 + 64;
-        const bool in0 = k0 < p.K, in1 = k1 < p.K;
-        const uint4 z = make_uint4(0, 0, 0, 0);
-        auto pair = [&](const uint8_t* row, uint4& a, uint4& c2) {
-            a = in0 ? *reinterpret_cast<const uint4*>(row + k0) : z;
-            c2 = in1 ? *reinterpret_cast<const uint4*>(row + k1) : z;
-        };
-        uint4 w0, w1;
-        pair(wrow, w0, w1);
-        const float sw = wscale[b];
-        const bf16x8 w[4] = {widen8(w0.x, w0.y), widen8(w0.z, w0.w), widen8(w1.x, w1.y), widen8(w1.z, w1.w)};
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    uint4 w[DEPTH][NT][2], x[DEPTH][MT][2];
+    float s[DEPTH][MT], sw[DEPTH];
+    // chunks past K are the row's last one again, cleared below
+    auto load = [&](int d, int b) {
+        const int k0 = min(b * 128 + 16 * g, p.K - 16), k1 = min(b * 128 + 64 + 16 * g, p.K - 16);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            w[d][j][0] = *reinterpret_cast<const uint4*>(wrow[j] + k0);
+            w[d][j][1] = *reinterpret_cast<const uint4*>(wrow[j] + k1);
+        }
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-            uint4 x0, x1;
-            pair(xrow[i], x0, x1);
-            const float s = sw * srow[i][(int64_t)b * p.xs_stride];
-            f32x4 t = f32x4{0.f, 0.f, 0.f, 0.f};
-            t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[0], widen8(x0.x, x0.y), t, 0, 0, 0);
-            t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[1], widen8(x0.z, x0.w), t, 0, 0, 0);
-            t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[2], widen8(x1.x, x1.y), t, 0, 0, 0);
-            t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[3], widen8(x1.z, x1.w), t, 0, 0, 0);
+            x[d][i][0] = *reinterpret_cast<const uint4*>(xrow[i] + k0);
+            x[d][i][1] = *reinterpret_cast<const uint4*>(xrow[i] + k1);
+            s[d][i] = srow[i][(int64_t)b * p.xs_stride];
+        }
+        sw[d] = wscale[b];
+    };
+    auto add = [&](int d, int b) {
+        if (b * 128 + 128 > p.K) {
+            const bool out0 = b * 128 + 16 * g >= p.K, out1 = b * 128 + 64 + 16 * g >= p.K;
+            const uint4 z = make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][e] += t[e] * s;
+            for (int j = 0; j < NT; ++j) {
+                if (out0) w[d][j][0] = z;
+                if (out1) w[d][j][1] = z;
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if (out0) x[d][i][0] = z;
+                if (out1) x[d][i][1] = z;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const f32x4 t = block_product<WIDE>(operand(w[d][j][0], w[d][j][1]), operand(x[d][i][0], x[d][i][1]));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] += t[e] * (s[d][i] * sw[d]);
+            }
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (wave + d * kRowWaves < p.nk) load(d, wave + d * kRowWaves);
+    for (int b0 = wave; b0 < p.nk; b0 += DEPTH * kRowWaves) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int b = b0 + d * kRowWaves, next = b + DEPTH * kRowWaves;
+            if (b < p.nk) add(d, b);
+            if (next < p.nk) load(d, next);
         }
     }
 #pragma unroll
-    for (int i = 0; i < MT; ++i) sums[wave][i][lane] = acc[i];
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sums[wave][i * NT + j][lane] = acc[i][j];
     __syncthreads();
-    for (int u = threadIdx.x; u < MT * 64; u += kRowWaves * 64) {
-        const int i = u >> 6, l = u & 63;
-        f32x4 v = sums[0][i][l];
+    for (int u = threadIdx.x; u < MT * NT * 64; u += kRowWaves * 64) {
+        const int q = u >> 6, l = u & 63;
+        f32x4 v = sums[0][q][l];
 #pragma unroll
-        for (int w = 1; w < kRowWaves; ++w) {
+        for (int k = 1; k < kRowWaves; ++k) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += sums[w][i][l][e];
+            for (int e = 0; e < 4; ++e) v[e] += sums[k][q][l][e];
         }
         const float o[4] = {v[0], v[1], v[2], v[3]};
-        store4(p, m0 + 16 * i + (l & 15), n0 + 4 * (l >> 4), o);
+        store4(p, m0 + 16 * (q / NT) + (l & 15), n0 + 16 * (q % NT) + 4 * (l >> 4), o);
     }
 }
 
+template <int MT, int NT, int DEPTH>
+static void rows_go(const LinearArgs& p, hipStream_t s)
+{
+    const dim3 grid(ceil_div(p.N, 16 * NT), ceil_div(p.M, 16 * MT)), block(kRowWaves * 64);
+    if (p.K <= kShortK) hipLaunchKernelGGL((linear_rows_kernel<MT, NT, 1, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((linear_rows_kernel<MT, NT, DEPTH, false>), grid, block, 0, s, p);
+}
+
 // ------------------------------------------------------------------------------------------------
-// Tiles of BM x BN, WM x WN waves, a ring of NST stages of one block of K in LDS, filled by direct loads.  A tile row is 128 bytes = eight
-// 16-byte chunks; chunk c of row r is stored in slot c ^ (r / 2 & 7), so the 16 lanes that the LDS serves together (16 rows, one
-// chunk) fall on 16 different bank groups.
+// Tiles of BM x BN, WM x WN waves; blocks of K in LDS, filled by direct loads.  A tile row is 128 bytes = eight 16-byte chunks; chunk c of row r is
+// stored in slot c ^ (r / 2 & 7), so the 16 lanes that the LDS serves together (16 rows, one chunk) fall on 16 different bank groups.
 // ------------------------------------------------------------------------------------------------
 // Direct loads to LDS, 16 or 4 bytes per lane: base (wave-uniform) + off -> lds + 16 (4) lane.  Written as instructions because the compiler puts a
-// wait for every such load in flight before each LDS read (it cannot tell their targets apart).  They have no result register; the kernel
-// waits for them by count before the barrier that hands their stage over.  Nothing else in the kernel uses m0.
+// wait for every such load in flight before each LDS read (it cannot tell their targets apart).  They have no result register; the kernels
+// wait for them by count before the barrier that hands their target over.  Nothing else in these kernels uses m0.
 __device__ __forceinline__ void load_lds16(const uint8_t* base, unsigned off, unsigned lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base));
@@ -145,61 +200,145 @@ __device__ __forceinline__ void load_lds4(const uint8_t* base, unsigned off, uns
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base));
 }
 
-template <int BM, int BN, int WM, int WN, int NST>
-__global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
-{
-    constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
-    constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LD = LA + LB + 1;       // loads of a wave and block of K
-    constexpr int TILE = (BM + BN) * 128, STAGE = TILE + BM * 4;
-    static_assert(NW % 2 == 0 && LA >= 1 && LB >= 1 && TN <= kScaleGroup && BM % 64 == 0 && NST * STAGE <= 160 * 1024, "shape");
-    extern __shared__ __attribute__((aligned(16))) char smem[];
-    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
+// What the kernels below have in common: a block's tile, its loads, fragments, scales and results.
+template <int BM, int BN, int WM, int WN>
+struct TileWork {
+    static constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, FM = TM / 16, FN = TN / 16;
+    static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW;  // loads of a wave and block of K: rows, columns
+    static constexpr int STAGE = (BM + BN) * 128;             // a block of K in LDS
+    static_assert(NW % 2 == 0 && LA >= 1 && LB >= 1 && TN <= kScaleGroup && kScaleGroup % TN == 0 && BM % 64 == 0 && FM % 2 == 0, "shape");
+    const LinearArgs& p;
+    int lane, wave, g, c, wm, wn, m0, n0, slice, nk;          // nk: blocks of K of this slice
+    int last, whole, chunk_at, back, k_tail;                  // last: the block that K ends in, -1: none; whole: blocks without it
+    unsigned oa[LA], ob[LB], os;
+    const uint8_t *xbase, *wbase, *sbase;
+    const float* wscale;
+    float w64;
+
+    __device__ __forceinline__ TileWork(const LinearArgs& args) : p(args) {}
 
     // Block -> tile: each XCD (block id mod 8) gets a contiguous range of tiles; group_m M tiles x all N tiles follow each other, M
     // fastest, so that the blocks an XCD runs at a time share rows of both operands in its L2.
-    const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.ksplit, chunk = (total + 7) >> 3;
-    const int L0 = ((int)blockIdx.x & 7) * chunk + ((int)blockIdx.x >> 3);
-    if (((int)blockIdx.x >> 3) >= chunk || L0 >= total) return;
-    const int slice = L0 / tiles, L = L0 - slice * tiles;
-    const int per_group = p.group_m * p.tiles_n, grp = L / per_group, in = L - grp * per_group;
-    const int gm = min(p.group_m, p.tiles_m - grp * p.group_m);
-    const int nt = in / gm, mt = grp * p.group_m + in - nt * gm;
-    const int m0 = mt * BM, n0 = nt * BN;
-    const int k_per = (p.nk + p.ksplit - 1) / p.ksplit, kb0 = min(p.nk, slice * k_per), nk = min(p.nk, kb0 + k_per) - kb0;
+    __device__ __forceinline__ bool find()
+    {
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        g = lane >> 4;
+        c = lane & 15;
+        wm = wave / WN;
+        wn = wave % WN;
+        const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.ksplit, chunk = (total + 7) >> 3;
+        const int L0 = ((int)blockIdx.x & 7) * chunk + ((int)blockIdx.x >> 3);
+        if (((int)blockIdx.x >> 3) >= chunk || L0 >= total) return false;
+        slice = L0 / tiles;
+        const int L = L0 - slice * tiles, per_group = p.group_m * p.tiles_n, grp = L / per_group, in = L - grp * per_group;
+        const int gm = min(p.group_m, p.tiles_m - grp * p.group_m), nt = in / gm, mt = grp * p.group_m + in - nt * gm;
+        m0 = mt * BM;
+        n0 = nt * BN;
+        const int k_per = (p.nk + p.ksplit - 1) / p.ksplit, kb0 = slice * k_per;
+        nk = min(p.nk, kb0 + k_per) - kb0;
+        // A load is a wave-uniform base plus a lane's offset.  Rows past the end are the last one again (never stored); chunks past K, in the last
+        // block, are the row's last one again and are cleared in LDS.
+        const int r8 = lane >> 3;
+        chunk_at = ((lane & 7) ^ ((4 * (wave & 1) + (r8 >> 1)) & 7)) * 16;
+        k_tail = p.K & 127;
+        last = (k_tail != 0 && kb0 + nk == p.nk) ? nk - 1 : -1;
+        whole = last < 0 ? nk : nk - 1;
+        back = max(0, chunk_at - (k_tail - 16));
+#pragma unroll
+        for (int i = 0; i < LA; ++i) oa[i] = (unsigned)min((wave + i * NW) * 8 + r8, p.M - 1 - m0) * (unsigned)p.x_stride + chunk_at;
+#pragma unroll
+        for (int i = 0; i < LB; ++i) ob[i] = (unsigned)min((wave + i * NW) * 8 + r8, p.N - 1 - n0) * (unsigned)p.K + chunk_at;
+        os = (unsigned)min((wave & (BM / 64 - 1)) * 64 + lane, p.M - 1 - m0) * 4;
+        xbase = p.x + (int64_t)m0 * p.x_stride + (int64_t)kb0 * 128;
+        wbase = p.w + (int64_t)n0 * p.K + (int64_t)kb0 * 128;
+        sbase = reinterpret_cast<const uint8_t*>(p.xs + (int64_t)kb0 * p.xs_stride + m0);
+        wscale = p.ws + (int64_t)(min(n0 + wn * TN, p.N - 1) / kScaleGroup) * p.nk + kb0;
+        w64 = 0.0f;
+        return true;
+    }
+    // Load i of the rows, of the columns, and that of the rows' scales (64 per wave) of block k.
+    __device__ __forceinline__ void load_rows(int k, int i, unsigned stage) const
+    {
+        load_lds16(xbase + (int64_t)k * 128, oa[i] - (k == last ? back : 0), stage + (wave + i * NW) * 1024);
+    }
+    __device__ __forceinline__ void load_columns(int k, int i, unsigned stage) const
+    {
+        load_lds16(wbase + (int64_t)k * 128, ob[i] - (k == last ? back : 0), stage + BM * 128 + (wave + i * NW) * 1024);
+    }
+    __device__ __forceinline__ void load_scales(int k, unsigned to) const
+    {
+        load_lds4(sbase + (int64_t)k * p.xs_stride * 4, os, to + (wave & (BM / 64 - 1)) * 256);
+    }
+    // Clears what this wave loaded in place of columns past K.
+    __device__ __forceinline__ void clear_tail(char* stage) const
+    {
+        if (chunk_at < k_tail) return;
+#pragma unroll
+        for (int i = 0; i < LA + LB; ++i) *reinterpret_cast<uint4*>(stage + (wave + i * NW) * 1024 + lane * 16) = make_uint4(0, 0, 0, 0);
+    }
+    // Fragments of 16 rows or columns: a lane's chunks g and 4 + g.
+    __device__ __forceinline__ i32x8 fragment(const char* St, int row) const
+    {
+        const int swz = (c >> 1) & 7;
+        const char* at = St + (row + c) * 128;
+        return operand(*reinterpret_cast<const uint4*>(at + ((g ^ swz) << 4)), *reinterpret_cast<const uint4*>(at + (((4 + g) ^ swz) << 4)));
+    }
+    __device__ __forceinline__ i32x8 rows(const char* St, int i) const { return fragment(St, wm * TM + i * 16); }
+    __device__ __forceinline__ i32x8 columns(const char* St, int j) const { return fragment(St, BM + wn * TN + j * 16); }
+    __device__ __forceinline__ float row_scale(const char* scales, int i) const { return reinterpret_cast<const float*>(scales)[wm * TM + i * 16 + c]; }
+    // The columns' scale of block kt (ascending): 64 blocks at a time, lane l has block l's.  (A load in every block would be waited for
+    // with all those on their way to LDS: 128 x 128 tiles, 256 rows by 14336 x 4096, 47 -> 30 us.)
+    __device__ __forceinline__ float column_scale(int kt)
+    {
+        if ((kt & 63) == 0) {
+            w64 = wscale[min(kt + lane, nk - 1)];
+            asm volatile("" : "+v"(w64));                     // waited for here
+        }
+        return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w64), kt & 63));
+    }
+    __device__ __forceinline__ void store(const f32x4 (&acc)[FM][FN]) const
+    {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            const int m = m0 + wm * TM + i * 16 + c;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int n = n0 + wn * TN + j * 16 + 4 * g;
+                const float o[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                if (p.ksplit == 1) store4(p, m, n, o);
+                else if (m < p.M && n < p.N)
+                    *reinterpret_cast<float4*>(p.part + ((int64_t)slice * p.M + m) * p.part_stride + n) = make_float4(o[0], o[1], o[2], o[3]);
+            }
+        }
+    }
+};
 
-    // A load is a wave-uniform base plus a lane's offset.  Rows past the end are the last one again (never stored); chunks past K, in the last
-    // block, are the row's last one again and are cleared in LDS.
-    const int r8 = lane >> 3, chunk_at = ((lane & 7) ^ ((4 * (wave & 1) + (r8 >> 1)) & 7)) * 16;
-    const int k_tail = p.K & 127, last = (k_tail != 0 && kb0 + nk == p.nk) ? nk - 1 : -1;       // the block that K ends in
-    const int back = max(0, chunk_at - (k_tail - 16));
-    unsigned oa[LA], ob[LB];
+// A ring of NST stages.  A block of K is FM steps; step i multiplies 16 rows by the wave's columns.  Behind each MFMA stand the multiply-adds of the
+// step before (left to itself the compiler has all MFMAs first, and the matrix pipe idles for as long as the multiply-adds take), the
+// reads of the next step's rows and, in the first steps, the loads of the block NST - 1 ahead.
+template <int BM, int BN, int WM, int WN, int NST>
+__global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
+{
+    using W = TileWork<BM, BN, WM, WN>;
+    constexpr int FM = W::FM, FN = W::FN, LA = W::LA, LB = W::LB, LD = LA + LB + 1, STAGE = W::STAGE + BM * 4;
+    static_assert((NST - 2) * LD <= 63 && NST * STAGE <= 160 * 1024, "shape");
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    W t(p);
+    if (!t.find()) return;
+    const int nk = t.nk;
+    // half of the loads of block k into stage st
+    auto issue = [&](int k, int st, int half) {
+        const unsigned to = lds0 + st * STAGE;
 #pragma unroll
-    for (int i = 0; i < LA; ++i) oa[i] = (unsigned)min((wave + i * NW) * 8 + r8, p.M - 1 - m0) * (unsigned)p.x_stride + chunk_at;
-#pragma unroll
-    for (int i = 0; i < LB; ++i) ob[i] = (unsigned)min((wave + i * NW) * 8 + r8, p.N - 1 - n0) * (unsigned)p.K + chunk_at;
-    const uint8_t* xbase = p.x + (int64_t)m0 * p.x_stride + (int64_t)kb0 * 128;
-    const uint8_t* wbase = p.w + (int64_t)n0 * p.K + (int64_t)kb0 * 128;
-    const int piece = wave & (BM / 64 - 1);               // 64 rows' scales
-    const unsigned os = (unsigned)min(piece * 64 + lane, p.M - 1 - m0) * 4;
-    const uint8_t* sbase = reinterpret_cast<const uint8_t*>(p.xs + (int64_t)kb0 * p.xs_stride + m0);
-    // part of FM of the loads of block kt into stage st
-    auto issue = [&](int kt, int st, int part) {
-        const unsigned to = lds0 + st * STAGE, less = kt == last ? back : 0;
-        const uint8_t *wk = wbase + (int64_t)kt * 128, *xk = xbase + (int64_t)kt * 128;
-#pragma unroll
-        for (int i = 0; i < LD; ++i) {
-            if (i * FM / LD != part) continue;
-            if (i < LB) load_lds16(wk, ob[i < LB ? i : 0] - less, to + BM * 128 + (wave + i * NW) * 1024);
-            else if (i < LB + LA) load_lds16(xk, oa[i < LB ? 0 : i < LB + LA ? i - LB : 0] - less, to + (wave + (i - LB) * NW) * 1024);
-            else load_lds4(sbase + (int64_t)kt * p.xs_stride * 4, os, to + TILE + piece * 256);
+        for (int u = 0; u < LD; ++u) {
+            if (u * 2 / LD != half) continue;
+            if (u < LB) t.load_columns(k, u < LB ? u : 0, to);
+            else if (u < LB + LA) t.load_rows(k, u < LB ? 0 : u < LB + LA ? u - LB : 0, to);
+            else t.load_scales(k, to + W::STAGE);
         }
     };
-
-    const int wm = wave / WN, wn = wave % WN;
-    const int swz = (c >> 1) & 7, s0 = (g ^ swz) << 4, s1 = ((4 + g) ^ swz) << 4;
-    const int a_off = (wm * TM + c) * 128, b_off = (BM + wn * TN + c) * 128;
-    const float* wscale = p.ws + (int64_t)(min(n0 + wn * TN, p.N - 1) / kScaleGroup) * p.nk + kb0;
     f32x4 acc[FM][FN], prod[2][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -207,145 +346,285 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < FN; ++j) prod[0][j] = prod[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float s[FM], s_last = 0.0f;                           // scales of the rows; of the last 16 rows of the block before
-
-    // A block of K: step i multiplies 16 rows by the wave's columns.  Behind each MFMA stand the multiply-adds of the step before, and in the
-    // steps the reads of the next step's rows and the loads of the block after next, one at a time.  The compiler would rather have all
-    // MFMAs first, which leaves the matrix pipe idle for as long as the multiply-adds take.
-    static_assert(FM % 2 == 0, "the last step's products are in the second set");
+    float s[FM], s_before = 0.0f;                         // scales of the rows; of the step before
 #pragma unroll
     for (int st = 0; st < NST - 1; ++st)
 #pragma unroll
-        for (int i = 0; i < FM; ++i) issue(min(st, nk - 1), st, i);
+        for (int half = 0; half < 2; ++half) issue(min(st, nk - 1), st, half);
     int stage = 0;
     for (int kt = 0; kt < nk; ++kt) {
-        const float sw = wscale[kt];
+        const float sw = t.column_scale(kt);
         __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm((NST - 2) * LD));
         lds_barrier();                                    // block kt is there; everyone has read block kt - 1
-        const char* St = smem + stage * STAGE;
+        char* St = smem + stage * STAGE;
         const int free = stage == 0 ? NST - 1 : stage - 1;
-        if (kt == last) {                                 // what was loaded in place of columns past K
-            char* mine = smem + stage * STAGE + wave * 1024 + lane * 16;
-            if (chunk_at >= k_tail) {
-#pragma unroll
-                for (int i = 0; i < LA + LB; ++i) *reinterpret_cast<uint4*>(mine + i * NW * 1024) = make_uint4(0, 0, 0, 0);
-            }
+        if (kt == t.last) {
+            t.clear_tail(St);
             __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0)
             lds_barrier();
         }
-        const int next = min(kt + NST - 1, nk - 1);       // past the end: the last block again, never read
+        const int ahead = min(kt + NST - 1, nk - 1);      // past the end: the last block again, never read
         i32x8 fb[FN], fa[2];
-        auto frag = [&](int at) {
-            return operand(*reinterpret_cast<const uint4*>(St + at + s0), *reinterpret_cast<const uint4*>(St + at + s1));
-        };
-        fa[0] = frag(a_off);
+        fa[0] = t.rows(St, 0);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) fb[j] = frag(b_off + j * 2048);
+        for (int j = 0; j < FN; ++j) fb[j] = t.columns(St, j);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) s[i] = *reinterpret_cast<const float*>(St + TILE + (wm * TM + i * 16 + c) * 4);
+        for (int i = 0; i < FM; ++i) s[i] = t.row_scale(St + W::STAGE, i);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const float sp = i == 0 ? s_last : s[i - 1];
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
                 prod[i & 1][j] = mfma_block(fb[j], fa[i & 1]);
                 __builtin_amdgcn_sched_barrier(0);
-                if (j == 0 && i + 1 < FM) fa[(i + 1) & 1] = frag(a_off + (i + 1) * 2048);
-                if (j == FN / 2) issue(next, free, i);
+                if (j == 0 && i + 1 < FM) fa[(i + 1) & 1] = t.rows(St, i + 1);
+                if (j == FN / 2 && i < 2) issue(ahead, free, i);
                 f32x4& into = acc[i == 0 ? FM - 1 : i - 1][j];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) into[e] += prod[(i + 1) & 1][j][e] * sp;
+                for (int e = 0; e < 4; ++e) into[e] += prod[(i + 1) & 1][j][e] * s_before;
                 __builtin_amdgcn_sched_barrier(0);
             }
-            s[i] *= sw;
+            s_before = s[i] * sw;
         }
-        s_last = s[FM - 1];
         stage = stage == NST - 1 ? 0 : stage + 1;
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));             // nothing is on its way to LDS when the block ends
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[FM - 1][j][e] += prod[1][j][e] * s_last;
+        for (int e = 0; e < 4; ++e) acc[FM - 1][j][e] += prod[1][j][e] * s_before;
+    t.store(acc);
+}
+
+// 256 x 256: two blocks of K are all that LDS holds, so a load that waits for a whole block to be read has less than a block's time.  The
+// columns' fragments stay in registers for the block, so their LDS is free soon after the block has begun, and that of the first half of each
+// wave's rows halfway.  Hence two barriers per block:
+//   before the middle step  the second half of the rows of this block has landed; the columns and the first half have been read by everyone,
+//                           and the block after next is loaded in their place;
+//   before the last step    the columns and the first half of the next block have landed; the second half of this one has been read, and that
+//                           of the block after next is loaded.  The last step's MFMAs run while the next block's first operands come in, each in place
+//                           of one that has been used for the last time.
+// So every load has about one and a half blocks' time.  16384 x 7168 x 7168 725 us (2323 TFLOP/s), in the ring kernel above with two stages 760;
+// without its loads 0.53 ms.  The LDS bounds it: 192 KB of reads and 64 KB of writes per block of 2048 MFMA cycles, where a wave tile of 128 x 64 is what
+// leaves room for accumulators that the multiply-adds reach (they cannot address the accumulation registers).
+template <int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(WM * WN * 64) linear_wide_kernel(LinearArgs p)
+{
+    using W = TileWork<BM, BN, WM, WN>;
+    constexpr int NW = W::NW, TM = W::TM, FM = W::FM, FN = W::FN, LA = W::LA, LB = W::LB, STAGE = W::STAGE;
+    constexpr int EARLY = LA / 2 + LB + 1, LATE = LA / 2; // loads behind the middle barrier (first halves, columns, scales), behind the last one
+    constexpr int SCALES = 2 * STAGE;
+    static_assert(SCALES + 3 * BM * 4 <= 160 * 1024, "LDS of a CU");
+    static_assert(FM >= 4 && LA % 2 == 0 && TM / 2 % (NW * 8) == 0, "a load's rows are in one half of a wave's rows");
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
+    W t(p);
+    if (!t.find()) return;
+    const int most = max(t.whole - 1, 0);
+    // Load u of block kt: 0 .. EARLY - 1 the first halves of the rows, the columns and the scales, then the second halves.  Blocks past the end are the
+    // last one again and never read.
+    auto load = [&](int kt, int st, int slot, int u) {
+        const int k = min(kt, most);
+        const unsigned to = lds0 + st * STAGE;
+        constexpr int RUN = TM / 2 / (NW * 8);            // loads of one half of a wave's rows follow each other
+        const int v = u < LATE ? u : u - EARLY;
+        const int i = v / RUN * 2 * RUN + v % RUN + (u < LATE ? 0 : RUN);
+        if (u < LATE || u >= EARLY) t.load_rows(k, u < LATE || u >= EARLY ? i : 0, to);
+        else if (u < EARLY - 1) t.load_columns(k, u - LATE, to);
+        else t.load_scales(k, lds0 + SCALES + slot * BM * 4);
+    };
+    // all but the youngest EARLY + LATE loads of every wave have landed, and every wave's reads are done
+    auto hand_over = [&]() {
+        __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm(EARLY + LATE));
+        lds_barrier();
+    };
+    auto scale_of = [&](int slot, int i) { return t.row_scale(smem + SCALES + slot * BM * 4, i); };
+    f32x4 acc[FM][FN], prod[2][FN];
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-        const int m = m0 + wm * TM + i * 16 + c;
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-            const int n = n0 + wn * TN + j * 16 + 4 * g;
-            const float o[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-            if (p.ksplit == 1) {
-                store4(p, m, n, o);
-            } else if (m < p.M) {
-                float* dst = p.part + ((int64_t)slice * p.M + m) * p.N + n;
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (n + e < p.N) dst[e] = o[e];
+    for (int j = 0; j < FN; ++j) prod[0][j] = prod[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    i32x8 fb[FN], fa[2];
+    float row_scale[2], s_before = 0.0f;
+#pragma unroll
+    for (int u = 0; u < EARLY + LATE; ++u) load(0, 0, 0, u);
+#pragma unroll
+    for (int u = 0; u < EARLY; ++u) load(1, 1, 1, u);
+    hand_over();
+#pragma unroll
+    for (int u = EARLY; u < EARLY + LATE; ++u) load(1, 1, 1, u);
+    fa[0] = t.rows(smem, 0);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) fb[j] = t.columns(smem, j);
+    row_scale[0] = scale_of(0, 0);
+    int slot = 0;                                         // scales have a third place: they are read to the end of their block
+    for (int kt = 0; kt < t.whole; ++kt) {
+        const float sw = t.column_scale(kt);
+        const int st = kt & 1, next_slot = slot == 2 ? 0 : slot + 1, free_slot = slot == 0 ? 2 : slot - 1;
+        const char *St = smem + st * STAGE, *Sn = smem + (st ^ 1) * STAGE;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            if (i == FM / 2 - 1 || i == FM - 1) hand_over();
+            const float s = row_scale[i & 1] * sw;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                prod[i & 1][j] = mfma_block(fb[j], fa[i & 1]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (j == 0) {
+                    fa[(i + 1) & 1] = i + 1 < FM ? t.rows(St, i + 1) : t.rows(Sn, 0);
+                    row_scale[(i + 1) & 1] = i + 1 < FM ? scale_of(slot, i + 1) : scale_of(next_slot, 0);
+                }
+                if (i == FM - 1) fb[j] = t.columns(Sn, j);
+                // one load at a time: several in a row queue up and hold the wave, and the MFMAs behind them
+                constexpr int FIRST = (FM / 2 - 1) * FN, SPAN = FM / 2 * FN, LAST = (FM - 1) * FN;
+                const int at = i * FN + j;
+#pragma unroll
+                for (int u = 0; u < EARLY; ++u)
+                    if (at == FIRST + u * SPAN / EARLY) load(kt + 2, st, free_slot, u);
+#pragma unroll
+                for (int u = 0; u < LATE; ++u)
+                    if (at == LAST + u * FN / LATE) load(kt + 2, st, free_slot, EARLY + u);
+                f32x4& into = acc[i == 0 ? FM - 1 : i - 1][j];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) into[e] += prod[(i + 1) & 1][j][e] * s_before;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            s_before = s;
+        }
+        slot = next_slot;
+    }
+    __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm(0));       // nothing is on its way to LDS, or being read there
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[FM - 1][j][e] += prod[1][j][e] * s_before;
+    if (t.last >= 0) {                                    // the block that K ends in, by itself
+        lds_barrier();
+#pragma unroll
+        for (int i = 0; i < LB; ++i) t.load_columns(t.last, i, lds0);
+#pragma unroll
+        for (int i = 0; i < LA; ++i) t.load_rows(t.last, i, lds0);
+        t.load_scales(t.last, lds0 + SCALES);
+        __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+        t.clear_tail(smem);
+        __syncthreads();
+        const float sw = t.wscale[t.last];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fb[j] = t.columns(smem, j);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            fa[0] = t.rows(smem, i);
+            const float s = scale_of(0, i) * sw;
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const f32x4 v = mfma_block(fb[j], fa[0]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] += v[e] * s;
             }
         }
     }
+    t.store(acc);
 }
 
-// Sum of the slices of K, in their order.
+// Sum of the slices of K, in their order: a thread has four columns of a row.
 __global__ void __launch_bounds__(256) linear_sum_kernel(LinearArgs p)
 {
-    const int64_t plane = (int64_t)p.M * p.N, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= plane) return;
-    float v = p.part[i];
-    for (int z = 1; z < p.ksplit; ++z) v += p.part[z * plane + i];
-    const int64_t m = i / p.N;
-    p.out[m * p.out_stride + (i - m * p.N)] = (bf16_t)v;
+    const int quads = p.part_stride / 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, m = i / quads;
+    if (m >= p.M) return;
+    const int n = (int)(i - m * quads) * 4;
+    const float4* src = reinterpret_cast<const float4*>(p.part + m * p.part_stride + n);
+    const int64_t plane = (int64_t)p.M * quads;
+    float4 v = src[0];
+    for (int z = 1; z < p.ksplit; ++z) {
+        const float4 u = src[z * plane];
+        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    const float o[4] = {v.x, v.y, v.z, v.w};
+    store4(p, (int)m, n, o);
 }
 
 // ------------------------------------------------------------------------------------------------
-struct LinearPlan { int kind, bm, bn, ksplit; };          // kind 0: rows kernel, 1: tiles
+template <int BM, int BN, int WM, int WN, int NST>
+struct RingTile {
+    static constexpr int kM = BM, kN = BN, kThreads = WM * WN * 64;
+    static constexpr size_t kLds = (size_t)NST * ((BM + BN) * 128 + BM * 4);
+    static constexpr auto kernel = &linear_tile_kernel<BM, BN, WM, WN, NST>;
+};
+struct WideTile {
+    static constexpr int kM = 256, kN = 256, kThreads = 512;
+    static constexpr size_t kLds = 2 * 512 * 128 + 3 * 256 * 4;
+    static constexpr auto kernel = &linear_wide_kernel<256, 256, 2, 4>;
+};
 
+// The ways to cut the product into tiles; all but the first leave room for one block per CU.
+enum { kRows, kTile64, kTile64x128, kTile128, kTile128x256, kTile256, kWays };
+template <typename F>
+static auto with_tile(int way, F&& f)
+{
+    switch (way) {
+        case kTile64: return f(RingTile<64, 64, 2, 2, 5>{});
+        case kTile64x128: return f(RingTile<64, 128, 2, 4, 6>{});
+        case kTile128: return f(RingTile<128, 128, 2, 4, 4>{});
+        case kTile128x256: return f(RingTile<128, 256, 2, 4, 3>{});
+        default: return f(WideTile{});
+    }
+}
+
+struct LinearPlan { int way, ksplit, rows, columns; };    // rows, columns: of the rows kernel's blocks
+
+// The way that should take the least time.  A CU works on one tile at a time, so a product takes rounds of tiles; a tile takes 2 us (its first loads,
+// its store) and for every block of K what is listed, from products of 2048 to 16384 rows; a launch takes 2 us.  Small tiles may be cut along K
+// as well, which costs a second launch and the partial sums' way to memory and back.  Foretold and measured (us), K blocks:
+//   64 x 64      0.32   256 rows by 6144 x 4096 26.5, 27.4; 1024 by 4096 x 7168 81.7, 82.7
+//   64 x 128     0.47   256 by 6144 x 4096 19.0, 19.4;      1024 by 4096 x 7168 58.6, 55.8
+//   128 x 128    0.65   1024 by 4096 x 7168 40.4, 41.2;     4096 by 4096 x 4096 93, 97
+//   128 x 256    1.06   2048 by 4096 x 4096 37.9, 40.3;     16384 by 7168 x 7168 861, 867
+//   256 x 256    1.77   4096 by 4096 x 4096 60.6, 63.9;     16384 by 7168 x 7168 710, 708
+// Up to 64 rows there is the rows kernel: its time goes with the weights, and from 33 rows on with the rows' trips as well.
 static LinearPlan linear_plan(int M, int N, int K)
 {
-    LinearPlan L{0, 0, 0, 1};
-    if (M <= 64 || K <= kShortK) return L;
-    L.kind = 1;
-    L.bm = L.bn = 128;
-    if ((int64_t)ceil_div(M, 256) * ceil_div(N, 256) >= 200) L.bm = L.bn = 256;
-    else {
-        const int tiles = ceil_div(M, 128) * ceil_div(N, 128), nk = ceil_div(K, 128);
-        while (L.ksplit < 8 && tiles * L.ksplit * 2 <= 256 && nk / (L.ksplit * 2) >= 4) L.ksplit *= 2;
-        L.ksplit = ceil_div(nk, ceil_div(nk, L.ksplit));  // no slice is empty
-    }
-    return L;
+    LinearPlan best{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 0};
+    best.columns = ceil_div(N, 32) * ceil_div(M, best.rows) >= 192 ? 32 : 16;
+    if (M <= 32 || K <= kShortK) return best;
+    static constexpr struct { int m, n; double block; } kTile[kWays] = {
+        {0, 0, 0}, {64, 64, 0.32}, {64, 128, 0.47}, {128, 128, 0.65}, {128, 256, 1.06}, {256, 256, 1.77}};
+    constexpr int kCus = 256;
+    const int nk = ceil_div(K, kScaleGroup);
+    double least = M <= 64 ? 4.0 + 0.46e-6 * N * K : 1e300;
+    for (int way = kTile64; way < kWays; ++way)
+        for (int ks = 1; ks <= (way == kTile64 ? 16 : 1); ks *= 2) {
+            const int per = ceil_div(nk, ks);
+            if (ks > 1 && (per < 4 || ceil_div(nk, per) != ks)) continue;          // no slice is empty
+            const int64_t tiles = (int64_t)ceil_div(M, kTile[way].m) * ceil_div(N, kTile[way].n) * ks;
+            double us = 2.0 + (double)((tiles + kCus - 1) / kCus) * (per * kTile[way].block + 2.0);
+            if (ks > 1) us += 2.5 + 2e-6 * M * N * ks;
+            if (us < least) {
+                least = us;
+                best = {way, ks, 0, 0};
+            }
+        }
+    return best;
 }
 
 size_t linear_workspace_bytes(int M, int N, int K)
 {
     const LinearPlan L = linear_plan(M, N, K);
-    return L.ksplit > 1 ? align_up((size_t)L.ksplit * M * N * sizeof(float), 256) : 0;
+    return L.ksplit > 1 ? align_up((size_t)L.ksplit * M * align_up(N, 4) * sizeof(float), 256) : 0;
 }
-
-template <int BM, int BN, int WM, int WN, int NST>
-struct TileKernel {
-    static constexpr size_t kLds = (size_t)NST * ((BM + BN) * 128 + BM * 4);
-    static hipError_t init()
-    {
-        return hipFuncSetAttribute(reinterpret_cast<const void*>(&linear_tile_kernel<BM, BN, WM, WN, NST>),
-                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)kLds);
-    }
-    static void go(LinearArgs& p, hipStream_t s)
-    {
-        p.tiles_m = ceil_div(p.M, BM);
-        p.tiles_n = ceil_div(p.N, BN);
-        p.group_m = 8;
-        const int total = p.tiles_m * p.tiles_n * p.ksplit;
-        hipLaunchKernelGGL((linear_tile_kernel<BM, BN, WM, WN, NST>), dim3((total + 7) / 8 * 8), dim3(WM * WN * 64), kLds, s, p);
-    }
-};
-using Tile256 = TileKernel<256, 256, 2, 4, 2>;
-using Tile128 = TileKernel<128, 128, 2, 2, 3>;
 
 hipError_t init_linear_kernels()
 {
-    hipError_t e = Tile256::init();
-    return e != hipSuccess ? e : Tile128::init();
+    for (int way = kTile64; way < kWays; ++way) {
+        hipError_t e = with_tile(way, [](auto tile) {
+            return hipFuncSetAttribute(reinterpret_cast<const void*>(tile.kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)tile.kLds);
+        });
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s)
@@ -357,22 +636,27 @@ hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s)
     p.out = static_cast<bf16_t*>(a.out);
     p.part = static_cast<float*>(ws);
     p.x_stride = a.x_stride; p.xs_stride = a.x_scale_stride; p.out_stride = a.out_stride;
-    p.M = a.M; p.N = a.N; p.K = a.K; p.nk = ceil_div(a.K, 128);
+    p.M = a.M; p.N = a.N; p.K = a.K; p.nk = ceil_div(a.K, kScaleGroup);
     p.ksplit = L.ksplit;
+    p.part_stride = (int)align_up(a.N, 4);
     p.vec = (a.out_stride & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 7u) == 0;
-    if (L.kind == 0) {
-        const int mt = a.M <= 16 ? 1 : a.M <= 32 ? 2 : 4;
-        const dim3 grid(ceil_div(a.N, 16), ceil_div(a.M, 16 * mt)), block(kRowWaves * 64);
-        if (mt == 1) hipLaunchKernelGGL((linear_rows_kernel<1>), grid, block, 0, s, p);
-        else if (mt == 2) hipLaunchKernelGGL((linear_rows_kernel<2>), grid, block, 0, s, p);
-        else hipLaunchKernelGGL((linear_rows_kernel<4>), grid, block, 0, s, p);
+    if (L.way == kRows) {
+        const bool two = L.columns == 32;
+        if (L.rows == 16) two ? rows_go<1, 2, 3>(p, s) : rows_go<1, 1, 4>(p, s);
+        else if (L.rows == 32) two ? rows_go<2, 2, 3>(p, s) : rows_go<2, 1, 4>(p, s);
+        else two ? rows_go<4, 2, 2>(p, s) : rows_go<4, 1, 2>(p, s);
         return hipGetLastError();
     }
-    if (L.bm == 256) Tile256::go(p, s);
-    else Tile128::go(p, s);
-    hipError_t e = hipGetLastError();
+    hipError_t e = with_tile(L.way, [&](auto tile) {
+        p.tiles_m = ceil_div(p.M, tile.kM);
+        p.tiles_n = ceil_div(p.N, tile.kN);
+        p.group_m = 8;
+        const int total = p.tiles_m * p.tiles_n * p.ksplit;
+        hipLaunchKernelGGL(tile.kernel, dim3((total + 7) / 8 * 8), dim3(tile.kThreads), tile.kLds, s, p);
+        return hipGetLastError();
+    });
     if (e != hipSuccess || L.ksplit == 1) return e;
-    hipLaunchKernelGGL(linear_sum_kernel, dim3((unsigned)(((int64_t)a.M * a.N + 255) / 256)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(linear_sum_kernel, dim3((unsigned)(((int64_t)a.M * (p.part_stride / 4) + 255) / 256)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 

@@ -75,7 +75,8 @@ def _linear(**kw):
 @pytest.mark.parametrize("change,status", [
     (dict(M=0), OK), (dict(M=-1), INVALID), (dict(x8=None), INVALID), (dict(w_scale=None), INVALID), (dict(out=None), INVALID),
     (dict(K=250), SHAPE), (dict(K=0), SHAPE), (dict(N=0), SHAPE), (dict(x8=P + 8), ALIGN), (dict(x_stride=264), ALIGN), (dict(out=P + 1), ALIGN),
-    (dict(x_scale=P + 2), ALIGN), (dict(x_scale_stride=7), SHAPE), (dict(out_stride=127), SHAPE), (dict(N=(1 << 20) + 1), UNSUPPORTED)])
+    (dict(x_scale=P + 2), ALIGN), (dict(x_scale_stride=7), SHAPE), (dict(out_stride=127), SHAPE), (dict(N=(1 << 20) + 1), UNSUPPORTED),
+    (dict(M=(1 << 21) + 1, x_scale_stride=1 << 22), UNSUPPORTED), (dict(x_stride=(1 << 23) + 16), UNSUPPORTED)])
 def test_linear_refusals(change, status):
     assert L._lib().moe_linear_e4m3(_linear(**change), P, 1 << 40, None) == status
 
