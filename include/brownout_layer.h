@@ -94,7 +94,7 @@ moe_status moe_linear_e4m3(const moe_linear_args *a, void *workspace, size_t wor
  * may be stored token by token or head by head.  Strides are 16-byte multiples.
  * A sequence's block table row lists the pages of its positions 0, page_size, 2*page_size, ...
  * With type MOE_KV_E4M3 a stored value c of head h stands for c * k_scale[h] (v_scale[h]); with MOE_KV_BF16 the scales
- * are ignored.
+ * are ignored.  k and v span at most 64 GiB each (MOE_ERR_UNSUPPORTED beyond).
  */
 #define MOE_KV_BF16 0
 #define MOE_KV_E4M3 1

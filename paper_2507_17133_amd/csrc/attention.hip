@@ -20,6 +20,7 @@
 #include "layer.h"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace bmoe {
 
@@ -28,12 +29,14 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kAttnWaves = 4, kAttnThreads = 64 * kAttnWaves;
 constexpr int kStep = 32;                         // positions of a wave's step
-constexpr int kTile = kStep * kAttnWaves;         // positions of a block's step
 constexpr int kAttnBlocks = 512;                  // shares at most
+template <int D>
+constexpr int kAttnResident = 2;  // blocks of a CU
 
 struct AttnArgs {
     const uint8_t *kc, *vc;
-    int64_t page_stride, token_stride, head_stride;
+    int64_t head_stride;
+    unsigned page_step, token_step;               // a page's and a position's stride in 16-byte steps
     const float *k_scale, *v_scale;
     const int32_t *pages, *token_row;
     int64_t row_stride;
@@ -44,14 +47,15 @@ struct AttnArgs {
     const bf16_t* q;
     int64_t q_stride;
     const int32_t* lengths;
-    int T, H, Hk, group, q_tiles, heads;          // heads: query heads of a work item (at most 16)
+    int T, H, Hk, group, q_tiles, heads;          // heads: query heads of a key head that a wave takes (at most 16)
+    int side, tile;                               // key heads side by side in a block; positions of its step
     float scale;
     int window;
     bf16_t* out;
     int64_t out_stride;
     float* lse;
     int4* cuts;                                   // per share: the item that it begins and does not end (token, item, shares, -)
-    float* parts;                                 // per share two parts: [heads][D] O, [heads] m, [heads] l
+    float* parts;                                 // per share two places of [side] parts: [heads][D] O, [heads] m, [heads] l
 };
 
 // Positions [lo, hi) that token t attends to.
@@ -62,7 +66,8 @@ __device__ __forceinline__ int2 span_of(const AttnArgs& p, int t)
     const bool there = (unsigned)row < (unsigned)p.n_rows;
     return make_int2(p.window > 0 ? max(hi - p.window, 0) : 0, there ? hi : 0);
 }
-__device__ __forceinline__ int tiles_of(const int2 s) { return s.y > s.x ? (int)(((unsigned)(s.y - s.x) + kTile - 1) / kTile) : 0; }
+__device__ __forceinline__ int tiles_of(const AttnArgs& p, const int2 s) { return s.y > s.x ? (int)((unsigned)(s.y - s.x - 1) / (unsigned)p.tile) + 1 : 0; }
+__device__ __forceinline__ int items_of(const AttnArgs& p) { return p.Hk / p.side * p.q_tiles; }
 
 // The block's share of the line of tiles: its bounds, and where it begins.
 struct Share {
@@ -87,9 +92,9 @@ __device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t* lds)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int each = (p.T + kAttnThreads - 1) / kAttnThreads, t0 = min(p.T, tid * each), t1 = min(p.T, t0 + each);
-    const int items = p.Hk * p.q_tiles;
+    const int items = items_of(p);
     int64_t mine = 0;
-    for (int t = t0; t < t1; ++t) mine += (int64_t)tiles_of(span_of(p, t)) * items;
+    for (int t = t0; t < t1; ++t) mine += (int64_t)tiles_of(p, span_of(p, t)) * items;
     int64_t total;
     int64_t before = wave_sum_before(mine, lane, total);
     if (lane == 0) lds[wave] = total;
@@ -108,7 +113,7 @@ __device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t* lds)
     if (s.first < s.end && before <= s.first && s.first < before + mine) {
         int t = t0;
         for (;; ++t) {
-            const int64_t n = (int64_t)tiles_of(span_of(p, t)) * items;
+            const int64_t n = (int64_t)tiles_of(p, span_of(p, t)) * items;
             if (s.first < before + n) break;
             before += n;
         }
@@ -120,6 +125,56 @@ __device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t* lds)
     s.before = lds[kAttnWaves + 1];
     return s;
 }
+
+// A tile of the line: its token, item (key heads side by side, and which 16 of their query heads) and number within the item.
+struct Place {
+    int64_t at;                                   // its number in the line
+    int t, item, tile, n;                         // n: tiles of the token's items
+    int lo, hi;                                   // positions that the token attends to
+    int hk, h0, nh;                               // the wave's key head, its first query head and number of those
+    const int32_t* row;                           // the token's row of the block table
+
+    __device__ __forceinline__ void token(const AttnArgs& p)
+    {
+        const int2 s = span_of(p, t);
+        lo = s.x;
+        hi = s.y;
+        n = tiles_of(p, s);
+    }
+    __device__ __forceinline__ void heads(const AttnArgs& p, int sub)
+    {
+        const int set = p.q_tiles == 1 ? item : item / p.q_tiles;
+        hk = set * p.side + sub;
+        h0 = hk * p.group + (item - set * p.q_tiles) * 16;
+        nh = min(16, (hk + 1) * p.group - h0);
+        row = p.pages + (int64_t)(p.token_row ? p.token_row[t] : t) * p.row_stride;
+    }
+    __device__ __forceinline__ void start(const AttnArgs& p, const Share& s, int sub)
+    {
+        at = s.first;
+        t = s.token;
+        token(p);
+        item = (int)((at - s.before) / n);
+        tile = (int)(at - s.before - (int64_t)item * n);
+        heads(p, sub);
+    }
+    // to the next tile; false at the share's end
+    __device__ __forceinline__ bool step(const AttnArgs& p, const Share& s, int sub)
+    {
+        if (++at >= s.end) return false;
+        if (++tile < n) return true;
+        tile = 0;
+        if (++item == items_of(p)) {
+            item = 0;
+            do {
+                ++t;
+                token(p);
+            } while (n == 0);                     // ends: the share's tiles belong to tokens that have some
+        }
+        heads(p, sub);
+        return true;
+    }
+};
 
 // Two e4m3 -> two bf16 (exact), from the low or the high half of a word.
 template <bool HIGH>
@@ -136,11 +191,11 @@ struct KRows {
     uint4 w[2][P16 ? P16 : 1];
     uint2 tail[2][P8 ? P8 : 1];
 
-    __device__ __forceinline__ void load(const uint8_t* base, const int64_t* off, int g)
+    __device__ __forceinline__ void load(const uint8_t* base, const unsigned* off, int g)
     {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint8_t* row = base + off[h] * (E4M3 ? 1 : 2);
+            const uint8_t* row = base + (uint64_t)off[h] * 16;
 #pragma unroll
             for (int i = 0; i < P16; ++i) w[h][i] = *reinterpret_cast<const uint4*>(row + 64 * i + 16 * g);
             if constexpr (P8) tail[h][0] = *reinterpret_cast<const uint2*>(row + 64 * P16 + 8 * g);
@@ -170,10 +225,10 @@ struct VPart {
     struct __attribute__((aligned(BYTES))) Raw { uint8_t b[BYTES]; };
     Raw v[8];
 
-    __device__ __forceinline__ void load(const uint8_t* base, int c0, const int64_t* off, int c)
+    __device__ __forceinline__ void load(const uint8_t* base, int c0, const unsigned* off, int c)
     {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const Raw*>(base + (off[e] + c0 + c * N) * (E4M3 ? 1 : 2));
+        for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const Raw*>(base + (c0 + c * N) * (E4M3 ? 1 : 2) + (uint64_t)off[e] * 16);
     }
     // word i of position e: columns 2 i and 2 i + 1 in bf16
     __device__ __forceinline__ unsigned word(int e, int i) const
@@ -223,7 +278,7 @@ struct VRows {
     VPart<128, E4M3> a[N128 ? N128 : 1];
     VPart<64, E4M3> b;
     VPart<32, E4M3> c;
-    __device__ __forceinline__ void load(const uint8_t* base, const int64_t* off, int col)
+    __device__ __forceinline__ void load(const uint8_t* base, const unsigned* off, int col)
     {
 #pragma unroll
         for (int i = 0; i < N128; ++i) a[i].load(base, 128 * i, off, col);
@@ -237,34 +292,49 @@ struct VRows {
         if constexpr (N64) b.add(acc + 8 * N128, prob, all, keep);
         if constexpr (N32) c.add(acc + 8 * N128 + 4 * N64, prob, all, keep);
     }
-    // column of head_dim behind register r of acc[j]: a lane's are N in a row for each r
-    static __device__ __forceinline__ int column(int j, int r, int g)
+    // body(first column, how many in a row (8, 4 or 2), first of the accumulators that hold them, their register): a lane's results
+    template <typename F>
+    static __device__ __forceinline__ void runs(int g, F&& body)
     {
-        if (j < 8 * N128) return 128 * (j >> 3) + 8 * (4 * g + r) + (j & 7);
-        j -= 8 * N128;
-        if (j < 4 * N64) return 128 * N128 + 4 * (4 * g + r) + j;
-        return 128 * N128 + 64 * N64 + 2 * (4 * g + r) + j - 4 * N64;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+#pragma unroll
+            for (int i = 0; i < N128; ++i) body(128 * i + 8 * (4 * g + r), std::integral_constant<int, 8>{}, 8 * i, r);
+            if constexpr (N64) body(128 * N128 + 4 * (4 * g + r), std::integral_constant<int, 4>{}, 8 * N128, r);
+            if constexpr (N32) body(128 * N128 + 64 * N64 + 2 * (4 * g + r), std::integral_constant<int, 2>{}, 8 * N128 + 4 * N64, r);
+        }
     }
 };
 
+// N floats (8, 4 or 2) in a row, in whole vectors.
+template <int N>
+__device__ __forceinline__ void put(float* dst, const float* v)
+{
+    if constexpr (N == 2) *reinterpret_cast<float2*>(dst) = make_float2(v[0], v[1]);
+    else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    }
+}
+
 template <int D, bool E4M3>
-__global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(AttnArgs p)
+__global__ void __launch_bounds__(kAttnThreads, kAttnResident<D>) attention_kernel(AttnArgs p)
 {
     using K = KRows<D, E4M3>;
     using V = VRows<D, E4M3>;
     constexpr int NJ = D / 16;                            // products of V's columns
     extern __shared__ __attribute__((aligned(16))) char smem[];
     __shared__ int64_t found[kAttnWaves + 2];
-    __shared__ int64_t places[kAttnWaves][kStep];         // offset of a step's positions in the cache
+    __shared__ __attribute__((aligned(16))) unsigned places[kAttnWaves][kStep];      // where a step's positions are in the cache, in 16-byte steps
     __shared__ float stat[kAttnWaves][2][16];
-    float* joined = reinterpret_cast<float*>(smem);       // [waves][heads][D + 4]
+    float* joined = reinterpret_cast<float*>(smem);       // [waves behind the first side][heads][D + 4]
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int g = lane >> 4, c = lane & 15;
+    const int g = lane >> 4, c = lane & 15, sub = wave & (p.side - 1), behind = wave / p.side;       // key head, positions of the step
 
     // tokens with nothing to attend to
     for (int t = blockIdx.x; t < p.T; t += gridDim.x) {
-        if (tiles_of(span_of(p, t)) > 0) continue;
+        if (tiles_of(p, span_of(p, t)) > 0) continue;
         for (int i = tid * 4; i < p.H * D; i += kAttnThreads * 4)
             *reinterpret_cast<uint2*>(p.out + (int64_t)t * p.out_stride + i) = make_uint2(0, 0);
         if (p.lse)
@@ -275,96 +345,162 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(AttnArgs p)
     if (tid == 0) p.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (share.first >= share.end) return;
 
-    int t = share.token;
-    int64_t before = share.before;
-    int64_t at = share.first;
-    while (at < share.end) {
-        int2 span = span_of(p, t);
-        int n = tiles_of(span);
-        while (at >= before + (int64_t)n * p.Hk * p.q_tiles) {          // on to the next token that has tiles
-            before += (int64_t)n * p.Hk * p.q_tiles;
-            ++t;
-            span = span_of(p, t);
-            n = tiles_of(span);
-        }
-        const int item = (int)((at - before) / n);
-        const int64_t item_first = before + (int64_t)item * n;
-        const int i0 = (int)(at - item_first), i1 = (int)min((int64_t)n, share.end - item_first);
-        at = item_first + i1;
-        const int hk = item / p.q_tiles, h0 = hk * p.group + (item - hk * p.q_tiles) * 16;
-        const int nh = min(16, (hk + 1) * p.group - h0);
-
-        // q of my head, in the order of K's columns
-        bf16x8 q[K::S];
+    // The share's tiles follow each other without a stop: while one is worked on, the next one's K and V and the page numbers of the one after are on
+    // their way, also where that is another head's or another token's.
+    Place at;
+    at.start(p, share, sub);
+    bf16x8 q[K::S];
+    K kr;
+    V vr;
+    unsigned koff[2], voff[8];
+    // page of the lane's position (lanes 0..31) of the wave in a tile, -1 beyond the end
+    auto page_of = [&](const Place& w, unsigned& in_page) -> int {
+        const unsigned pos = (unsigned)w.lo + (unsigned)w.tile * p.tile + behind * kStep + (lane & 31);
+        in_page = 0;
+        if (pos >= (unsigned)w.hi) return -1;
+        const unsigned pg = (unsigned)((uint64_t)pos * p.page_magic >> p.page_shift);
+        in_page = pos - pg * (unsigned)p.page_size;
+        return w.row[pg];
+    };
+    // where those positions are, by way of LDS to the lanes that load them; returns which are there
+    auto place = [&](int page, unsigned in_page) -> unsigned {
+        const bool there = (unsigned)page < (unsigned)p.n_pages;
+        if (lane < kStep) places[wave][lane] = there ? (unsigned)page * p.page_step + in_page * p.token_step : 0;
+        wave_lds_order();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) koff[h] = places[wave][16 * h + c];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) voff[e] = places[wave][16 * (e >> 2) + 4 * g + (e & 3)];
+        wave_lds_order();
+        return (unsigned)__ballot(there);                 // lanes 0..31
+    };
+    auto load_q = [&](const Place& w) {                   // of my head, in the order of K's columns
 #pragma unroll
         for (int s = 0; s < K::S; ++s) {
-            uint4 w = make_uint4(0, 0, 0, 0);
-            if (c < nh) w = *reinterpret_cast<const uint4*>(p.q + (int64_t)t * p.q_stride + (int64_t)(h0 + c) * D + K::column(s, g));
-            q[s] = __builtin_bit_cast(bf16x8, w);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (c < w.nh) v = *reinterpret_cast<const uint4*>(p.q + (int64_t)w.t * p.q_stride + (int64_t)(w.h0 + c) * D + K::column(s, g));
+            q[s] = __builtin_bit_cast(bf16x8, v);
         }
-        const float to_log2 = p.scale * (E4M3 ? p.k_scale[hk] : 1.0f) * 1.4426950408889634f;
-        const int32_t* row = p.pages + (int64_t)(p.token_row ? p.token_row[t] : t) * p.row_stride;
-        const uint8_t* kbase = p.kc + (int64_t)hk * p.head_stride * (E4M3 ? 1 : 2);
-        const uint8_t* vbase = p.vc + (int64_t)hk * p.head_stride * (E4M3 ? 1 : 2);
+    };
+    auto head_base = [&](const uint8_t* cache, int hk) { return cache + (int64_t)hk * p.head_stride * (E4M3 ? 1 : 2); };
 
-        // page of lane's position of step i (lanes 0..31), -1 beyond the end
-        const unsigned first_pos = (unsigned)span.x + wave * kStep + (lane & 31);
-        auto page_of = [&](int i, unsigned& at_in_page) -> int {
-            const unsigned pos = first_pos + (unsigned)i * kTile;
-            at_in_page = 0;
-            if (pos >= (unsigned)span.y) return -1;
-            const unsigned pg = (unsigned)((uint64_t)pos * p.page_magic >> p.page_shift);
-            at_in_page = pos - pg * (unsigned)p.page_size;
-            return row[pg];
-        };
-        unsigned mask = 0, next_mask = 0;
-        int64_t koff[2], voff[8];
-        // the places of a step's positions, by way of LDS to the lanes that load them
-        auto place = [&](int page, unsigned at_in_page) -> unsigned {
-            const bool there = (unsigned)page < (unsigned)p.n_pages;
-            const int64_t off = there ? (int64_t)page * p.page_stride + (int64_t)at_in_page * p.token_stride : 0;
-            if (lane < kStep) places[wave][lane] = off;
-            wave_lds_order();
-#pragma unroll
-            for (int h = 0; h < 2; ++h) koff[h] = places[wave][16 * h + c];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) voff[e] = places[wave][16 * (e >> 2) + 4 * g + (e & 3)];
-            wave_lds_order();
-            return (unsigned)__ballot(there);             // lanes 0..31
-        };
-
-        f32x4 acc[NJ];
+    f32x4 acc[NJ];
+    float m, l, to_log2 = 0.0f;
+    auto begin_item = [&](const Place& w) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        float m = -__builtin_inff(), l = 0.0f;
-        K kr;
-        V vr;
-        // steps of this wave: all but perhaps the last tile, whose end may lie before its positions
-        int last = i1;
-        if ((int64_t)span.x + (int64_t)(i1 - 1) * kTile + wave * kStep >= span.y) --last;
-        unsigned in_page = 0;
-        int page = -1;
-        if (i0 < last) {
-            page = page_of(i0, in_page);
-            mask = place(page, in_page);
-            page = page_of(i0 + 1, in_page);
-            kr.load(kbase, koff, g);
-            vr.load(vbase, voff, c);
+        m = -__builtin_inff();
+        l = 0.0f;
+        to_log2 = p.scale * (E4M3 ? p.k_scale[w.hk] : 1.0f) * 1.4426950408889634f;
+    };
+    // The end of an item, or of what the share has of it: the waves of a key head are joined, and the first of them writes the output or a part in
+    // the workspace.  The next tile's loads stay in flight: barriers wait for LDS only.
+    auto lds_sync = [&]() {
+        __builtin_amdgcn_s_waitcnt(0xC07F);               // lgkmcnt(0)
+        lds_barrier();
+    };
+    auto finish_item = [&](const Place& w, int first_tile) {
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (p.side < kAttnWaves) {
+            if (g == 0) {
+                stat[wave][0][c] = m;
+                stat[wave][1][c] = l;
+            }
+            lds_sync();
+            float top = -__builtin_inff();
+            for (int k = sub; k < kAttnWaves; k += p.side) top = fmaxf(top, stat[k][0][c]);
+            const float ref = top == -__builtin_inff() ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - ref);
+            l = 0.0f;
+            for (int k = sub; k < kAttnWaves; k += p.side) l += stat[k][1][c] * __builtin_amdgcn_exp2f(stat[k][0][c] - ref);
+            m = top;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc[j][r] *= f;
+            if (behind > 0 && c < w.nh) {
+                float* dst = joined + ((wave - p.side) * p.heads + c) * (D + 4);
+                V::runs(g, [&](int col, auto n, int j, int r) {
+                    float v[n.value];
+#pragma unroll
+                    for (int i = 0; i < n.value; ++i) v[i] = acc[j + i][r];
+                    put<n.value>(dst + col, v);
+                });
+            }
+            lds_sync();
+            if (behind == 0 && c < w.nh)
+                for (int k = sub; k < kAttnWaves - p.side; k += p.side) {
+                    const float* src = joined + (k * p.heads + c) * (D + 4);
+                    V::runs(g, [&](int col, auto n, int j, int r) {
+#pragma unroll
+                        for (int i = 0; i < n.value; ++i) acc[j + i][r] += src[col + i];
+                    });
+                }
+            lds_sync();                                   // LDS is free for the next item
         }
-        for (int i = i0; i < last; ++i) {
-            f32x4 s[2];
+        if (behind > 0) return;
+        const bool begins = first_tile == 0, ends = w.tile + 1 == w.n;
+        if (begins && !ends && tid == 0) {
+            const int64_t last_share = (w.at - w.tile + w.n - 1) / share.per;
+            p.cuts[blockIdx.x] = make_int4(w.t, w.item, (int)(last_share - blockIdx.x) + 1, 0);
+        }
+        if (c >= w.nh) return;
+        if (begins && ends) {
+            const float k = l > 0.0f || l != l ? (E4M3 ? p.v_scale[w.hk] : 1.0f) / l : 0.0f;
+            bf16_t* dst = p.out + (int64_t)w.t * p.out_stride + (int64_t)(w.h0 + c) * D;
+            V::runs(g, [&](int col, auto n, int j, int r) {
+                if constexpr (n.value == 2) *reinterpret_cast<unsigned*>(dst + col) = pack_bf16(acc[j][r] * k, acc[j + 1][r] * k);
+                else {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    for (int i = 0; i < n.value; i += 4)
+                        *reinterpret_cast<uint2*>(dst + col + i) =
+                            make_uint2(pack_bf16(acc[j + i][r] * k, acc[j + i + 1][r] * k), pack_bf16(acc[j + i + 2][r] * k, acc[j + i + 3][r] * k));
+                }
+            });
+            if (p.lse && g == 0) p.lse[(int64_t)w.t * p.H + w.h0 + c] = (m + __log2f(l)) * 0.6931471805599453f;
+        } else {
+            float* part = p.parts + (((int64_t)2 * blockIdx.x + (begins ? 1 : 0)) * p.side + sub) * ((int64_t)p.heads * (D + 2));
+            V::runs(g, [&](int col, auto n, int j, int r) {
+                float v[n.value];
 #pragma unroll
-                for (int k = 0; k < K::S; ++k) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr.operand(h, k), q[k], s[h], 0, 0, 0);
+                for (int i = 0; i < n.value; ++i) v[i] = acc[j + i][r];
+                put<n.value>(part + c * D + col, v);
+            });
+            if (g == 0) {
+                part[p.heads * D + c] = m;
+                part[p.heads * D + p.heads + c] = l;
             }
-            const bool more = i + 1 < last;
-            if (more) {
-                next_mask = place(page, in_page);
-                page = page_of(i + 2, in_page);
-                kr.load(kbase, koff, g);
-            }
+        }
+    };
+    unsigned in_page, mask, next_mask = 0;
+    int page = page_of(at, in_page), first_tile = at.tile;
+    mask = place(page, in_page);
+    load_q(at);
+    kr.load(head_base(p.kc, at.hk), koff, g);
+    vr.load(head_base(p.vc, at.hk), voff, c);
+    begin_item(at);
+    Place next = at;
+    bool more = next.step(p, share, sub);
+    if (more) page = page_of(next, in_page);
+    for (;;) {
+        f32x4 s[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            s[h] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < K::S; ++k) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kr.operand(h, k), q[k], s[h], 0, 0, 0);
+        }
+        const bool same = more && next.item == at.item && next.t == at.t;
+        Place after = next;
+        bool more_after = false;
+        if (more) {
+            next_mask = place(page, in_page);
+            more_after = after.step(p, share, sub);
+            if (more_after) page = page_of(after, in_page);
+            if (!same) load_q(next);
+            kr.load(head_base(p.kc, next.hk), koff, g);
+        }
+        if (mask) {
             // scores in powers of two
             float top = -__builtin_inff();
             const bool all = mask == 0xFFFFFFFFu;
@@ -399,97 +535,51 @@ __global__ void __launch_bounds__(kAttnThreads, 2) attention_kernel(AttnArgs p)
                     l += e[4 * h + r];
                 }
             vr.add(acc, __builtin_bit_cast(bf16x8, pack_bf16x8(e)), all, keep);
-            if (more) {
-                vr.load(vbase, voff, c);
-                mask = next_mask;
-            }
         }
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-
-        // join the waves
-        if (g == 0) {
-            stat[wave][0][c] = m;
-            stat[wave][1][c] = l;
+        if (more) vr.load(head_base(p.vc, next.hk), voff, c);
+        if (!same) {
+            finish_item(at, first_tile);
+            if (!more) return;
+            first_tile = next.tile;
+            begin_item(next);
         }
-        __syncthreads();
-        float top = -__builtin_inff();
-#pragma unroll
-        for (int w = 0; w < kAttnWaves; ++w) top = fmaxf(top, stat[w][0][c]);
-        const float ref = top == -__builtin_inff() ? 0.0f : top, f = __builtin_amdgcn_exp2f(m - ref);
-        float sum = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kAttnWaves; ++w) sum += stat[w][1][c] * __builtin_amdgcn_exp2f(stat[w][0][c] - ref);
-        if (c < nh) {
-            float* dst = joined + (wave * p.heads + c) * (D + 4);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) dst[V::column(j, r, g)] = acc[j][r] * f;
-        }
-        __syncthreads();                                  // also: everyone has read stat
-        if (wave == 0 && g == 0) {
-            stat[0][0][c] = top;
-            stat[0][1][c] = sum;
-        }
-        __syncthreads();
-        const bool begins = i0 == 0, ends = i1 == n;
-        float* part = p.parts + ((int64_t)2 * blockIdx.x + (begins ? 1 : 0)) * ((int64_t)p.heads * (D + 2));
-        const float vs = E4M3 ? p.v_scale[hk] : 1.0f;
-        for (int i = tid * 4; i < nh * D; i += kAttnThreads * 4) {
-            const int h = i / D;
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int w = 0; w < kAttnWaves; ++w) {
-                const float4 v = *reinterpret_cast<const float4*>(joined + (w * p.heads + h) * (D + 4) + (i - h * D));
-                o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
-            }
-            if (begins && ends) {
-                const float total = stat[0][1][h], k = total > 0.0f || total != total ? vs / total : 0.0f;
-                *reinterpret_cast<uint2*>(p.out + (int64_t)t * p.out_stride + (int64_t)h0 * D + i) =
-                    make_uint2(pack_bf16(o.x * k, o.y * k), pack_bf16(o.z * k, o.w * k));
-            } else {
-                *reinterpret_cast<float4*>(part + i) = o;
-            }
-        }
-        if (tid < nh) {
-            const float top_h = stat[0][0][tid], sum_h = stat[0][1][tid];
-            if (begins && ends) {
-                if (p.lse) p.lse[(int64_t)t * p.H + h0 + tid] = (top_h + __log2f(sum_h)) * 0.6931471805599453f;
-            } else {
-                part[p.heads * D + tid] = top_h;
-                part[p.heads * D + p.heads + tid] = sum_h;
-            }
-        }
-        if (begins && !ends && tid == 0) {
-            const int64_t last_share = (item_first + n - 1) / share.per;
-            p.cuts[blockIdx.x] = make_int4(t, item, (int)(last_share - blockIdx.x) + 1, 0);
-        }
-        __syncthreads();                                  // LDS is free for the next item
+        mask = next_mask;
+        at = next;
+        next = after;
+        more = more_after;
     }
 }
 
-// Joins the parts of the item that share x begins and does not end: one block per (share, head of the item).
-template <int D>
+// Joins the parts of the item that share x begins and does not end.  SPREAD: a block of four waves for each head, where items are few and so cut
+// into many parts; else a wave for each head: hardly any then has more than two parts to read, and the launch's time goes with its blocks.
+template <int D, bool SPREAD>
 __global__ void __launch_bounds__(256) join_kernel(AttnArgs p, int e4m3)
 {
+    constexpr int THREADS = SPREAD ? 256 : 64, LANES = D / 4, ROWS = THREADS / LANES;      // threads of a head, of a row of O; rows side by side
+    __shared__ float4 rows[SPREAD ? 1 : 4][ROWS][LANES];
+    __shared__ float sums[SPREAD ? 1 : 4][ROWS], red[4];
     const int4 cut = p.cuts[blockIdx.x];
-    const int n = cut.z, hk = cut.y / p.q_tiles, h0 = hk * p.group + (cut.y - hk * p.q_tiles) * 16, h = blockIdx.y;
-    if (n == 0 || h >= min(16, (hk + 1) * p.group - h0)) return;
+    const int which = SPREAD ? 0 : threadIdx.x >> 6, y = SPREAD ? blockIdx.y : blockIdx.y * 4 + which, tid = threadIdx.x & (THREADS - 1);
+    const int n = cut.z, set = cut.y / p.q_tiles, sub = y / p.heads, h = y - sub * p.heads;
+    const int hk = set * p.side + sub, h0 = hk * p.group + (cut.y - set * p.q_tiles) * 16;
+    if (n == 0 || sub >= p.side || h >= min(16, (hk + 1) * p.group - h0)) return;          // all threads of the head
     const int64_t size = (int64_t)p.heads * (D + 2);
     // share x left its part in its second place, the others in their first
-    auto part = [&](int i) { return p.parts + (2 * ((int64_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * size; };
-    const int tid = threadIdx.x;
-    __shared__ float red[2][4];
+    auto part = [&](int i) { return p.parts + ((2 * ((int64_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * p.side + sub) * size; };
+    auto sync = [&]() {
+        if constexpr (SPREAD) __syncthreads();
+        else wave_lds_order();
+    };
     float top = -__builtin_inff();
-    for (int i = tid; i < n; i += 256) top = fmaxf(top, part(i)[p.heads * D + h]);
+    for (int i = tid; i < n; i += THREADS) top = fmaxf(top, part(i)[p.heads * D + h]);
 #pragma unroll
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if ((tid & 63) == 0) red[0][tid >> 6] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+    if constexpr (SPREAD) {
+        if ((tid & 63) == 0) red[tid >> 6] = top;
+        sync();
+        top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    }
     const float ref = top == -__builtin_inff() ? 0.0f : top;
-    constexpr int LANES = D / 4, ROWS = 256 / LANES;      // threads of a row of O; rows side by side
     const int r = tid / LANES, col = (tid - r * LANES) * 4;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.0f;
@@ -502,20 +592,16 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs p, int e4m3)
             o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
             sum += f * q[p.heads * D + p.heads + h];
         }
+        rows[which][r][col / 4] = o;
+        if (col == 0) sums[which][r] = sum;
     }
-    __shared__ float4 rows[ROWS][LANES];
-    __shared__ float sums[ROWS];
-    if (r < ROWS) {
-        rows[r][col / 4] = o;
-        if (col == 0) sums[r] = sum;
-    }
-    __syncthreads();
+    sync();
     if (r != 0) return;
 #pragma unroll
     for (int i = 1; i < ROWS; ++i) {
-        const float4 v = rows[i][col / 4];
+        const float4 v = rows[which][i][col / 4];
         o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
-        sum += sums[i];
+        sum += sums[which][i];
     }
     const float k = sum > 0.0f || sum != sum ? (e4m3 ? p.v_scale[hk] : 1.0f) / sum : 0.0f;
     *reinterpret_cast<uint2*>(p.out + (int64_t)cut.x * p.out_stride + (int64_t)(h0 + h) * D + col) =
@@ -525,25 +611,42 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs p, int e4m3)
 
 static int item_heads(int group) { return group < 16 ? group : 16; }
 
+// Key heads that the waves of a block take side by side.  Where a token's heads lie next to each other, heads that are read at different times
+// leave the memory's pages (and lines, where a row is no whole number of them) half used; side by side they share them, but every cut then
+// leaves as many parts to write and join.  So: while the parts are at most 1/50 of what a share reads (1/3 where rows share lines), both
+// at the table's full length.  One, two and four heads, us: 64 tokens, 32 over 8 heads of 128, 4096 to 8192 positions, page 16 303 / 289 / 285; 512 tokens,
+// 16 over 16, up to 200 positions 110 / 95 / 93; e4m3, 64 tokens, 16 over 16, up to 4000 139 / 131 / 125; one token, 131072 positions 111 / 107 / 111; 256 tokens,
+// 32 over 4, up to 2048 159 / 161 / 162; heads of 192, 16 tokens, 32 over 4, up to 8192 65 / 68 / 71; e4m3, heads of 96 33 / 28 / 29.  Stored head by
+// head: 64 tokens of 8192 356 / 363 / 375.
+static int heads_side_by_side(const moe_kv_cache& c, int heads, int64_t T, int64_t longest)
+{
+    if (c.n_kv_heads == 1 || c.head_stride >= c.token_stride) return 1;
+    const int row = c.head_dim * (c.type == MOE_KV_E4M3 ? 1 : 2);
+    const double share = (double)T * c.n_kv_heads * longest * 2 * row / kAttnBlocks, most = share * (row % 128 ? 0.33 : 0.02);
+    int side = 4;
+    while (side > 1 && (c.n_kv_heads % side != 0 || 16.0 * side * heads * c.head_dim > most)) side /= 2;
+    return side;
+}
+
 size_t attention_workspace_bytes(const moe_kv_cache& c, int T, int n_heads)
 {
-    (void)T;                                              // the shares are as many for every T
+    (void)T;                                              // the shares are as many for every T, and each has at most four heads' parts
     const int heads = item_heads(n_heads / c.n_kv_heads);
-    return align_up(kAttnBlocks * sizeof(int4), 256) + align_up((size_t)2 * kAttnBlocks * heads * (c.head_dim + 2) * sizeof(float), 256);
+    return align_up(kAttnBlocks * sizeof(int4), 256) + align_up((size_t)2 * kAttnBlocks * (c.n_kv_heads % 4 == 0 ? 4 : c.n_kv_heads % 2 == 0 ? 2 : 1) * heads * (c.head_dim + 2) * sizeof(float), 256);
 }
 
 // A row of O in LDS is 4 floats longer, so that the heads of a wave write to different banks.
 template <int D>
-static size_t attention_lds(int heads) { return (size_t)kAttnWaves * heads * (D + 4) * sizeof(float); }
+static size_t attention_lds(int heads, int side) { return (size_t)(kAttnWaves - side) * heads * (D + 4) * sizeof(float); }
 
 template <int D>
 static hipError_t attention_init()
 {
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_kernel<D, true>),
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)attention_lds<D>(16));
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)attention_lds<D>(16, 1));
     if (e != hipSuccess) return e;
     return hipFuncSetAttribute(reinterpret_cast<const void*>(&attention_kernel<D, false>),
-                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)attention_lds<D>(16));
+                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)attention_lds<D>(16, 1));
 }
 
 hipError_t init_attention_kernels()
@@ -558,12 +661,15 @@ hipError_t init_attention_kernels()
 template <int D>
 static hipError_t attention_go(const AttnArgs& p, bool e4m3, int grid, hipStream_t s)
 {
-    const size_t lds = attention_lds<D>(p.heads);
+    const size_t lds = attention_lds<D>(p.heads, p.side);
     if (e4m3) hipLaunchKernelGGL((attention_kernel<D, true>), dim3(grid), dim3(kAttnThreads), lds, s, p);
     else hipLaunchKernelGGL((attention_kernel<D, false>), dim3(grid), dim3(kAttnThreads), lds, s, p);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || grid == 1) return e;           // one share: nothing is cut
-    hipLaunchKernelGGL((join_kernel<D>), dim3(grid, p.heads), dim3(256), 0, s, p, e4m3 ? 1 : 0);
+    const int64_t items = (int64_t)p.T * (p.Hk / p.side) * p.q_tiles;
+    const int heads = p.heads * p.side;
+    if (items * 4 >= grid) hipLaunchKernelGGL((join_kernel<D, false>), dim3(grid, ceil_div(heads, 4)), dim3(256), 0, s, p, e4m3 ? 1 : 0);
+    else hipLaunchKernelGGL((join_kernel<D, true>), dim3(grid, heads), dim3(256), 0, s, p, e4m3 ? 1 : 0);
     return hipGetLastError();
 }
 
@@ -573,7 +679,10 @@ hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, con
 {
     AttnArgs p;
     p.kc = static_cast<const uint8_t*>(c.k); p.vc = static_cast<const uint8_t*>(c.v);
-    p.page_stride = c.page_stride; p.token_stride = c.token_stride; p.head_stride = c.head_stride;
+    const int per16 = c.type == MOE_KV_E4M3 ? 16 : 8;
+    p.head_stride = c.head_stride;
+    p.page_step = (unsigned)(c.page_stride / per16);
+    p.token_step = (unsigned)(c.token_stride / per16);
     p.k_scale = c.k_scale; p.v_scale = c.v_scale;
     p.pages = t.pages; p.token_row = t.token_row; p.row_stride = t.row_stride; p.n_rows = t.n_rows;
     p.n_pages = c.n_pages; p.page_size = c.page_size;
@@ -592,7 +701,9 @@ hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, con
     p.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(kAttnBlocks * sizeof(int4), 256));
     // no more shares than there can be tiles
     const int64_t longest = window > 0 ? std::min(window, p.cap) : p.cap;
-    const int64_t most = (int64_t)T * p.Hk * p.q_tiles * ((longest + kTile - 1) / kTile);
+    p.side = heads_side_by_side(c, p.heads, T, longest);
+    p.tile = kStep * kAttnWaves / p.side;
+    const int64_t most = (int64_t)T * (p.Hk / p.side) * p.q_tiles * ((longest + p.tile - 1) / p.tile);
     const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(most, kAttnBlocks));
     const bool e4m3 = c.type == MOE_KV_E4M3;
     switch (c.head_dim) {

@@ -1,6 +1,7 @@
 // C ABI of the operators around the MoE layer: argument checks, then the launch.
 #include "layer.h"
 
+#include <algorithm>
 #include <cmath>
 
 namespace bmoe {
@@ -48,6 +49,13 @@ moe_status check_cache(const moe_kv_cache* c)
     if ((c->n_pages > 1 && c->page_stride < c->head_dim) || (c->page_size > 1 && c->token_stride < c->head_dim) ||
         (c->n_kv_heads > 1 && c->head_stride < c->head_dim))
         return MOE_ERR_SHAPE;
+    // a position's place is held in 32 bits, in 16-byte steps
+    constexpr int64_t most = 0xFFFFFFFF;
+    const int64_t pages = c->n_pages - 1, positions = c->page_size - 1;
+    const int64_t page_step = pages ? c->page_stride / unit : 0, token_step = positions ? c->token_stride / unit : 0;
+    if (page_step > most / std::max<int64_t>(pages, 1) || token_step > most / std::max<int64_t>(positions, 1) ||
+        page_step * pages + token_step * positions > most)
+        return MOE_ERR_UNSUPPORTED;
     if (c->type == MOE_KV_E4M3) {
         if (!c->k_scale || !c->v_scale) return MOE_ERR_INVALID_ARG;
         if (off(c->k_scale, 4) || off(c->v_scale, 4)) return MOE_ERR_ALIGNMENT;

@@ -12,7 +12,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from .binding import _check, _ptr, _stream, lib
+from .binding import MOE_OK, _check, _ptr, lib
 
 E4M3 = torch.float8_e4m3fn
 MOE_KV_BF16, MOE_KV_E4M3 = 0, 1
@@ -81,10 +81,26 @@ def _lib():
     return _ready
 
 
-def _rows(t: torch.Tensor, dtype, cols: int):
+# The calls below are a few microseconds of GPU time for a single token, so the Python around them is kept short: a raw stream handle (a
+# torch.cuda.Stream object costs as much as a launch), no checks of what was allocated here, no error path on the way to success.
+_current_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _on(stream, t: torch.Tensor):
+    return _current_stream(t.get_device()) if stream is None else stream.cuda_stream
+
+
+def _rows(t: torch.Tensor, dtype, rows: int, cols: int):
     """A [rows, cols] tensor whose rows are contiguous; returns its row stride."""
-    assert t.is_cuda and t.dtype == dtype and t.dim() == 2 and t.shape[1] == cols and (cols == 1 or t.stride(1) == 1)
+    assert t.is_cuda and t.dtype is dtype and t.shape == (rows, cols)
+    if t.is_contiguous():
+        return cols
+    assert cols == 1 or t.stride(1) == 1
     return t.stride(0)
+
+
+def _like(t: torch.Tensor, dtype=torch.bfloat16) -> torch.Tensor:
+    return torch.empty_like(t, dtype=dtype) if t.is_contiguous() else torch.empty(t.shape, dtype=dtype, device=t.device)
 
 
 def _groups(d: int) -> int:
@@ -101,62 +117,69 @@ class NormOut(NamedTuple):
 
 
 def alloc_norm_out(T: int, d: int, want=("y",), residual: bool = False, device="cuda") -> NormOut:
-    bf = dict(dtype=torch.bfloat16, device=device)
+    bf, f32 = torch.bfloat16, torch.float32
     q = "y8" in want
-    return NormOut(torch.empty((T, d), **bf) if "y" in want else None, torch.empty((T, d), dtype=E4M3, device=device) if q else None,
-                   torch.empty((_groups(d), T), dtype=torch.float32, device=device) if q else None,
-                   torch.empty((T, d), **bf) if residual else None)
+    return NormOut(torch.empty((T, d), dtype=bf, device=device) if "y" in want else None,
+                   torch.empty((T, d), dtype=E4M3, device=device) if q else None,
+                   torch.empty(((d + 127) // 128, T), dtype=f32, device=device) if q else None,
+                   torch.empty((T, d), dtype=bf, device=device) if residual else None)
 
 
-def _norm_args(x, out: NormOut) -> moe_norm_args:
+def _norm(call, x, weight, eps, residual, want, out, stream) -> NormOut:
     T, d = x.shape
-    a = moe_norm_args(x=x.data_ptr(), x_stride=_rows(x, torch.bfloat16, d), T=T, d=d)
+    bf = torch.bfloat16
+    xs, xp = _rows(x, bf, T, d), x.data_ptr()
+    r = rs = w = y = ys = y8 = y8s = s = ss = ro = ros = None
+    if residual is not None:
+        r, rs = residual.data_ptr(), _rows(residual, bf, T, d)
+    if weight is not None:
+        assert weight.is_cuda and weight.dtype is bf and weight.shape == (d,) and weight.is_contiguous()
+        w = weight.data_ptr()
+    if out is None:
+        q = "y8" in want
+        out = NormOut(_like(x) if "y" in want else None, _like(x, E4M3) if q else None,
+                      torch.empty(((d + 127) // 128, T), dtype=torch.float32, device=x.device) if q else None,
+                      _like(x) if residual is not None else None)
+        ys = y8s = ros = d
+        ss = T
+    else:
+        if out.y is not None:
+            ys = _rows(out.y, bf, T, d)
+        if out.y8 is not None:
+            y8s, ss = _rows(out.y8, E4M3, T, d), _rows(out.scale, torch.float32, (d + 127) // 128, T)
+        if out.residual is not None:
+            ros = _rows(out.residual, bf, T, d)
     if out.y is not None:
-        assert out.y.shape[0] == T
-        a.y, a.y_stride = out.y.data_ptr(), _rows(out.y, torch.bfloat16, d)
+        y = out.y.data_ptr()
     if out.y8 is not None:
-        assert out.y8.shape[0] == T and out.scale.shape[0] == _groups(d)
-        a.y8, a.y8_stride = out.y8.data_ptr(), _rows(out.y8, E4M3, d)
-        a.scale, a.scale_stride = out.scale.data_ptr(), _rows(out.scale, torch.float32, T)
-    return a
+        y8, s = out.y8.data_ptr(), out.scale.data_ptr()
+    if out.residual is not None:
+        ro = out.residual.data_ptr()
+    st = call(C.byref(moe_norm_args(xp, xs, r, rs or 0, w, ro, ros or 0, y, ys or 0, y8, y8s or 0, s, ss or 0, T, d, eps)), _on(stream, x))
+    if st != MOE_OK:
+        _check(st, call.__name__)
+    return out
 
 
 def moe_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
                  want=("y",), out: Optional[NormOut] = None, stream=None) -> NormOut:
     """Norm of x + residual; `want`: "y" (bf16), "y8" (e4m3 with scales), or both.  The sum comes back as `residual` if one was given."""
-    T, d = x.shape
-    if out is None:
-        out = alloc_norm_out(T, d, want, residual is not None, x.device)
-    a = _norm_args(x, out)
-    a.eps = eps
-    if residual is not None:
-        assert residual.shape[0] == T
-        a.residual, a.residual_stride = residual.data_ptr(), _rows(residual, torch.bfloat16, d)
-    if weight is not None:
-        assert weight.is_cuda and weight.dtype == torch.bfloat16 and weight.shape == (d,) and weight.is_contiguous()
-        a.weight = weight.data_ptr()
-    if out.residual is not None:
-        assert out.residual.shape[0] == T
-        a.residual_out, a.residual_out_stride = out.residual.data_ptr(), _rows(out.residual, torch.bfloat16, d)
-    _check(_lib().moe_rms_norm(C.byref(a), _stream(stream)), "moe_rms_norm")
-    return out
+    return _norm((_ready or _lib()).moe_rms_norm, x, weight, eps, residual, want, out, stream)
 
 
 def moe_quantize_rows(x: torch.Tensor, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None):
     """(x8 [T][d] e4m3, scale [ceil(d/128)][T])."""
-    T, d = x.shape
-    o = alloc_norm_out(T, d, ("y8",), device=x.device) if out is None else NormOut(y8=out[0], scale=out[1])
-    _check(_lib().moe_quantize_rows(C.byref(_norm_args(x, o)), _stream(stream)), "moe_quantize_rows")
+    o = _norm((_ready or _lib()).moe_quantize_rows, x, None, 0.0, None, ("y8",), None if out is None else NormOut(y8=out[0], scale=out[1]), stream)
     return o.y8, o.scale
 
 
 def moe_quantize_weight(w: torch.Tensor, stream=None):
     """(w8 [N][K] e4m3, w_scale [ceil(N/128)][ceil(K/128)]) of a bf16 weight [N][K]."""
     N, K = w.shape
-    assert w.is_cuda and w.dtype == torch.bfloat16 and w.is_contiguous()
+    assert w.is_cuda and w.dtype is torch.bfloat16 and w.is_contiguous()
     w8 = torch.empty((N, K), dtype=E4M3, device=w.device)
     scale = torch.empty((_groups(N), _groups(K)), dtype=torch.float32, device=w.device)
-    _check(_lib().moe_quantize_weight(_ptr(w), N, K, _ptr(w8), _ptr(scale), _stream(stream)), "moe_quantize_weight")
+    _check(_lib().moe_quantize_weight(_ptr(w), N, K, _ptr(w8), _ptr(scale), _on(stream, w)), "moe_quantize_weight")
     return w8, scale
 
 
@@ -174,17 +197,21 @@ def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w
                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M, K = x8.shape
     N = w8.shape[0]
-    assert w8.is_cuda and w8.dtype == E4M3 and w8.shape == (N, K) and w8.is_contiguous()
-    assert w_scale.is_cuda and w_scale.dtype == torch.float32 and w_scale.shape == (_groups(N), _groups(K)) and w_scale.is_contiguous()
-    assert x_scale.shape[0] == _groups(K)
+    G = (K + 127) // 128
+    assert w8.is_cuda and w8.dtype is E4M3 and w8.shape[1] == K and w8.is_contiguous()
+    assert w_scale.is_cuda and w_scale.dtype is torch.float32 and w_scale.shape == (_groups(N), G) and w_scale.is_contiguous()
+    L = _ready or _lib()
     if out is None:
-        out = torch.empty((M, N), dtype=torch.bfloat16, device=x8.device)
-    assert out.shape[0] == M
+        out, out_stride = torch.empty((M, N), dtype=torch.bfloat16, device=x8.device), N
+    else:
+        out_stride = _rows(out, torch.bfloat16, M, N)
     if workspace is None:
         workspace = alloc_linear_workspace(M, N, K, x8.device)
-    a = moe_linear_args(x8.data_ptr(), _rows(x8, E4M3, K), x_scale.data_ptr(), _rows(x_scale, torch.float32, M), w8.data_ptr(),
-                        w_scale.data_ptr(), out.data_ptr(), _rows(out, torch.bfloat16, N), M, N, K)
-    _check(_lib().moe_linear_e4m3(C.byref(a), workspace.data_ptr(), workspace.numel(), _stream(stream)), "moe_linear_e4m3")
+    a = moe_linear_args(x8.data_ptr(), _rows(x8, E4M3, M, K), x_scale.data_ptr(), _rows(x_scale, torch.float32, G, M), w8.data_ptr(),
+                        w_scale.data_ptr(), out.data_ptr(), out_stride, M, N, K)
+    st = L.moe_linear_e4m3(C.byref(a), workspace.data_ptr(), workspace.numel(), _on(stream, x8))
+    if st != MOE_OK:
+        _check(st, "moe_linear_e4m3")
     return out
 
 
@@ -206,6 +233,7 @@ class KvCache:
         self.struct = moe_kv_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2),
                                    None if k_scale is None else k_scale.data_ptr(), None if v_scale is None else v_scale.data_ptr(),
                                    MOE_KV_E4M3 if e4m3 else MOE_KV_BF16, n, page, heads, dim)
+        self.heads, self.dim, self.ref = heads, dim, C.byref(self.struct)
 
 
 def alloc_kv_cache(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int, k_scale=None, v_scale=None, heads_first: bool = False,
@@ -217,13 +245,9 @@ def alloc_kv_cache(n_pages: int, page_size: int, n_kv_heads: int, head_dim: int,
     return KvCache(k.transpose(1, 2), v.transpose(1, 2), k_scale, v_scale) if heads_first else KvCache(k, v, k_scale, v_scale)
 
 
-def _table(block_table: torch.Tensor, token_row: Optional[torch.Tensor], T: int) -> moe_block_table:
-    assert block_table.is_cuda and block_table.dtype == torch.int32 and block_table.dim() == 2
-    assert block_table.shape[1] <= 1 or block_table.stride(1) == 1
-    if token_row is not None:
-        assert token_row.is_cuda and token_row.dtype == torch.int32 and token_row.shape == (T,) and token_row.is_contiguous()
-    return moe_block_table(block_table.data_ptr(), block_table.stride(0), None if token_row is None else token_row.data_ptr(),
-                           block_table.shape[0], block_table.shape[1])
+def _table(block_table: torch.Tensor, table_row: Optional[torch.Tensor], T: int) -> moe_block_table:
+    rows, pages = block_table.shape
+    return moe_block_table(block_table.data_ptr(), _rows(block_table, torch.int32, rows, pages), None if table_row is None else _ints(table_row, T), rows, pages)
 
 
 def rope_frequencies(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: float = 0.0,
@@ -249,6 +273,7 @@ class Rope:
             assert self.turns.is_cuda and self.turns.dtype == torch.float64 and self.turns.shape == (self.rotary_dim // 2,)
             assert self.turns.is_contiguous()
         self.struct = moe_rope(self.turns.data_ptr() if self.rotary_dim else None, self.rotary_dim, 1 if self.interleaved else 0, self.factor)
+        self.ref = C.byref(self.struct)
 
 
 def make_rope(rotary_dim: int, interleaved: bool = False, device="cuda", **frequencies) -> Rope:
@@ -257,15 +282,18 @@ def make_rope(rotary_dim: int, interleaved: bool = False, device="cuda", **frequ
     return Rope(turns.to(device), rotary_dim, interleaved, factor)
 
 
-def _heads(t: torch.Tensor, T: int, dim: int) -> int:
+def _heads(t: torch.Tensor, T: int, heads: int, dim: int) -> int:
     """A [T, heads, dim] tensor whose heads are next to each other; returns its token stride."""
-    assert t.is_cuda and t.dtype == torch.bfloat16 and t.dim() == 3 and t.shape[0] == T and t.shape[2] == dim
-    assert t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == dim)
-    return t.stride(0)
+    assert t.is_cuda and t.dtype is torch.bfloat16 and t.shape == (T, heads, dim)
+    if t.is_contiguous():
+        return heads * dim
+    stride = t.stride()
+    assert stride[2] == 1 and (heads == 1 or stride[1] == dim)
+    return stride[0]
 
 
 def _ints(t: torch.Tensor, T: int):
-    assert t.is_cuda and t.dtype == torch.int32 and t.shape == (T,) and t.is_contiguous()
+    assert t.is_cuda and t.dtype is torch.int32 and t.shape == (T,) and t.is_contiguous()
     return t.data_ptr()
 
 
@@ -274,16 +302,17 @@ def moe_rope_append(cache: KvCache, rope: Rope, q: torch.Tensor, k: torch.Tensor
                     stream=None) -> torch.Tensor:
     """Rotates q [T, heads, dim] and k [T, kv heads, dim] (views of one projection's output as they are), writes k and v to the cache at
     `positions` of the tokens' rows of block_table (table_row; None: row t), and returns the rotated q (`out`; may be q)."""
-    T, c = q.shape[0], cache.struct
-    qs, ks, vs = (_heads(t, T, c.head_dim) for t in (q, k, v))
-    assert k.shape[1] == v.shape[1] == c.n_kv_heads
+    T, H = q.shape[:2]
+    Hk, D = cache.heads, cache.dim
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    assert out.shape == q.shape
-    tab = _table(block_table, table_row, T)
-    _check(_lib().moe_rope_append(C.byref(c), C.byref(tab), C.byref(rope.struct), q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
-                                  q.shape[1], T, _ints(positions, T), out.data_ptr(), _heads(out, T, c.head_dim), _stream(stream)),
-           "moe_rope_append")
+        out, out_stride = _like(q), H * D
+    else:
+        out_stride = _heads(out, T, H, D)
+    st = (_ready or _lib()).moe_rope_append(
+        cache.ref, C.byref(_table(block_table, table_row, T)), rope.ref, q.data_ptr(), _heads(q, T, H, D), k.data_ptr(),
+        _heads(k, T, Hk, D), v.data_ptr(), _heads(v, T, Hk, D), H, T, _ints(positions, T), out.data_ptr(), out_stride, _on(stream, q))
+    if st != MOE_OK:
+        _check(st, "moe_rope_append")
     return out
 
 
@@ -303,16 +332,18 @@ def moe_paged_attention(cache: KvCache, q: torch.Tensor, block_table: torch.Tens
     """Attention of q [T, heads, dim] over the first `lengths` positions of the tokens' sequences (the last `window` of them if that
     is not 0); scale None: 1 / sqrt(dim).  Returns out, or (out, lse [T, heads]) with want_lse."""
     T, H = q.shape[:2]
-    c = cache.struct
-    qs = _heads(q, T, c.head_dim)
+    D = cache.dim
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    assert out.shape == q.shape
+        out, out_stride = _like(q), H * D
+    else:
+        out_stride = _heads(out, T, H, D)
     lse = torch.empty((T, H), dtype=torch.float32, device=q.device) if want_lse else None
     if workspace is None:
         workspace = alloc_attention_workspace(cache, T, H)
-    tab = _table(block_table, table_row, T)
-    _check(_lib().moe_paged_attention(C.byref(c), C.byref(tab), q.data_ptr(), qs, H, T, _ints(lengths, T),
-                                      c.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), _heads(out, T, c.head_dim),
-                                      _ptr(lse), workspace.data_ptr(), workspace.numel(), _stream(stream)), "moe_paged_attention")
+    st = (_ready or _lib()).moe_paged_attention(
+        cache.ref, C.byref(_table(block_table, table_row, T)), q.data_ptr(), _heads(q, T, H, D), H, T, _ints(lengths, T),
+        D ** -0.5 if scale is None else scale, window, out.data_ptr(), out_stride, lse.data_ptr() if want_lse else None,
+        workspace.data_ptr(), workspace.numel(), _on(stream, q))
+    if st != MOE_OK:
+        _check(st, "moe_paged_attention")
     return (out, lse) if want_lse else out

@@ -116,7 +116,8 @@ def _rope_call(cache={}, table={}, rope={}, **kw):
 CACHE_REFUSALS = [
     (dict(k=None), INVALID), (dict(type=2), INVALID), (dict(type=1), INVALID), (dict(n_pages=0), SHAPE), (dict(page_size=0), SHAPE),
     (dict(n_kv_heads=0), SHAPE), (dict(k=P + 4), ALIGN), (dict(token_stride=1028), ALIGN), (dict(head_stride=64), SHAPE),
-    (dict(type=1, k_scale=P, v_scale=P, head_stride=136), ALIGN), (dict(type=1, k_scale=P, v_scale=P + 1), ALIGN), (dict(page_stride=-16384), ALIGN)]
+    (dict(type=1, k_scale=P, v_scale=P, head_stride=136), ALIGN), (dict(type=1, k_scale=P, v_scale=P + 1), ALIGN), (dict(page_stride=-16384), ALIGN),
+    (dict(n_pages=1 << 22, page_stride=1 << 15), UNSUPPORTED), (dict(page_size=1 << 30, token_stride=1 << 40), UNSUPPORTED)]
 TABLE_REFUSALS = [(dict(pages=None), INVALID), (dict(n_rows=0), SHAPE), (dict(max_pages=0), SHAPE), (dict(row_stride=-1), SHAPE),
                   (dict(token_row=None), SHAPE), (dict(pages=P + 2), ALIGN), (dict(token_row=P + 1), ALIGN)]
 
