@@ -29,9 +29,17 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kAttnWaves = 4, kAttnThreads = 64 * kAttnWaves;
 constexpr int kStep = 32;                         // positions of a wave's step
-constexpr int kAttnBlocks = 512;                  // shares at most
-template <int D>
-constexpr int kAttnResident = 2;  // blocks of a CU
+constexpr int kAttnBlocks = 512;                  // shares at most: two blocks for each CU
+// Blocks of a CU that the registers are dealt out for.  bf16 heads of 128 and more columns have 16 KB and more on their way per wave, which four waves of a
+// CU keep the memory busy with; heads of 192 and 256 would spill at two.
+constexpr int attention_resident(int D, bool e4m3) { return D >= 128 && !e4m3 ? 1 : 2; }
+// Shares.  One block per CU for such heads: shares are longer, the parts fewer, and fewer places of memory are read at a time (256 and 512 shares, us:
+// 256 tokens, 32 over 4 heads of 128, 1024 to 2048 positions 153, 160; one token of 131072 positions 100, 107; 64 of 4096 to 8192 271, 277; heads of 256, 32 over
+// 2 50, 60).  Two where items are many, and so short that one's end should overlap another's work (512 tokens of up to 200, 16 heads: 99, 92).
+static int most_shares(int D, bool e4m3, int64_t items)
+{
+    return attention_resident(D, e4m3) == 2 || (D == 128 && items >= 2 * kAttnBlocks) ? kAttnBlocks : kAttnBlocks / 2;
+}
 
 struct AttnArgs {
     const uint8_t *kc, *vc;
@@ -318,7 +326,7 @@ __device__ __forceinline__ void put(float* dst, const float* v)
 }
 
 template <int D, bool E4M3>
-__global__ void __launch_bounds__(kAttnThreads, kAttnResident<D>) attention_kernel(AttnArgs p)
+__global__ void __launch_bounds__(kAttnThreads, attention_resident(D, E4M3)) attention_kernel(AttnArgs p)
 {
     using K = KRows<D, E4M3>;
     using V = VRows<D, E4M3>;
@@ -704,8 +712,8 @@ hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, con
     p.side = heads_side_by_side(c, p.heads, T, longest);
     p.tile = kStep * kAttnWaves / p.side;
     const int64_t most = (int64_t)T * (p.Hk / p.side) * p.q_tiles * ((longest + p.tile - 1) / p.tile);
-    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(most, kAttnBlocks));
     const bool e4m3 = c.type == MOE_KV_E4M3;
+    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(most, most_shares(c.head_dim, e4m3, (int64_t)T * (p.Hk / p.side) * p.q_tiles)));
     switch (c.head_dim) {
         case 64: return attention_go<64>(p, e4m3, grid, s);
         case 96: return attention_go<96>(p, e4m3, grid, s);
