@@ -33,6 +33,23 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float* f)
     return make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
 }
 
+// 16 bytes past the caches where ONCE: what is read once, or written for a reader who comes too late to find it there.
+constexpr int64_t kCachedBytes = (int64_t)8 << 20;        // a result of more is not kept: an XCD's L2 holds 4 MiB
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+template <bool ONCE>
+__device__ __forceinline__ uint4 load16(const bf16_t* q)
+{
+    const u32x4* s = reinterpret_cast<const u32x4*>(q);
+    return __builtin_bit_cast(uint4, ONCE ? __builtin_nontemporal_load(s) : *s);
+}
+template <bool ONCE>
+__device__ __forceinline__ void store16(bf16_t* q, uint4 v)
+{
+    u32x4* d = reinterpret_cast<u32x4*>(q);
+    if (ONCE) __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), d);
+    else *d = __builtin_bit_cast(u32x4, v);
+}
+
 hipError_t launch_norm(const moe_norm_args& a, bool norm, hipStream_t s);
 hipError_t launch_quantize_weight(const bf16_t* w, int N, int K, uint8_t* w8, float* w_scale, hipStream_t s);
 

@@ -3,8 +3,12 @@
 //   h = x + r      y = h * rsqrt(mean(h^2) + eps) * w      per group of 128 columns: s = max(amax|y|, 2^-100) / 448, y8 = e4m3(y / s)
 //
 // One pass: a row's vectors stay in the registers of the threads that share it between the sum of squares and the outputs, so every
-// input is read once and every output written once: HBM bound.
+// input is read once and every output written once: HBM bound.  The norm's inputs and the residual, whose next reader is far off, pass by the caches, and so do large bf16
+// rows (16384 x 7168 with residual to e4m3 149 -> 137 us, 6.0 TB/s; 256 x 4096 5.1 -> 4.2); e4m3 rows stay for the product that reads them (8-byte
+// stores past the caches are slower besides: 142).
 #include "layer.h"
+
+#include <type_traits>
 
 namespace bmoe {
 
@@ -24,31 +28,30 @@ __device__ __forceinline__ unsigned abs_bits(float v) { return __float_as_uint(v
 
 __device__ __forceinline__ float group_magnitude(unsigned bits) { return __uint_as_float(max(bits, __float_as_uint(kLeastMagnitude))); }
 
-// THREADS threads share a row, NV vectors of 8 columns each: vector v of thread i is columns 8 (v THREADS + i) .., so 16 neighbouring
-// lanes hold one group of 128 columns.  256 threads: four rows' worth of waves per block where rows are short (THREADS = 64).
-template <int THREADS, int NV, bool NORM>
-__global__ void __launch_bounds__(256) norm_kernel(NormArgs p)
+// A row's vectors of 8 columns are dealt out over `across` threads, NV each: vector v of thread i is columns 8 (v across + i) .., so 16 neighbouring lanes
+// hold one group of 128 columns.  ONE_ROW: the whole block, in as many waves as leave few lanes without a vector; else a wave per row, four to a block.
+template <bool ONE_ROW, int NV, bool NORM, bool ONCE>
+__global__ void __launch_bounds__(ONE_ROW ? 1024 : 256) norm_kernel(NormArgs p)
 {
-    constexpr int ROWS = 256 / THREADS, WAVES = THREADS / 64;
-    const int lane_row = threadIdx.x / THREADS, i = threadIdx.x % THREADS;
-    const int t = blockIdx.x * ROWS + lane_row;
-    if (ROWS > 1 && t >= p.T) return;                     // whole waves, and no barrier then
+    const int across = ONE_ROW ? (int)blockDim.x : 64, i = ONE_ROW ? (int)threadIdx.x : (int)threadIdx.x & 63;
+    const int t = ONE_ROW ? (int)blockIdx.x : (int)blockIdx.x * 4 + ((int)threadIdx.x >> 6);
+    if (!ONE_ROW && t >= p.T) return;                     // whole waves, and no barrier then
     const bf16_t* xr = p.x + (int64_t)t * p.xs;
     float h[NV][8];
     float sum = 0.0f;
     uint4 xv[NV], rv[NV];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int c = 8 * (v * THREADS + i);
+        const int c = 8 * (v * across + i);
         xv[v] = rv[v] = make_uint4(0, 0, 0, 0);
         if (c < p.d) {
-            xv[v] = *reinterpret_cast<const uint4*>(xr + c);
-            if (NORM && p.r) rv[v] = *reinterpret_cast<const uint4*>(p.r + (int64_t)t * p.rs + c);
+            xv[v] = load16<NORM || ONCE>(xr + c);
+            if (NORM && p.r) rv[v] = load16<true>(p.r + (int64_t)t * p.rs + c);
         }
     }
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int c = 8 * (v * THREADS + i);
+        const int c = 8 * (v * across + i);
         unpack_bf16(xv[v], h[v]);
         if constexpr (NORM) {
             float f[8];
@@ -59,24 +62,23 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs p)
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum += h[v][e] * h[v][e];
-            if (p.ro && c < p.d) *reinterpret_cast<uint4*>(p.ro + (int64_t)t * p.ros + c) = pack_bf16x8(h[v]);
+            if (p.ro && c < p.d) store16<true>(p.ro + (int64_t)t * p.ros + c, pack_bf16x8(h[v]));
         }
     }
     if constexpr (NORM) {
 #pragma unroll
         for (int m = 32; m; m >>= 1) sum += __shfl_xor(sum, m);
-        if constexpr (WAVES > 1) {
-            __shared__ float part[WAVES];
+        if constexpr (ONE_ROW) {
+            __shared__ float part[16];
             if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = sum;
             __syncthreads();
             sum = 0.0f;
-#pragma unroll
-            for (int k = 0; k < WAVES; ++k) sum += part[k];
+            for (int k = 0; k < across >> 6; ++k) sum += part[k];
         }
         const float inv = 1.0f / sqrtf(sum / (float)p.d + p.eps);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
-            const int c = 8 * (v * THREADS + i);
+            const int c = 8 * (v * across + i);
             float w[8];
             if (p.w) {
                 uint4 wv = make_uint4(0, 0, 0, 0);
@@ -85,13 +87,13 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs p)
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) h[v][e] *= p.w ? inv * w[e] : inv;
-            if (p.y && c < p.d) *reinterpret_cast<uint4*>(p.y + (int64_t)t * p.ys + c) = pack_bf16x8(h[v]);
+            if (p.y && c < p.d) store16<ONCE>(p.y + (int64_t)t * p.ys + c, pack_bf16x8(h[v]));
         }
     }
     if (!p.y8) return;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-        const int c = 8 * (v * THREADS + i);
+        const int c = 8 * (v * across + i);
         unsigned bits = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) bits = max(bits, abs_bits(h[v][e]));
@@ -108,12 +110,16 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs p)
     }
 }
 
-template <int THREADS, int NV>
+template <bool ONE_ROW, int NV>
 static void norm_go(const NormArgs& p, bool norm, hipStream_t s)
 {
-    const int rows = 256 / THREADS, grid = ceil_div(p.T, rows);
-    if (norm) hipLaunchKernelGGL((norm_kernel<THREADS, NV, true>), dim3(grid), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((norm_kernel<THREADS, NV, false>), dim3(grid), dim3(256), 0, s, p);
+    const int vectors = p.d / 8, threads = ONE_ROW ? ceil_div(vectors, NV * 64) * 64 : 256, grid = ONE_ROW ? p.T : ceil_div(p.T, 4);
+    const bool once = (int64_t)p.T * p.d * 2 > kCachedBytes;
+    auto go = [&](auto norms, auto past) {
+        hipLaunchKernelGGL((norm_kernel<ONE_ROW, NV, decltype(norms)::value, decltype(past)::value>), dim3(grid), dim3(threads), 0, s, p);
+    };
+    if (norm) once ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+    else once ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
 }
 
 hipError_t launch_norm(const moe_norm_args& a, bool norm, hipStream_t s)
@@ -121,12 +127,11 @@ hipError_t launch_norm(const moe_norm_args& a, bool norm, hipStream_t s)
     NormArgs p{static_cast<const bf16_t*>(a.x), static_cast<const bf16_t*>(a.residual), static_cast<const bf16_t*>(a.weight),
                static_cast<bf16_t*>(a.residual_out), static_cast<bf16_t*>(a.y), static_cast<uint8_t*>(a.y8), a.scale,
                a.x_stride, a.residual_stride, a.residual_out_stride, a.y_stride, a.y8_stride, a.scale_stride, a.T, a.d, a.eps};
-    if (a.d <= 512) norm_go<64, 1>(p, norm, s);
-    else if (a.d <= 1024) norm_go<64, 2>(p, norm, s);
-    else if (a.d <= 2048) norm_go<256, 1>(p, norm, s);
-    else if (a.d <= 4096) norm_go<256, 2>(p, norm, s);
-    else if (a.d <= 8192) norm_go<256, 4>(p, norm, s);
-    else norm_go<256, 8>(p, norm, s);
+    if (a.d <= 512) norm_go<false, 1>(p, norm, s);
+    else if (a.d <= 1024) norm_go<false, 2>(p, norm, s);
+    else if (a.d <= 4096) norm_go<true, 1>(p, norm, s);
+    else if (a.d <= 8192) norm_go<true, 2>(p, norm, s);
+    else norm_go<true, 4>(p, norm, s);
     return hipGetLastError();
 }
 

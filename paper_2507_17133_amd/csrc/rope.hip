@@ -7,6 +7,8 @@
 // output written once.
 #include "layer.h"
 
+#include <type_traits>
+
 namespace bmoe {
 
 struct RopeArgs {
@@ -26,8 +28,6 @@ struct RopeArgs {
     int n_pages, page_size;
     int H, Hk, D, T;
 };
-
-constexpr int kRopeThreads = 256;
 
 // Where the token's k and v go, in elements from the cache's base; negative: nowhere.
 __device__ __forceinline__ int64_t cache_place(const RopeArgs& p, int t, int pos)
@@ -53,13 +53,13 @@ __device__ __forceinline__ uint2 clamp_e4m3x8(const float* f, float inv)
 
 // One block per token.  A thread's unit is 16 columns of a head in two pieces of 8: where pairs are (i, i + R/2), columns i.. and i + R/2..
 // of the rotated part; else 16 columns in a row.  So a unit never needs another thread's columns.
-template <bool E4M3>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeArgs p)
+template <bool E4M3, bool ONCE>
+__global__ void __launch_bounds__(512) rope_kernel(RopeArgs p)
 {
     __shared__ float cs[128], sn[128];                    // R/2 <= 128
     const int t = blockIdx.x, half = p.R >> 1;
     const int pos = p.positions[t];
-    for (int i = threadIdx.x; i < half; i += kRopeThreads) {
+    for (int i = threadIdx.x; i < half; i += blockDim.x) {
         double turns = (double)pos * p.turns[i];
         const float part = (float)(turns - rint(turns));  // within half a turn
         float s, c;
@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeArgs p)
     const int64_t place = cache_place(p, t, pos);
     __syncthreads();
     const int per_head = p.D >> 4, units = (p.H + 2 * p.Hk) * per_head, rot = p.R >> 4;
-    for (int u = threadIdx.x; u < units; u += kRopeThreads) {
+    for (int u = threadIdx.x; u < units; u += blockDim.x) {
         const int head = u / per_head, j = u - head * per_head;
         const bool is_q = head < p.H, is_v = head >= p.H + p.Hk;
         if (!is_q && place < 0) continue;
@@ -106,8 +106,8 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(RopeArgs p)
                 for (int e = 0; e < 8; ++e) a[e] = b[e] = 0.0f;
             }
             bf16_t* dst = p.qo + (int64_t)t * p.qos + (int64_t)head * p.D;
-            *reinterpret_cast<uint4*>(dst + o0) = pack_bf16x8(a);
-            *reinterpret_cast<uint4*>(dst + o1) = pack_bf16x8(b);
+            store16<ONCE>(dst + o0, pack_bf16x8(a));
+            store16<ONCE>(dst + o1, pack_bf16x8(b));
             continue;
         }
         const int64_t at = place + (int64_t)hk * p.head_stride;
@@ -137,8 +137,15 @@ hipError_t launch_rope(const moe_kv_cache& c, const moe_block_table& t, const mo
     p.page_stride = c.page_stride; p.token_stride = c.token_stride; p.head_stride = c.head_stride;
     p.k_scale = c.k_scale; p.v_scale = c.v_scale; p.n_pages = c.n_pages; p.page_size = c.page_size;
     p.H = n_heads; p.Hk = c.n_kv_heads; p.D = c.head_dim; p.T = T;
-    if (c.type == MOE_KV_E4M3) hipLaunchKernelGGL((rope_kernel<true>), dim3(T), dim3(kRopeThreads), 0, s, p);
-    else hipLaunchKernelGGL((rope_kernel<false>), dim3(T), dim3(kRopeThreads), 0, s, p);
+    // Few tokens: a thread for every unit of most shapes.  A large q goes past the caches (16384 tokens of 56 heads 113 -> 106 us, 5.7 TB/s; 8192 of 16
+    // heads of 64 24 -> 19).
+    const int threads = T <= 512 ? 512 : 256;
+    const bool once = (int64_t)T * n_heads * c.head_dim * 2 > kCachedBytes;
+    auto go = [&](auto e4m3, auto past) {
+        hipLaunchKernelGGL((rope_kernel<decltype(e4m3)::value, decltype(past)::value>), dim3(T), dim3(threads), 0, s, p);
+    };
+    if (c.type == MOE_KV_E4M3) once ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+    else once ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
     return hipGetLastError();
 }
 
