@@ -27,7 +27,7 @@ struct LinearArgs {
     int M, N, K, nk;                                      // nk: blocks of K
     int tiles_m, tiles_n, group_m, ksplit;
     int part_stride;                                      // N in whole quads
-    int vec;                                              // out rows take 8-byte stores
+    int vec, vec16;                                       // out rows take 8-byte, 16-byte stores
 };
 
 __device__ __forceinline__ f32x4 mfma_block(i32x8 w, i32x8 x)
@@ -54,10 +54,10 @@ __device__ __forceinline__ void store4(const LinearArgs& p, int m, int n, const 
 }
 
 // ------------------------------------------------------------------------------------------------
-// Few rows (at most 64), or short K: a block takes 16 NT columns and 16 MT rows, its eight waves take the blocks of K by turns and are
+// Few rows (at most 64): a block takes 16 NT columns and 16 MT rows, its eight waves take the blocks of K by turns and are
 // summed through LDS in wave order.  Operands come straight from memory into registers, DEPTH blocks of K ahead.  Bound by the weights'
 // stream, and for few columns by the latency of a wave's few trips to memory.
-// WIDE (K up to kShortK): operands are widened to bf16 (exact) for four 16x16x32 bf16 MFMAs per block of K, which add up in fp32.  The 8-bit
+// WIDE (K up to kShortK, here and in the ring kernel below): operands are widened to bf16 (exact) for four 16x16x32 bf16 MFMAs per block of K, which add up in fp32.  The 8-bit
 // MFMA drops what lies below 2^-13 of the largest product it adds up at a time: over many k's that is 1/100 of the result's rounding to
 // bf16, over a few it is not.
 // ------------------------------------------------------------------------------------------------
@@ -297,19 +297,50 @@ struct TileWork {
         }
         return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w64), kt & 63));
     }
-    __device__ __forceinline__ void store(const f32x4 (&acc)[FM][FN]) const
+    // The wave's results.  In the accumulators neighbouring lanes hold different rows; 16 rows at a time go through LDS (the stages, read to the end
+    // by everyone: the caller's barrier) and are written as whole pieces of rows, 16 bytes per lane.  8-byte slot s of row r stands at s ^ 2 (r / 2) in
+    // rows of 128 bytes, at s ^ 2 (r / 4) in rows of 64: writes and reads are free of bank conflicts.  (Straight from the accumulators,
+    // 16384 x 4096 x 128 63 us.)
+    __device__ __forceinline__ void store(const f32x4 (&acc)[FM][FN], char* smem) const
     {
+        constexpr int PIECES = TN / 8, SHIFT = PIECES == 8 ? 1 : 2;       // 16-byte pieces of a row
+        static_assert(TN == 64 || TN == 32, "rows of 128 or 64 bytes");
+        char* mine = smem + wave * 16 * TN * 2;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            const int m = m0 + wm * TM + i * 16 + c;
+            const int m16 = m0 + wm * TM + i * 16, n64 = n0 + wn * TN;
+            if (p.ksplit > 1) {
+                const int m = m16 + c;
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                const int n = n0 + wn * TN + j * 16 + 4 * g;
-                const float o[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
-                if (p.ksplit == 1) store4(p, m, n, o);
-                else if (m < p.M && n < p.N)
-                    *reinterpret_cast<float4*>(p.part + ((int64_t)slice * p.M + m) * p.part_stride + n) = make_float4(o[0], o[1], o[2], o[3]);
+                for (int j = 0; j < FN; ++j) {
+                    const int n = n64 + j * 16 + 4 * g;
+                    if (m < p.M && n < p.N)
+                        *reinterpret_cast<float4*>(p.part + ((int64_t)slice * p.M + m) * p.part_stride + n) =
+                            make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+                }
+                continue;
             }
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                *reinterpret_cast<uint2*>(mine + c * TN * 2 + (((4 * j + g) ^ ((c >> SHIFT) << 1)) & (2 * PIECES - 1)) * 8) =
+                    make_uint2(pack_bf16(acc[i][j][0], acc[i][j][1]), pack_bf16(acc[i][j][2], acc[i][j][3]));
+            wave_lds_order();
+#pragma unroll
+            for (int q = 0; q < 16 * PIECES / 64; ++q) {
+                const int row = (q * 64 + lane) / PIECES, piece = lane % PIECES, m = m16 + row, n = n64 + piece * 8;
+                const uint4 v = *reinterpret_cast<const uint4*>(mine + row * TN * 2 + (((2 * piece) ^ ((row >> SHIFT) << 1)) & (2 * PIECES - 1)) * 8);
+                if (m >= p.M) continue;
+                bf16_t* dst = p.out + (int64_t)m * p.out_stride + n;
+                if (p.vec16 && n + 8 <= p.N) {
+                    *reinterpret_cast<uint4*>(dst) = v;
+                } else {
+                    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (n + e < p.N) reinterpret_cast<uint16_t*>(dst)[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+                }
+            }
+            wave_lds_order();
         }
     }
 };
@@ -317,7 +348,7 @@ struct TileWork {
 // A ring of NST stages.  A block of K is FM steps; step i multiplies 16 rows by the wave's columns.  Behind each MFMA stand the multiply-adds of the
 // step before (left to itself the compiler has all MFMAs first, and the matrix pipe idles for as long as the multiply-adds take), the
 // reads of the next step's rows and, in the first steps, the loads of the block NST - 1 ahead.
-template <int BM, int BN, int WM, int WN, int NST>
+template <int BM, int BN, int WM, int WN, int NST, bool WIDE>
 __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
 {
     using W = TileWork<BM, BN, WM, WN>;
@@ -375,7 +406,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
         for (int i = 0; i < FM; ++i) {
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                prod[i & 1][j] = mfma_block(fb[j], fa[i & 1]);
+                prod[i & 1][j] = block_product<WIDE>(fb[j], fa[i & 1]);
                 __builtin_amdgcn_sched_barrier(0);
                 if (j == 0 && i + 1 < FM) fa[(i + 1) & 1] = t.rows(St, i + 1);
                 if (j == FN / 2 && i < 2) issue(ahead, free, i);
@@ -388,12 +419,13 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
         }
         stage = stage == NST - 1 ? 0 : stage + 1;
     }
-    __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));             // nothing is on its way to LDS when the block ends
+    __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm(0));       // nothing is on its way to LDS, or being read there
+    lds_barrier();
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[FM - 1][j][e] += prod[1][j][e] * s_before;
-    t.store(acc);
+    t.store(acc, smem);
 }
 
 // 256 x 256: two blocks of K are all that LDS holds, so a load that waits for a whole block to be read has less than a block's time.  The
@@ -497,12 +529,12 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_wide_kernel(LinearArgs p)
         slot = next_slot;
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_lgkm0_imm(0));       // nothing is on its way to LDS, or being read there
+    lds_barrier();
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[FM - 1][j][e] += prod[1][j][e] * s_before;
     if (t.last >= 0) {                                    // the block that K ends in, by itself
-        lds_barrier();
 #pragma unroll
         for (int i = 0; i < LB; ++i) t.load_columns(t.last, i, lds0);
 #pragma unroll
@@ -525,8 +557,9 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_wide_kernel(LinearArgs p)
                 for (int e = 0; e < 4; ++e) acc[i][j][e] += v[e] * s;
             }
         }
+        __syncthreads();
     }
-    t.store(acc);
+    t.store(acc, smem);
 }
 
 // Sum of the slices of K, in their order: a thread has four columns of a row.
@@ -548,11 +581,11 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(LinearArgs p)
 }
 
 // ------------------------------------------------------------------------------------------------
-template <int BM, int BN, int WM, int WN, int NST>
+template <int BM, int BN, int WM, int WN, int NST, bool WIDE = false>
 struct RingTile {
     static constexpr int kM = BM, kN = BN, kThreads = WM * WN * 64;
     static constexpr size_t kLds = (size_t)NST * ((BM + BN) * 128 + BM * 4);
-    static constexpr auto kernel = &linear_tile_kernel<BM, BN, WM, WN, NST>;
+    static constexpr auto kernel = &linear_tile_kernel<BM, BN, WM, WN, NST, WIDE>;
 };
 struct WideTile {
     static constexpr int kM = 256, kN = 256, kThreads = 512;
@@ -561,7 +594,7 @@ struct WideTile {
 };
 
 // The ways to cut the product into tiles; all but the first leave room for one block per CU.
-enum { kRows, kTile64, kTile64x128, kTile128, kTile128x256, kTile256, kWays };
+enum { kRows, kTile64, kTile64x128, kTile128, kTile128x256, kTile256, kShort64, kShort128, kWays };
 template <typename F>
 static auto with_tile(int way, F&& f)
 {
@@ -570,6 +603,8 @@ static auto with_tile(int way, F&& f)
         case kTile64x128: return f(RingTile<64, 128, 2, 4, 6>{});
         case kTile128: return f(RingTile<128, 128, 2, 4, 4>{});
         case kTile128x256: return f(RingTile<128, 256, 2, 4, 3>{});
+        case kShort64: return f(RingTile<64, 64, 2, 2, 2, true>{});
+        case kShort128: return f(RingTile<128, 128, 2, 4, 2, true>{});
         default: return f(WideTile{});
     }
 }
@@ -589,13 +624,17 @@ static LinearPlan linear_plan(int M, int N, int K)
 {
     LinearPlan best{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 0};
     best.columns = ceil_div(N, 32) * ceil_div(M, best.rows) >= 192 ? 32 : 16;
-    if (M <= 32 || K <= kShortK) return best;
-    static constexpr struct { int m, n; double block; } kTile[kWays] = {
+    if (M <= 32 || (M <= 64 && K <= kShortK)) return best;
+    if (K <= kShortK) {                                   // a tile is its loads and its store: large ones where they still fill the CUs
+        best.way = (int64_t)ceil_div(M, 128) * ceil_div(N, 128) >= 256 ? kShort128 : kShort64;
+        return best;
+    }
+    static constexpr struct { int m, n; double block; } kTile[] = {
         {0, 0, 0}, {64, 64, 0.32}, {64, 128, 0.47}, {128, 128, 0.65}, {128, 256, 1.06}, {256, 256, 1.77}};
     constexpr int kCus = 256;
     const int nk = ceil_div(K, kScaleGroup);
     double least = M <= 64 ? 4.0 + 0.46e-6 * N * K : 1e300;
-    for (int way = kTile64; way < kWays; ++way)
+    for (int way = kTile64; way <= kTile256; ++way)
         for (int ks = 1; ks <= (way == kTile64 ? 16 : 1); ks *= 2) {
             const int per = ceil_div(nk, ks);
             if (ks > 1 && (per < 4 || ceil_div(nk, per) != ks)) continue;          // no slice is empty
@@ -640,6 +679,7 @@ hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s)
     p.ksplit = L.ksplit;
     p.part_stride = (int)align_up(a.N, 4);
     p.vec = (a.out_stride & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 7u) == 0;
+    p.vec16 = (a.out_stride & 7) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0;
     if (L.way == kRows) {
         const bool two = L.columns == 32;
         if (L.rows == 16) two ? rows_go<1, 2, 3>(p, s) : rows_go<1, 1, 4>(p, s);
