@@ -609,50 +609,84 @@ static auto with_tile(int way, F&& f)
     }
 }
 
-struct LinearPlan { int way, ksplit, rows, columns; };    // rows, columns: of the rows kernel's blocks
+struct LinearPlan {
+    int way, ksplit, rows, columns;               // rows, columns: of the rows kernel's blocks
+    int first_way, first_rows;                    // rows that go ahead in tiles of their own (0: none)
+};
 
 // The way that should take the least time.  A CU works on one tile at a time, so a product takes rounds of tiles; a tile takes 2 us (its first loads,
 // its store) and for every block of K what is listed, from products of 2048 to 16384 rows; a launch takes 2 us.  Small tiles may be cut along K
 // as well, which costs a second launch and the partial sums' way to memory and back.  Foretold and measured (us), K blocks:
 //   64 x 64      0.32   256 rows by 6144 x 4096 26.5, 27.4; 1024 by 4096 x 7168 81.7, 82.7
-//   64 x 128     0.47   256 by 6144 x 4096 19.0, 19.4;      1024 by 4096 x 7168 58.6, 55.8
-//   128 x 128    0.65   1024 by 4096 x 7168 40.4, 41.2;     4096 by 4096 x 4096 93, 97
+//   64 x 128     0.47   256 by 6144 x 4096 19.0, 18.9;      1024 by 4096 x 7168 58.6, 55.8
+//   128 x 128    0.65   1024 by 4096 x 7168 40.4, 40.7;     4096 by 4096 x 4096 93, 97
 //   128 x 256    1.06   2048 by 4096 x 4096 37.9, 40.3;     16384 by 7168 x 7168 861, 867
-//   256 x 256    1.77   4096 by 4096 x 4096 60.6, 63.9;     16384 by 7168 x 7168 710, 708
+//   256 x 256    1.72   4096 by 4096 x 4096 59, 62;         16384 by 7168 x 7168 690, 680
 // Up to 64 rows there is the rows kernel: its time goes with the weights, and from 33 rows on with the rows' trips as well.
-static LinearPlan linear_plan(int M, int N, int K)
+// A last round that few CUs have a tile in costs as much as a full one, so the rows of whole rounds may go ahead, and the rest be cut in tiles
+// that suit it.
+static constexpr struct { int m, n; double block; } kTile[] = {
+    {0, 0, 0}, {64, 64, 0.32}, {64, 128, 0.47}, {128, 128, 0.65}, {128, 256, 1.06}, {256, 256, 1.72}};
+constexpr int kCus = 256;
+
+static double tile_rounds(int way, int64_t tiles, int blocks)
 {
-    LinearPlan best{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 0};
+    return (double)((tiles + kCus - 1) / kCus) * (blocks * kTile[way].block + 2.0);
+}
+
+static LinearPlan one_way(int M, int N, int K, double& least)
+{
+    LinearPlan best{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 0, 0, 0};
     best.columns = ceil_div(N, 32) * ceil_div(M, best.rows) >= 192 ? 32 : 16;
+    least = 4.0 + (M <= 16 ? 0.2e-6 : M <= 32 ? 0.28e-6 : 0.46e-6) * N * K;
     if (M <= 32 || (M <= 64 && K <= kShortK)) return best;
     if (K <= kShortK) {                                   // a tile is its loads and its store: large ones where they still fill the CUs
-        best.way = (int64_t)ceil_div(M, 128) * ceil_div(N, 128) >= 256 ? kShort128 : kShort64;
+        best.way = (int64_t)ceil_div(M, 128) * ceil_div(N, 128) >= kCus ? kShort128 : kShort64;
         return best;
     }
-    static constexpr struct { int m, n; double block; } kTile[] = {
-        {0, 0, 0}, {64, 64, 0.32}, {64, 128, 0.47}, {128, 128, 0.65}, {128, 256, 1.06}, {256, 256, 1.77}};
-    constexpr int kCus = 256;
     const int nk = ceil_div(K, kScaleGroup);
-    double least = M <= 64 ? 4.0 + 0.46e-6 * N * K : 1e300;
+    if (M > 64) least = 1e300;
     for (int way = kTile64; way <= kTile256; ++way)
         for (int ks = 1; ks <= (way == kTile64 ? 16 : 1); ks *= 2) {
             const int per = ceil_div(nk, ks);
             if (ks > 1 && (per < 4 || ceil_div(nk, per) != ks)) continue;          // no slice is empty
             const int64_t tiles = (int64_t)ceil_div(M, kTile[way].m) * ceil_div(N, kTile[way].n) * ks;
-            double us = 2.0 + (double)((tiles + kCus - 1) / kCus) * (per * kTile[way].block + 2.0);
+            double us = 2.0 + tile_rounds(way, tiles, per);
             if (ks > 1) us += 2.5 + 2e-6 * M * N * ks;
             if (us < least) {
                 least = us;
-                best = {way, ks, 0, 0};
+                best = {way, ks, 0, 0, 0, 0};
             }
         }
+    return best;
+}
+
+static LinearPlan linear_plan(int M, int N, int K)
+{
+    double least, rest;
+    LinearPlan best = one_way(M, N, K, least);
+    if (K <= kShortK || M <= 128) return best;
+    for (int way = kTile128; way <= kTile256; ++way) {
+        const int cols = ceil_div(N, kTile[way].n);
+        const int64_t rounds = (int64_t)ceil_div(M, kTile[way].m) * cols / kCus, rows = rounds * kCus / cols * kTile[way].m;
+        if (rows <= 0 || rows >= M) continue;
+        const double us = 2.0 + tile_rounds(way, rows / kTile[way].m * cols, ceil_div(K, kScaleGroup));
+        if (us >= least) continue;
+        LinearPlan p = one_way(M - (int)rows, N, K, rest);
+        if (us + rest < least) {
+            least = us + rest;
+            best = p;
+            best.first_way = way;
+            best.first_rows = (int)rows;
+        }
+    }
     return best;
 }
 
 size_t linear_workspace_bytes(int M, int N, int K)
 {
     const LinearPlan L = linear_plan(M, N, K);
-    return L.ksplit > 1 ? align_up((size_t)L.ksplit * M * align_up(N, 4) * sizeof(float), 256) : 0;
+    return L.ksplit > 1 ? align_up((size_t)L.ksplit * (M - L.first_rows) * align_up(N, 4) * sizeof(float), 256) : 0;
 }
 
 hipError_t init_linear_kernels()
@@ -676,10 +710,30 @@ hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s)
     p.part = static_cast<float*>(ws);
     p.x_stride = a.x_stride; p.xs_stride = a.x_scale_stride; p.out_stride = a.out_stride;
     p.M = a.M; p.N = a.N; p.K = a.K; p.nk = ceil_div(a.K, kScaleGroup);
-    p.ksplit = L.ksplit;
     p.part_stride = (int)align_up(a.N, 4);
     p.vec = (a.out_stride & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 7u) == 0;
     p.vec16 = (a.out_stride & 7) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0;
+    auto tiles = [&](int way) {
+        return with_tile(way, [&](auto tile) {
+            p.tiles_m = ceil_div(p.M, tile.kM);
+            p.tiles_n = ceil_div(p.N, tile.kN);
+            p.group_m = 8;
+            const int total = p.tiles_m * p.tiles_n * p.ksplit;
+            hipLaunchKernelGGL(tile.kernel, dim3((total + 7) / 8 * 8), dim3(tile.kThreads), tile.kLds, s, p);
+            return hipGetLastError();
+        });
+    };
+    hipError_t e;
+    if (L.first_rows > 0) {
+        p.M = L.first_rows;
+        p.ksplit = 1;
+        if ((e = tiles(L.first_way)) != hipSuccess) return e;
+        p.M = a.M - L.first_rows;
+        p.x += L.first_rows * p.x_stride;
+        p.xs += L.first_rows;
+        p.out += L.first_rows * p.out_stride;
+    }
+    p.ksplit = L.ksplit;
     if (L.way == kRows) {
         const bool two = L.columns == 32;
         if (L.rows == 16) two ? rows_go<1, 2, 3>(p, s) : rows_go<1, 1, 4>(p, s);
@@ -687,16 +741,9 @@ hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s)
         else two ? rows_go<4, 2, 2>(p, s) : rows_go<4, 1, 2>(p, s);
         return hipGetLastError();
     }
-    hipError_t e = with_tile(L.way, [&](auto tile) {
-        p.tiles_m = ceil_div(p.M, tile.kM);
-        p.tiles_n = ceil_div(p.N, tile.kN);
-        p.group_m = 8;
-        const int total = p.tiles_m * p.tiles_n * p.ksplit;
-        hipLaunchKernelGGL(tile.kernel, dim3((total + 7) / 8 * 8), dim3(tile.kThreads), tile.kLds, s, p);
-        return hipGetLastError();
-    });
+    e = tiles(L.way);
     if (e != hipSuccess || L.ksplit == 1) return e;
-    hipLaunchKernelGGL(linear_sum_kernel, dim3((unsigned)(((int64_t)a.M * (p.part_stride / 4) + 255) / 256)), dim3(256), 0, s, p);
+    hipLaunchKernelGGL(linear_sum_kernel, dim3((unsigned)(((int64_t)p.M * (p.part_stride / 4) + 255) / 256)), dim3(256), 0, s, p);
     return hipGetLastError();
 }
 
