@@ -29,6 +29,7 @@ extern "C" {
 /* Limits (MOE_ERR_UNSUPPORTED beyond). */
 #define MOE_NORM_MAX_D 16384
 #define MOE_MAX_HEADS 1024
+#define MOE_MAX_ROWS (1 << 21)                /* rows (tokens) of a call */
 
 /*
  * Root-mean-square norm of T rows of d columns with the residual's addition:
@@ -40,7 +41,7 @@ extern "C" {
  * overlap the inputs.
  *   x, residual, residual_out, y  [T][d] bf16, row strides multiples of 8;  weight [d] bf16 or NULL (ones)
  *   y8 [T][d] e4m3 with 8-byte aligned rows;  scale [ceil(d/128)][scale_stride >= T] fp32
- * Limits: d a multiple of 8 (MOE_ERR_SHAPE), d <= MOE_NORM_MAX_D.
+ * Limits: d a multiple of 8 (MOE_ERR_SHAPE), d <= MOE_NORM_MAX_D, T <= MOE_MAX_ROWS.
  */
 typedef struct moe_norm_args {
     const void *x; int64_t x_stride;
@@ -74,8 +75,9 @@ moe_status moe_quantize_weight(const void *w, int32_t N, int32_t K, void *w8, fl
  *   x8 [M][K] e4m3, rows x_stride apart (a multiple of 16); x_scale [ceil(K/128)][x_scale_stride >= M] (as moe_rms_norm
  *   and moe_quantize_rows write them); w8 [N][K] e4m3 dense; w_scale [ceil(N/128)][ceil(K/128)];
  *   out [M][N] bf16, rows out_stride apart (any; 2-byte aligned).
- * K a multiple of 16 (MOE_ERR_SHAPE); M <= 2^21, N, K <= 2^20, x_stride <= 2^23 (MOE_ERR_UNSUPPORTED).  The workspace holds partial sums where the work is split along K:
- * moe_linear_workspace_size bytes (0 for many shapes) for exactly this M, N, K, 256-byte aligned.
+ * K a multiple of 16 (MOE_ERR_SHAPE); M <= MOE_MAX_ROWS, N, K <= 2^20, x_stride <= 2^23 (MOE_ERR_UNSUPPORTED).  out overlaps no
+ * input.  The workspace holds partial sums where the work is split along K: moe_linear_workspace_size bytes (0 for many shapes) for
+ * exactly this M, N, K, 256-byte aligned.
  */
 typedef struct moe_linear_args {
     const void *x8; int64_t x_stride;
@@ -152,7 +154,8 @@ moe_status moe_rope_frequencies(int32_t rotary_dim, double base, const moe_rope_
  *   call may name the same place.  In an 8-bit cache values beyond 448 scales are held as 448 scales.
  * A token of a negative position is padding: its q_out is zero, and nothing goes to the cache.  Nor does a token whose
  * page or row is not there (see moe_block_table, or a position beyond max_pages * page_size); its q_out is written as usual.
- * Errors: head_dim not a multiple of 16, rotary_dim not a multiple of 16 or beyond head_dim (MOE_ERR_SHAPE).
+ * Errors: head_dim not a multiple of 16, rotary_dim not a multiple of 16 or beyond head_dim (MOE_ERR_SHAPE); head_dim > 256,
+ * n_heads > MOE_MAX_HEADS, T > MOE_MAX_ROWS (MOE_ERR_UNSUPPORTED).
  */
 moe_status moe_rope_append(const moe_kv_cache *cache, const moe_block_table *table, const moe_rope *rope, const void *q,
                            int64_t q_stride, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
@@ -165,7 +168,7 @@ moe_status moe_rope_append(const moe_kv_cache *cache, const moe_block_table *tab
  * over the positions p of [0, lengths[t]), with window > 0 only the last `window` of them.  Positions whose page is not
  * there (see moe_block_table) are left out; lengths beyond max_pages * page_size end there.  A token with no position left
  * has out = 0 and lse = -infinity.  What the cache holds in places that are left out does not matter, NaN included.
- *   q [T][n_heads][head_dim] bf16, tokens q_stride apart (a multiple of 8); out the same, out_stride (a multiple of 4, 8-byte aligned)
+ *   q [T][n_heads][head_dim] bf16, tokens q_stride apart (a multiple of 8); out the same, out_stride (a multiple of 4, 8-byte aligned), not q itself
  *   lse [T][n_heads] fp32 or NULL: log of the sum of exp(scale * q . k), to join attention over several caches
  * The tokens of a prompt's chunk are T rows with lengths position + 1, appended first.
  * Scores and sums are fp32; the probabilities are rounded to bf16 for the product with v (its sum is of the unrounded ones).

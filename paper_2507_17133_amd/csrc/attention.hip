@@ -66,6 +66,9 @@ struct AttnArgs {
     float* parts;                                 // per share two places of [side] parts: [heads][D] O, [heads] m, [heads] l
 };
 
+// Floats of a part: whole 16-byte pieces, so that rows of O are written and read in such.
+constexpr __host__ __device__ int64_t part_floats(int heads, int D) { return (int64_t)heads * (D + 4); }
+
 // Positions [lo, hi) that token t attends to.
 __device__ __forceinline__ int2 span_of(const AttnArgs& p, int t)
 {
@@ -467,7 +470,7 @@ __global__ void __launch_bounds__(kAttnThreads, attention_resident(D, E4M3)) att
             });
             if (p.lse && g == 0) p.lse[(int64_t)w.t * p.H + w.h0 + c] = (m + __log2f(l)) * 0.6931471805599453f;
         } else {
-            float* part = p.parts + (((int64_t)2 * blockIdx.x + (begins ? 1 : 0)) * p.side + sub) * ((int64_t)p.heads * (D + 2));
+            float* part = p.parts + (((int64_t)2 * blockIdx.x + (begins ? 1 : 0)) * p.side + sub) * part_floats(p.heads, D);
             V::runs(g, [&](int col, auto n, int j, int r) {
                 float v[n.value];
 #pragma unroll
@@ -571,7 +574,7 @@ __global__ void __launch_bounds__(256) join_kernel(AttnArgs p, int e4m3)
     const int n = cut.z, set = cut.y / p.q_tiles, sub = y / p.heads, h = y - sub * p.heads;
     const int hk = set * p.side + sub, h0 = hk * p.group + (cut.y - set * p.q_tiles) * 16;
     if (n == 0 || sub >= p.side || h >= min(16, (hk + 1) * p.group - h0)) return;          // all threads of the head
-    const int64_t size = (int64_t)p.heads * (D + 2);
+    const int64_t size = part_floats(p.heads, D);
     // share x left its part in its second place, the others in their first
     auto part = [&](int i) { return p.parts + ((2 * ((int64_t)blockIdx.x + i) + (i == 0 ? 1 : 0)) * p.side + sub) * size; };
     auto sync = [&]() {
@@ -640,7 +643,8 @@ size_t attention_workspace_bytes(const moe_kv_cache& c, int T, int n_heads)
 {
     (void)T;                                              // the shares are as many for every T, and each has at most four heads' parts
     const int heads = item_heads(n_heads / c.n_kv_heads);
-    return align_up(kAttnBlocks * sizeof(int4), 256) + align_up((size_t)2 * kAttnBlocks * (c.n_kv_heads % 4 == 0 ? 4 : c.n_kv_heads % 2 == 0 ? 2 : 1) * heads * (c.head_dim + 2) * sizeof(float), 256);
+    const int side = c.n_kv_heads % 4 == 0 ? 4 : c.n_kv_heads % 2 == 0 ? 2 : 1;
+    return align_up(kAttnBlocks * sizeof(int4), 256) + align_up((size_t)2 * kAttnBlocks * side * part_floats(heads, c.head_dim) * sizeof(float), 256);
 }
 
 // A row of O in LDS is 4 floats longer, so that the heads of a wave write to different banks.

@@ -7,7 +7,7 @@
 namespace bmoe {
 namespace {
 
-constexpr int32_t kMaxRows = 1 << 21, kMaxColumns = 1 << 20;     // tile counts and grids stay within what launches take
+constexpr int32_t kMaxColumns = 1 << 20;                         // with MOE_MAX_ROWS: tile counts and grids stay within what launches take
 constexpr int64_t kMaxRowBytes = (int64_t)1 << 23;               // a tile's offsets stay in 32 bits
 
 bool off(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
@@ -19,7 +19,7 @@ moe_status check_norm(const moe_norm_args* a, bool norm)
 {
     if (!a || a->T < 0) return MOE_ERR_INVALID_ARG;
     if (a->d < 8 || a->d % 8 != 0) return MOE_ERR_SHAPE;
-    if (a->d > MOE_NORM_MAX_D) return MOE_ERR_UNSUPPORTED;
+    if (a->d > MOE_NORM_MAX_D || a->T > MOE_MAX_ROWS) return MOE_ERR_UNSUPPORTED;
     if (a->T == 0) return MOE_OK;
     if (!a->x || (a->y8 ? !a->scale : !a->y)) return MOE_ERR_INVALID_ARG;
     if (norm ? !(a->eps >= 0.0f && std::isfinite(a->eps)) : a->residual || a->weight || a->residual_out || a->y || !a->y8)
@@ -76,7 +76,7 @@ moe_status check_linear(int32_t M, int32_t N, int32_t K)
 {
     if (M < 0) return MOE_ERR_INVALID_ARG;
     if (N < 1 || K < 16 || K % 16 != 0) return MOE_ERR_SHAPE;
-    if (M > kMaxRows || N > kMaxColumns || K > kMaxColumns) return MOE_ERR_UNSUPPORTED;
+    if (M > MOE_MAX_ROWS || N > kMaxColumns || K > kMaxColumns) return MOE_ERR_UNSUPPORTED;
     return MOE_OK;
 }
 
@@ -201,7 +201,7 @@ moe_status moe_rope_append(const moe_kv_cache* cache, const moe_block_table* tab
     if ((st = check_table(table, T)) != MOE_OK) return st;
     const int D = cache->head_dim, R = rope->rotary_dim;
     if (D % 16 != 0 || R < 0 || R > D || R % 16 != 0 || n_heads < 1) return MOE_ERR_SHAPE;
-    if (D > 256 || n_heads > MOE_MAX_HEADS) return MOE_ERR_UNSUPPORTED;
+    if (D > 256 || n_heads > MOE_MAX_HEADS || T > MOE_MAX_ROWS) return MOE_ERR_UNSUPPORTED;
     if (R > 0 && !rope->turns) return MOE_ERR_INVALID_ARG;
     if (T == 0) return MOE_OK;
     if (!q || !k || !v || !positions || !q_out) return MOE_ERR_INVALID_ARG;

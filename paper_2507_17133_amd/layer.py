@@ -2,7 +2,8 @@
 8-bit output, the 8-bit linear layer, rotary positions with the append to a paged key-value cache, attention over it.
 
 Like `binding`: argument marshalling only, no fallback path.  Tensors are on the current device; work goes to the
-current stream, or to `stream`.
+current stream.  A call with `stream` is the same call under torch.cuda.stream(stream): what it allocates belongs to that stream.
+Tensors of other streams are the caller's to order before it, and to keep until it has run (Tensor.record_stream).
 """
 from __future__ import annotations
 
@@ -86,8 +87,13 @@ def _lib():
 _current_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _on(stream, t: torch.Tensor):
-    return _current_stream(t.get_device()) if stream is None else stream.cuda_stream
+def _on(t: torch.Tensor):
+    return _current_stream(t.get_device())
+
+
+def _under(stream, call, *args):
+    with torch.cuda.stream(stream):
+        return call(*args)
 
 
 def _rows(t: torch.Tensor, dtype, rows: int, cols: int):
@@ -125,7 +131,7 @@ def alloc_norm_out(T: int, d: int, want=("y",), residual: bool = False, device="
                    torch.empty((T, d), dtype=bf, device=device) if residual else None)
 
 
-def _norm(call, x, weight, eps, residual, want, out, stream) -> NormOut:
+def _norm(call, x, weight, eps, residual, want, out) -> NormOut:
     T, d = x.shape
     bf = torch.bfloat16
     xs, xp = _rows(x, bf, T, d), x.data_ptr()
@@ -155,7 +161,7 @@ def _norm(call, x, weight, eps, residual, want, out, stream) -> NormOut:
         y8, s = out.y8.data_ptr(), out.scale.data_ptr()
     if out.residual is not None:
         ro = out.residual.data_ptr()
-    st = call(C.byref(moe_norm_args(xp, xs, r, rs or 0, w, ro, ros or 0, y, ys or 0, y8, y8s or 0, s, ss or 0, T, d, eps)), _on(stream, x))
+    st = call(C.byref(moe_norm_args(xp, xs, r, rs or 0, w, ro, ros or 0, y, ys or 0, y8, y8s or 0, s, ss or 0, T, d, eps)), _on(x))
     if st != MOE_OK:
         _check(st, call.__name__)
     return out
@@ -164,22 +170,28 @@ def _norm(call, x, weight, eps, residual, want, out, stream) -> NormOut:
 def moe_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor], eps: float = 1e-6, residual: Optional[torch.Tensor] = None,
                  want=("y",), out: Optional[NormOut] = None, stream=None) -> NormOut:
     """Norm of x + residual; `want`: "y" (bf16), "y8" (e4m3 with scales), or both.  The sum comes back as `residual` if one was given."""
-    return _norm((_ready or _lib()).moe_rms_norm, x, weight, eps, residual, want, out, stream)
+    if stream is not None:
+        return _under(stream, moe_rms_norm, x, weight, eps, residual, want, out)
+    return _norm((_ready or _lib()).moe_rms_norm, x, weight, eps, residual, want, out)
 
 
 def moe_quantize_rows(x: torch.Tensor, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, stream=None):
     """(x8 [T][d] e4m3, scale [ceil(d/128)][T])."""
-    o = _norm((_ready or _lib()).moe_quantize_rows, x, None, 0.0, None, ("y8",), None if out is None else NormOut(y8=out[0], scale=out[1]), stream)
+    if stream is not None:
+        return _under(stream, moe_quantize_rows, x, out)
+    o = _norm((_ready or _lib()).moe_quantize_rows, x, None, 0.0, None, ("y8",), None if out is None else NormOut(y8=out[0], scale=out[1]))
     return o.y8, o.scale
 
 
 def moe_quantize_weight(w: torch.Tensor, stream=None):
     """(w8 [N][K] e4m3, w_scale [ceil(N/128)][ceil(K/128)]) of a bf16 weight [N][K]."""
+    if stream is not None:
+        return _under(stream, moe_quantize_weight, w)
     N, K = w.shape
     assert w.is_cuda and w.dtype is torch.bfloat16 and w.is_contiguous()
     w8 = torch.empty((N, K), dtype=E4M3, device=w.device)
     scale = torch.empty((_groups(N), _groups(K)), dtype=torch.float32, device=w.device)
-    _check(_lib().moe_quantize_weight(_ptr(w), N, K, _ptr(w8), _ptr(scale), _on(stream, w)), "moe_quantize_weight")
+    _check(_lib().moe_quantize_weight(_ptr(w), N, K, _ptr(w8), _ptr(scale), _on(w)), "moe_quantize_weight")
     return w8, scale
 
 
@@ -195,6 +207,8 @@ def alloc_linear_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tenso
 
 def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w_scale: torch.Tensor, out: Optional[torch.Tensor] = None,
                     workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    if stream is not None:
+        return _under(stream, moe_linear_e4m3, x8, x_scale, w8, w_scale, out, workspace)
     M, K = x8.shape
     N = w8.shape[0]
     G = (K + 127) // 128
@@ -209,7 +223,7 @@ def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w
         workspace = alloc_linear_workspace(M, N, K, x8.device)
     a = moe_linear_args(x8.data_ptr(), _rows(x8, E4M3, M, K), x_scale.data_ptr(), _rows(x_scale, torch.float32, G, M), w8.data_ptr(),
                         w_scale.data_ptr(), out.data_ptr(), out_stride, M, N, K)
-    st = L.moe_linear_e4m3(C.byref(a), workspace.data_ptr(), workspace.numel(), _on(stream, x8))
+    st = L.moe_linear_e4m3(C.byref(a), workspace.data_ptr(), workspace.numel(), _on(x8))
     if st != MOE_OK:
         _check(st, "moe_linear_e4m3")
     return out
@@ -302,6 +316,8 @@ def moe_rope_append(cache: KvCache, rope: Rope, q: torch.Tensor, k: torch.Tensor
                     stream=None) -> torch.Tensor:
     """Rotates q [T, heads, dim] and k [T, kv heads, dim] (views of one projection's output as they are), writes k and v to the cache at
     `positions` of the tokens' rows of block_table (table_row; None: row t), and returns the rotated q (`out`; may be q)."""
+    if stream is not None:
+        return _under(stream, moe_rope_append, cache, rope, q, k, v, positions, block_table, table_row, out)
     T, H = q.shape[:2]
     Hk, D = cache.heads, cache.dim
     if out is None:
@@ -310,7 +326,7 @@ def moe_rope_append(cache: KvCache, rope: Rope, q: torch.Tensor, k: torch.Tensor
         out_stride = _heads(out, T, H, D)
     st = (_ready or _lib()).moe_rope_append(
         cache.ref, C.byref(_table(block_table, table_row, T)), rope.ref, q.data_ptr(), _heads(q, T, H, D), k.data_ptr(),
-        _heads(k, T, Hk, D), v.data_ptr(), _heads(v, T, Hk, D), H, T, _ints(positions, T), out.data_ptr(), out_stride, _on(stream, q))
+        _heads(k, T, Hk, D), v.data_ptr(), _heads(v, T, Hk, D), H, T, _ints(positions, T), out.data_ptr(), out_stride, _on(q))
     if st != MOE_OK:
         _check(st, "moe_rope_append")
     return out
@@ -331,6 +347,8 @@ def moe_paged_attention(cache: KvCache, q: torch.Tensor, block_table: torch.Tens
                         out: Optional[torch.Tensor] = None, want_lse: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
     """Attention of q [T, heads, dim] over the first `lengths` positions of the tokens' sequences (the last `window` of them if that
     is not 0); scale None: 1 / sqrt(dim).  Returns out, or (out, lse [T, heads]) with want_lse."""
+    if stream is not None:
+        return _under(stream, moe_paged_attention, cache, q, block_table, lengths, table_row, scale, window, out, want_lse, workspace)
     T, H = q.shape[:2]
     D = cache.dim
     if out is None:
@@ -343,7 +361,7 @@ def moe_paged_attention(cache: KvCache, q: torch.Tensor, block_table: torch.Tens
     st = (_ready or _lib()).moe_paged_attention(
         cache.ref, C.byref(_table(block_table, table_row, T)), q.data_ptr(), _heads(q, T, H, D), H, T, _ints(lengths, T),
         D ** -0.5 if scale is None else scale, window, out.data_ptr(), out_stride, lse.data_ptr() if want_lse else None,
-        workspace.data_ptr(), workspace.numel(), _on(stream, q))
+        workspace.data_ptr(), workspace.numel(), _on(q))
     if st != MOE_OK:
         _check(st, "moe_paged_attention")
     return (out, lse) if want_lse else out

@@ -189,3 +189,10 @@ def test_frequencies_of_the_formulas():
 def test_frequencies_refusals(args):
     with pytest.raises(B.MoeError):
         L.rope_frequencies(*args)
+
+
+@pytest.mark.parametrize("rows,status", [((1 << 21) + 1, UNSUPPORTED), ((1 << 31) - 1, UNSUPPORTED)])
+def test_more_rows_than_a_launch_takes(rows, status):
+    assert L._lib().moe_rms_norm(_norm(T=rows), None) == status
+    assert L._lib().moe_quantize_rows(_quant(T=rows, scale_stride=rows), None) == status
+    assert _rope_call(T=rows) == status
