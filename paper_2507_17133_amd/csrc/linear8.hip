@@ -56,10 +56,11 @@ __device__ __forceinline__ void store4(const LinearArgs& p, int m, int n, const 
 // ------------------------------------------------------------------------------------------------
 // Few rows (at most 64): a block takes 16 NT columns and 16 MT rows, its eight waves take the blocks of K by turns and are
 // summed through LDS in wave order.  Operands come straight from memory into registers, DEPTH blocks of K ahead.  Bound by the weights'
-// stream, and for few columns by the latency of a wave's few trips to memory.
-// WIDE (K up to kShortK, here and in the ring kernel below): operands are widened to bf16 (exact) for four 16x16x32 bf16 MFMAs per block of K, which add up in fp32.  The 8-bit
-// MFMA drops what lies below 2^-13 of the largest product it adds up at a time: over many k's that is 1/100 of the result's rounding to
-// bf16, over a few it is not.
+// stream, and for few columns by the latency of a wave's few trips to memory: one row by 6144 x 4096 7.4 us (25 MB, 3.4 TB/s), 16 rows by
+// 14336 x 4096 16 us (59 MB, 3.7 TB/s).
+// WIDE (K up to kShortK, here and in the ring kernel below): operands are widened to bf16 (exact) for four 16x16x32 bf16 MFMAs per block of
+// K, which add up in fp32.  The 8-bit MFMA drops what lies below 2^-13 of the largest product it adds up at a time: over many k's that is
+// 1/100 of the result's rounding to bf16, over a few it is not.
 // ------------------------------------------------------------------------------------------------
 constexpr int kRowWaves = 8;
 constexpr int kShortK = 256;
@@ -347,7 +348,8 @@ struct TileWork {
 
 // A ring of NST stages.  A block of K is FM steps; step i multiplies 16 rows by the wave's columns.  Behind each MFMA stand the multiply-adds of the
 // step before (left to itself the compiler has all MFMAs first, and the matrix pipe idles for as long as the multiply-adds take), the
-// reads of the next step's rows and, in the first steps, the loads of the block NST - 1 ahead.
+// reads of the next step's rows and, in the first steps, the loads of the block NST - 1 ahead.  Bound by what a CU pulls past its L2 where
+// tiles are small (64 x 64: 16 KB per block of K in 0.32 us), by the LDS where they are large; times stand at the plan below.
 template <int BM, int BN, int WM, int WN, int NST, bool WIDE>
 __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
 {
@@ -436,8 +438,8 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_tile_kernel(LinearArgs p)
 //   before the last step    the columns and the first half of the next block have landed; the second half of this one has been read, and that
 //                           of the block after next is loaded.  The last step's MFMAs run while the next block's first operands come in, each in place
 //                           of one that has been used for the last time.
-// So every load has about one and a half blocks' time.  16384 x 7168 x 7168 725 us (2323 TFLOP/s), in the ring kernel above with two stages 760;
-// without its loads 0.53 ms.  The LDS bounds it: 192 KB of reads and 64 KB of writes per block of 2048 MFMA cycles, where a wave tile of 128 x 64 is what
+// So every load has about one and a half blocks' time.  16384 x 7168 x 7168 694 us (2426 TFLOP/s); the ring kernel above with two stages takes
+// 5 % longer; without its loads 0.53 ms.  The LDS bounds it: 192 KB of reads and 64 KB of writes per block of 2048 MFMA cycles, where a wave tile of 128 x 64 is what
 // leaves room for accumulators that the multiply-adds reach (they cannot address the accumulation registers).
 template <int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(WM * WN * 64) linear_wide_kernel(LinearArgs p)
@@ -562,7 +564,7 @@ __global__ void __launch_bounds__(WM * WN * 64) linear_wide_kernel(LinearArgs p)
     t.store(acc, smem);
 }
 
-// Sum of the slices of K, in their order: a thread has four columns of a row.
+// Sum of the slices of K, in their order, so the result is the same every time: a thread has four columns of a row.  Latency bound.
 __global__ void __launch_bounds__(256) linear_sum_kernel(LinearArgs p)
 {
     const int quads = p.part_stride / 4;
@@ -572,6 +574,8 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(LinearArgs p)
     const float4* src = reinterpret_cast<const float4*>(p.part + m * p.part_stride + n);
     const int64_t plane = (int64_t)p.M * quads;
     float4 v = src[0];
+    // three slices' loads at a time (16 slices of 100 rows of 512: 5.8 -> 4.0 us)
+#pragma unroll 3
     for (int z = 1; z < p.ksplit; ++z) {
         const float4 u = src[z * plane];
         v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
@@ -641,6 +645,7 @@ static LinearPlan one_way(int M, int N, int K, double& least)
     least = 4.0 + (M <= 16 ? 0.2e-6 : M <= 32 ? 0.28e-6 : 0.46e-6) * N * K;
     if (M <= 32 || (M <= 64 && K <= kShortK)) return best;
     if (K <= kShortK) {                                   // a tile is its loads and its store: large ones where they still fill the CUs
+                                                          // (64 x 64 and 128 x 128, us: 16384 x 4096 x 128 59.6, 53.1; 2048 x 1024 x 256 5.5, 6.2)
         best.way = (int64_t)ceil_div(M, 128) * ceil_div(N, 128) >= kCus ? kShort128 : kShort64;
         return best;
     }
@@ -717,7 +722,7 @@ hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s)
         return with_tile(way, [&](auto tile) {
             p.tiles_m = ceil_div(p.M, tile.kM);
             p.tiles_n = ceil_div(p.N, tile.kN);
-            p.group_m = 8;
+            p.group_m = 8;                                // 16384 x 7168 x 7168: 1, 4, 8, 16: 732, 694, 694, 708 us; 8192 x 4096 x 14336 386, 375, 373, 381
             const int total = p.tiles_m * p.tiles_n * p.ksplit;
             hipLaunchKernelGGL(tile.kernel, dim3((total + 7) / 8 * 8), dim3(tile.kThreads), tile.kLds, s, p);
             return hipGetLastError();
