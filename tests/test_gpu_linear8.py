@@ -112,3 +112,22 @@ def test_no_rows_and_graph_replays():
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(out, P.moe_linear_e4m3(x8, xs, w8, ws))
+
+
+# rows of whole rounds in tiles of 128 x 128, 128 x 256 or 256 x 256, the rest in rows, small tiles with and without slices of K, middle tiles
+@pytest.mark.parametrize("M,N,K", [(3600, 1027, 1488), (1056, 15595, 288), (4793, 1675, 1440), (10909, 1283, 304), (8425, 398, 3088), (10825, 1447, 2464),
+                                   (723, 10988, 2704), (9229, 2108, 400), (15189, 1055, 272)])
+def test_rows_of_whole_rounds_and_the_rest(M, N, K):
+    x8, xs, w8, ws = _case(M, N, K, 2, ld=K + 32)
+    want, tol = _exact(x8, xs, w8, ws)
+    wide = torch.full((M, N + 9), 7.0, dtype=torch.bfloat16, device="cuda")
+    near(P.moe_linear_e4m3(x8, xs, w8, ws, out=wide[:, 1:1 + N]), want, tol, "out")
+    assert bool((wide[:, 0] == 7).all()) and bool((wide[:, 1 + N:] == 7).all())
+    near(P.moe_linear_e4m3(x8.contiguous(), xs, w8, ws), want, tol, "dense")
+
+
+@pytest.mark.parametrize("M,N,K", [(4100, 1000, 256), (2000, 2100, 144), (129, 520, 16)])
+def test_many_rows_of_short_k(M, N, K):
+    x8, xs, w8, ws = _case(M, N, K, 3)
+    want, tol = _exact(x8, xs, w8, ws)
+    near(P.moe_linear_e4m3(x8, xs, w8, ws), want, tol, "out")

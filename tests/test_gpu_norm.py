@@ -133,3 +133,15 @@ def test_quantize_weight(N, K):
     near(scale, s, 2.0 ** -23 * s, "scale")
     full = scale.cpu().repeat_interleave(128, 0)[:N].repeat_interleave(128, 1)[:, :K].double()
     near(w8.float().cpu().double() * full, w.double(), (HALF_E4M3 * w.double().abs()).clamp_min(2.0 ** -10 * full) * (1 + 1e-5), "w8")
+
+
+@pytest.mark.parametrize("T,d", [(9001, 504), (5003, 1000), (1100, 4096), (700, 8000), (333, 16384)])
+def test_results_too_large_for_the_caches(T, d):
+    """More than 8 MiB of bf16 rows: they go past the caches."""
+    x, r = _x(T, d, 5), _x(T, d, 6)
+    got = P.moe_rms_norm(x.cuda(), None, 1e-5, residual=r.cuda(), want=("y", "y8"))
+    _, y = _exact(x, r, None, 1e-5)
+    near(got.y, y, (HALF_BF16 + REL) * y.abs(), "y")
+    _check8(got.y8, got.scale, y)
+    assert torch.equal(got.residual.cpu(), (x.float() + r.float()).to(torch.bfloat16))
+    _check8(*P.moe_quantize_rows(x.cuda()), x.double())

@@ -149,3 +149,28 @@ def test_far_positions_keep_their_angle(pos):
     want = torch.cat((ang.cos(), ang.sin()))[None, None]
     # pos * turns in 64 bits is itself off by 2^-53 of the turns made
     near(got, want, HALF_BF16 * want.abs() + 1e-6 + pos * 2.0 ** -50, "cos, sin")
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_q_too_large_for_the_caches(e4m3):
+    """More than 8 MiB of q: it goes past the caches; two sequences' prompts in one call."""
+    T, H, Hk, D, page = 1301, 32, 4, 128, 16
+    q, k, v = _case(T, H, Hk, D, 31)
+    rows = (torch.arange(T) >= 600).to(torch.int32)
+    pos = torch.where(rows == 0, torch.arange(T), torch.arange(T) - 600).to(torch.int32)
+    n = -(-701 // page)
+    table = torch.randperm(2 * n, generator=torch.Generator().manual_seed(32)).to(torch.int32).view(2, n)
+    scale = torch.full((Hk,), 0.02) if e4m3 else None
+    cache = P.alloc_kv_cache(2 * n, page, Hk, D, *(None if scale is None else scale.cuda() for _ in range(2)))
+    rope = P.make_rope(D)
+    got = P.moe_rope_append(cache, rope, q, k, v, pos.cuda(), table.cuda(), table_row=rows.cuda())
+    turns = rope.turns.cpu()
+    want, size = _rotate(q.cpu(), pos, turns, rope.factor, D, False)
+    near(got, want, HALF_BF16 * want.abs() + 1e-6 * size, "q")
+    at = table[rows.long(), pos.long() // page].long(), pos.long() % page
+    want, size = _rotate(k.cpu(), pos, turns, rope.factor, D, False)
+    if e4m3:
+        want, size = (want / 0.02).clamp(-448, 448), size / 0.02
+        near(cache.k.float().cpu()[at], want, (HALF_E4M3 * want.abs()).clamp_min(2.0 ** -10) + 2e-6 * size, "k")
+    else:
+        near(cache.k.float().cpu()[at], want, HALF_BF16 * want.abs() + 1e-6 * size, "k")
