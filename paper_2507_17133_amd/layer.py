@@ -106,7 +106,7 @@ def _rows(t: torch.Tensor, dtype, rows: int, cols: int):
 
 
 def _like(t: torch.Tensor, dtype=torch.bfloat16) -> torch.Tensor:
-    return torch.empty_like(t, dtype=dtype) if t.is_contiguous() else torch.empty(t.shape, dtype=dtype, device=t.device)
+    return torch.empty_like(t, dtype=dtype) if t.is_contiguous() else t.new_empty(t.shape, dtype=dtype)
 
 
 def _groups(d: int) -> int:
@@ -144,7 +144,7 @@ def _norm(call, x, weight, eps, residual, want, out) -> NormOut:
     if out is None:
         q = "y8" in want
         out = NormOut(_like(x) if "y" in want else None, _like(x, E4M3) if q else None,
-                      torch.empty(((d + 127) // 128, T), dtype=torch.float32, device=x.device) if q else None,
+                      x.new_empty(((d + 127) // 128, T), dtype=torch.float32) if q else None,
                       _like(x) if residual is not None else None)
         ys = y8s = ros = d
         ss = T
@@ -216,14 +216,15 @@ def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w
     assert w_scale.is_cuda and w_scale.dtype is torch.float32 and w_scale.shape == (_groups(N), G) and w_scale.is_contiguous()
     L = _ready or _lib()
     if out is None:
-        out, out_stride = torch.empty((M, N), dtype=torch.bfloat16, device=x8.device), N
+        out, out_stride = x8.new_empty((M, N), dtype=torch.bfloat16), N
     else:
         out_stride = _rows(out, torch.bfloat16, M, N)
     if workspace is None:
-        workspace = alloc_linear_workspace(M, N, K, x8.device)
+        need = linear_workspace_size(M, N, K)
+        workspace = x8.new_empty(need, dtype=torch.uint8) if need else None
     a = moe_linear_args(x8.data_ptr(), _rows(x8, E4M3, M, K), x_scale.data_ptr(), _rows(x_scale, torch.float32, G, M), w8.data_ptr(),
                         w_scale.data_ptr(), out.data_ptr(), out_stride, M, N, K)
-    st = L.moe_linear_e4m3(C.byref(a), workspace.data_ptr(), workspace.numel(), _on(x8))
+    st = L.moe_linear_e4m3(C.byref(a), None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _on(x8))
     if st != MOE_OK:
         _check(st, "moe_linear_e4m3")
     return out
@@ -355,7 +356,7 @@ def moe_paged_attention(cache: KvCache, q: torch.Tensor, block_table: torch.Tens
         out, out_stride = _like(q), H * D
     else:
         out_stride = _heads(out, T, H, D)
-    lse = torch.empty((T, H), dtype=torch.float32, device=q.device) if want_lse else None
+    lse = q.new_empty((T, H), dtype=torch.float32) if want_lse else None
     if workspace is None:
         workspace = alloc_attention_workspace(cache, T, H)
     st = (_ready or _lib()).moe_paged_attention(
