@@ -75,6 +75,9 @@ moe_status moe_quantize_weight(const void *w, int32_t N, int32_t K, void *w8, fl
  *   x8 [M][K] e4m3, rows x_stride apart (a multiple of 16); x_scale [ceil(K/128)][x_scale_stride >= M] (as moe_rms_norm
  *   and moe_quantize_rows write them); w8 [N][K] e4m3 dense; w_scale [ceil(N/128)][ceil(K/128)];
  *   out [M][N] bf16, rows out_stride apart (any; 2-byte aligned).
+ * Blocks are scaled and added up in fp32.  Within a block, K > 512 goes through the 8-bit matrix instructions, which add up products aligned
+ * to the largest of them: of each, what lies below 2^-13 of that one is lost (around 1e-5 of sum |x||w| for values of like size; at worst,
+ * one value among 127 that are 2^13 smaller, 127 * 2^-13).  Up to K = 512 products are exact and their sums fp32.
  * K a multiple of 16 (MOE_ERR_SHAPE); M <= MOE_MAX_ROWS, N, K <= 2^20, x_stride <= 2^23 (MOE_ERR_UNSUPPORTED).  out overlaps no
  * input.  The workspace holds partial sums where the work is split along K: moe_linear_workspace_size bytes (0 for many shapes) for
  * exactly this M, N, K, 256-byte aligned.
