@@ -13,6 +13,8 @@
 //   V^T: lane (g, c) reads the same 8 positions' columns 8 c .. 8 c + 7 (whole rows of 16 lanes x 16 bytes) and transposes its 8 x 8 block with
 //   byte permutes; product j then gives the rows d = 8 c + j.
 // The maximum and the rescaling are per head = per lane; only the maximum crosses lanes (two exchanges per 32 positions).
+// A probability goes to the second product as two bf16 that add up to it within 2^-15 (one bf16 alone: 2^-8 of it, and as errors do not cancel where
+// values of v do, an error of the result beyond its own rounding).
 //
 // Work: the positions of every (token, key head, 16 query heads) in tiles of 128 form one line of tiles, cut into equal shares, one per block:
 // one long sequence among short ones is spread over the whole GPU.  A share that begins or ends inside a sequence leaves (m, l, O) in the
@@ -232,6 +234,27 @@ struct KRows {
     }
 };
 
+// The probabilities of a lane's 8 positions as the MFMA's second operand, in two parts: cut off at bf16's bits, and what that leaves (rounded to bf16).
+struct Probs {
+    bf16x8 head, rest;
+    template <bool FINITE>                        // v holds no infinities
+    __device__ __forceinline__ void set(const float* e)
+    {
+        unsigned h[4];
+        float r[8];
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            // an infinite v times a rest of 0 would be NaN: a last bit keeps the rest above 0
+            const unsigned a = __float_as_uint(e[i]) | (FINITE ? 0u : 1u), b = __float_as_uint(e[i + 1]) | (FINITE ? 0u : 1u);
+            h[i / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+            r[i] = __uint_as_float(a) - __uint_as_float(a & 0xFFFF0000u);
+            r[i + 1] = __uint_as_float(b) - __uint_as_float(b & 0xFFFF0000u);
+        }
+        head = __builtin_bit_cast(bf16x8, make_uint4(h[0], h[1], h[2], h[3]));
+        rest = __builtin_bit_cast(bf16x8, pack_bf16x8(r));
+    }
+};
+
 // The 8 positions' columns [C0 + c N, + N) of V that a lane holds, N = W / 16 (8, 4 or 2).
 template <int W, bool E4M3>
 struct VPart {
@@ -264,7 +287,7 @@ struct VPart {
         }
     }
     // acc[j] += (column c N + j of the 8 positions) x p.  keep: bits of the positions that count; what the others hold may be anything.
-    __device__ __forceinline__ void add(f32x4* acc, bf16x8 prob, bool all, unsigned keep) const
+    __device__ __forceinline__ void add(f32x4* acc, const Probs& prob, bool all, unsigned keep) const
     {
 #pragma unroll
         for (int i = 0; i < N / 2; ++i) {
@@ -279,8 +302,11 @@ struct VPart {
             lo.y = __builtin_amdgcn_perm(w[3], w[2], 0x05040100u); hi.y = __builtin_amdgcn_perm(w[3], w[2], 0x07060302u);
             lo.z = __builtin_amdgcn_perm(w[5], w[4], 0x05040100u); hi.z = __builtin_amdgcn_perm(w[5], w[4], 0x07060302u);
             lo.w = __builtin_amdgcn_perm(w[7], w[6], 0x05040100u); hi.w = __builtin_amdgcn_perm(w[7], w[6], 0x07060302u);
-            acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, lo), prob, acc[2 * i], 0, 0, 0);
-            acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hi), prob, acc[2 * i + 1], 0, 0, 0);
+            const bf16x8 v0 = __builtin_bit_cast(bf16x8, lo), v1 = __builtin_bit_cast(bf16x8, hi);
+            acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, prob.head, acc[2 * i], 0, 0, 0);
+            acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, prob.head, acc[2 * i + 1], 0, 0, 0);
+            acc[2 * i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, prob.rest, acc[2 * i], 0, 0, 0);
+            acc[2 * i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, prob.rest, acc[2 * i + 1], 0, 0, 0);
         }
     }
 };
@@ -299,7 +325,7 @@ struct VRows {
         if constexpr (N64) b.load(base, 128 * N128, off, col);
         if constexpr (N32) c.load(base, 128 * N128 + 64 * N64, off, col);
     }
-    __device__ __forceinline__ void add(f32x4* acc, bf16x8 prob, bool all, unsigned keep) const
+    __device__ __forceinline__ void add(f32x4* acc, const Probs& prob, bool all, unsigned keep) const
     {
 #pragma unroll
         for (int i = 0; i < N128; ++i) a[i].add(acc + 8 * i, prob, all, keep);
@@ -548,7 +574,9 @@ __global__ void __launch_bounds__(kAttnThreads, attention_resident(D, E4M3)) att
                     e[4 * h + r] = __builtin_amdgcn_exp2f(s[h][r] - ref);
                     l += e[4 * h + r];
                 }
-            vr.add(acc, __builtin_bit_cast(bf16x8, pack_bf16x8(e)), all, keep);
+            Probs prob;
+            prob.set<E4M3>(e);
+            vr.add(acc, prob, all, keep);
         }
         if (more) vr.load(head_base(p.vc, next.hk), voff, c);
         if (!same) {
