@@ -28,30 +28,6 @@ __device__ __forceinline__ unsigned abs_bits(float v) { return __float_as_uint(v
 
 __device__ __forceinline__ float group_scale(unsigned bits) { return __uint_as_float(max(bits, __float_as_uint(kLeastMagnitude))) / kE4m3Max; }
 
-// y / s to the last bit for the price of three multiplications: the product with the rounded 1 / s, corrected by its own remainder.  (Every pair of bf16
-// significands, of the value and of the group's largest, gives what the division gives; the product alone takes about one code in 1400 to its
-// neighbour.  The division itself: norm of 16384 x 7168 136 -> 145 us, its rows alone 63 -> 70, weight of 7168 x 7168 28 -> 34; this way 138, 64, 28.)
-// An infinite s leaves y * 0.
-struct Divisor {
-    float s, k;
-    __device__ __forceinline__ explicit Divisor(float by) : s(by < __builtin_inff() ? by : 0.0f), k(1.0f / by) {}
-    __device__ __forceinline__ float operator()(float y) const
-    {
-        const float q = y * k;
-        return __builtin_fmaf(-__builtin_fmaf(q, s, -y), k, q);           // in this order -0 stays -0
-    }
-};
-
-// Takes the values of a group of tiny scale, and the scale that it returns, out of the way of subnormal remainders.
-template <int N>
-__device__ __forceinline__ float lift_tiny(float (&v)[N], float s)
-{
-    if (s >= 5.421010862427522e-20f || s != s) return s;                  // 2^-64
-#pragma unroll
-    for (int e = 0; e < N; ++e) v[e] *= 1.8446744073709552e19f;           // 2^64
-    return s * 1.8446744073709552e19f;
-}
-
 // A row's vectors of 8 columns are dealt out over `across` threads, NV each: vector v of thread i is columns 8 (v across + i) .., so 16 neighbouring lanes
 // hold one group of 128 columns.  ONE_ROW: the whole block, in as many waves as leave few lanes without a vector; else a wave per row, four to a block.
 template <bool ONE_ROW, int NV, bool NORM, bool ONCE>

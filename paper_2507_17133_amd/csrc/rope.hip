@@ -39,14 +39,16 @@ __device__ __forceinline__ int64_t cache_place(const RopeArgs& p, int t, int pos
     return (int64_t)page * p.page_stride + (int64_t)(pos - page_at * p.page_size) * p.token_stride;
 }
 
-// Eight values for an 8-bit cache: beyond 448 they stay at 448, NaN stays NaN.
-__device__ __forceinline__ uint2 clamp_e4m3x8(const float* f, float inv)
+// Eight values over their head's scale for an 8-bit cache: beyond 448 they stay at 448, NaN stays NaN.  (By division 16384 tokens of 16 + 2 * 16 heads of 64
+// 34 -> 38 us, this way 35.)
+__device__ __forceinline__ uint2 clamp_e4m3x8(float (&f)[8], float scale)
 {
+    const Divisor div(lift_tiny(f, scale));
     float g[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        g[e] = f[e] * inv;
-        if (fabsf(g[e]) > kE4m3Max) g[e] = copysignf(kE4m3Max, g[e]);
+        const float q = div.near(f[e]);
+        g[e] = fabsf(q) > kE4m3Max ? copysignf(kE4m3Max, q) : div.exact(f[e], q);
     }
     return make_uint2(pack_e4m3(g[0], g[1], g[2], g[3]), pack_e4m3(g[4], g[5], g[6], g[7]));
 }
@@ -113,9 +115,9 @@ __global__ void __launch_bounds__(512) rope_kernel(RopeArgs p)
         const int64_t at = place + (int64_t)hk * p.head_stride;
         uint8_t* dst = is_v ? p.vc : p.kc;
         if constexpr (E4M3) {
-            const float inv = 1.0f / (is_v ? p.v_scale : p.k_scale)[hk];
-            *reinterpret_cast<uint2*>(dst + at + o0) = clamp_e4m3x8(a, inv);
-            *reinterpret_cast<uint2*>(dst + at + o1) = clamp_e4m3x8(b, inv);
+            const float scale = (is_v ? p.v_scale : p.k_scale)[hk];
+            *reinterpret_cast<uint2*>(dst + at + o0) = clamp_e4m3x8(a, scale);
+            *reinterpret_cast<uint2*>(dst + at + o1) = clamp_e4m3x8(b, scale);
         } else {
             *reinterpret_cast<uint4*>(dst + 2 * (at + o0)) = pack_bf16x8(a);
             *reinterpret_cast<uint4*>(dst + 2 * (at + o1)) = pack_bf16x8(b);
