@@ -12,7 +12,7 @@
  *   - Strides are in elements of their tensor and may exceed what the shape needs (slices of wider tensors); the last
  *     dimension is contiguous.  Pointers are 16-byte aligned, and so is every row that a stride leads to (8 bytes where
  *     it says so); pointers to int32, fp32 and fp64 arrays need the alignment of their type.
- *   - T == 0 (M == 0) is a valid call that does nothing.
+ *   - T == 0 (M == 0) is a valid call that does nothing; the block table of an empty batch may have no rows.
  *   - The calls work per row: a token's result has the same bits whatever other tokens are in the call, with two
  *     exceptions, where the way that a sum is split goes by the whole call: moe_paged_attention and moe_linear_e4m3.
  *     The same call gives the same bits every time.

@@ -198,12 +198,12 @@ moe_status moe_rope_append(const moe_kv_cache* cache, const moe_block_table* tab
     moe_status st = check_cache(cache);
     if (st != MOE_OK) return st;
     if (T < 0 || !rope) return MOE_ERR_INVALID_ARG;
-    if ((st = check_table(table, T)) != MOE_OK) return st;
     const int D = cache->head_dim, R = rope->rotary_dim;
     if (D % 16 != 0 || R < 0 || R > D || R % 16 != 0 || n_heads < 1) return MOE_ERR_SHAPE;
     if (D > 256 || n_heads > MOE_MAX_HEADS || T > MOE_MAX_ROWS) return MOE_ERR_UNSUPPORTED;
     if (R > 0 && !rope->turns) return MOE_ERR_INVALID_ARG;
-    if (T == 0) return MOE_OK;
+    if (T == 0) return MOE_OK;                            // an empty batch's table has no rows
+    if ((st = check_table(table, T)) != MOE_OK) return st;
     if (!q || !k || !v || !positions || !q_out) return MOE_ERR_INVALID_ARG;
     if (off(q, 16) || off(k, 16) || off(v, 16) || off(q_out, 16) || off(positions, 4) || off(rope->turns, 8) || bad_stride(q_stride, 8) ||
         bad_stride(k_stride, 8) || bad_stride(v_stride, 8) || bad_stride(q_out_stride, 8))
@@ -231,9 +231,9 @@ moe_status moe_paged_attention(const moe_kv_cache* cache, const moe_block_table*
 {
     moe_status st = check_attention(cache, n_heads, T);
     if (st != MOE_OK) return st;
-    if ((st = check_table(table, T)) != MOE_OK) return st;
     if (window < 0 || !std::isfinite(scale)) return MOE_ERR_INVALID_ARG;
     if (T == 0) return MOE_OK;
+    if ((st = check_table(table, T)) != MOE_OK) return st;
     if (!q || !lengths || !out) return MOE_ERR_INVALID_ARG;
     if (off(q, 16) || off(lengths, 4) || off(out, 8) || off(lse, 4) || bad_stride(q_stride, 8) || bad_stride(out_stride, 4))
         return MOE_ERR_ALIGNMENT;
