@@ -171,7 +171,8 @@ moe_status moe_rope_append(const moe_kv_cache *cache, const moe_block_table *tab
  * over the positions p of [0, lengths[t]), with window > 0 only the last `window` of them.  Positions whose page is not
  * there (see moe_block_table) are left out; lengths beyond max_pages * page_size end there.  A token with no position left
  * has out = 0 and lse = -infinity.  What the cache holds in places that are left out does not matter, NaN included.
- *   q [T][n_heads][head_dim] bf16, tokens q_stride apart (a multiple of 8); out the same, out_stride (a multiple of 4, 8-byte aligned), not q itself
+ *   q [T][n_heads][head_dim] bf16, tokens q_stride apart (a multiple of 8); out the same, out_stride (a multiple of 4, 8-byte aligned); no row
+ *   of out shares memory with one of q (MOE_ERR_INVALID_ARG)
  *   lse [T][n_heads] fp32 or NULL: log of the sum of exp(scale * q . k), to join attention over several caches
  * The tokens of a prompt's chunk are T rows with lengths position + 1, appended first.
  * Scores and sums are fp32; the probabilities are rounded to bf16 for the product with v (its sum is of the unrounded ones).

@@ -15,6 +15,20 @@ bool off(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p)
 // A row stride of a tensor that is read: whole 16-byte (or `unit`-element) steps forward.
 bool bad_stride(int64_t stride, int unit) { return stride < 0 || stride % unit != 0; }
 
+// Whether a row of a shares memory with a row of b; T rows of `width` bytes each, strides in bytes, not negative.
+bool rows_meet(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int T, int64_t width)
+{
+    const int64_t a0 = (int64_t)reinterpret_cast<uintptr_t>(a), b0 = (int64_t)reinterpret_cast<uintptr_t>(b);
+    if (a0 + (T - 1) * a_stride + width <= b0 || b0 + (T - 1) * b_stride + width <= a0) return false;
+    for (int i = 0, j = 0; i < T && j < T;) {
+        const int64_t ai = a0 + i * a_stride, bj = b0 + j * b_stride;
+        if (ai + width <= bj) ++i;
+        else if (bj + width <= ai) ++j;
+        else return true;
+    }
+    return false;
+}
+
 moe_status check_norm(const moe_norm_args* a, bool norm)
 {
     if (!a || a->T < 0) return MOE_ERR_INVALID_ARG;
@@ -240,6 +254,8 @@ moe_status moe_paged_attention(const moe_kv_cache* cache, const moe_block_table*
     if (T > 1 && out_stride < (int64_t)n_heads * cache->head_dim) return MOE_ERR_SHAPE;
     if (!workspace || workspace_bytes < attention_workspace_bytes(*cache, T, n_heads)) return MOE_ERR_WORKSPACE;
     if (off(workspace, 256)) return MOE_ERR_ALIGNMENT;
+    // blocks read a token's q where others have written its out
+    if (rows_meet(q, 2 * q_stride, out, 2 * out_stride, T, (int64_t)2 * n_heads * cache->head_dim)) return MOE_ERR_INVALID_ARG;
     hipError_t e = ensure_device_init(nullptr);
     if (e != hipSuccess) return hip_fail(e, "moe_paged_attention/init");
     e = launch_attention(*cache, *table, static_cast<const bf16_t*>(q), q_stride, n_heads, T, lengths, scale, window,

@@ -347,7 +347,7 @@ def moe_paged_attention(cache: KvCache, q: torch.Tensor, block_table: torch.Tens
                         table_row: Optional[torch.Tensor] = None, scale: Optional[float] = None, window: int = 0,
                         out: Optional[torch.Tensor] = None, want_lse: bool = False, workspace: Optional[torch.Tensor] = None, stream=None):
     """Attention of q [T, heads, dim] over the first `lengths` positions of the tokens' sequences (the last `window` of them if that
-    is not 0); scale None: 1 / sqrt(dim).  Returns out, or (out, lse [T, heads]) with want_lse."""
+    is not 0); scale None: 1 / sqrt(dim).  Returns out (which may not be q), or (out, lse [T, heads]) with want_lse."""
     if stream is not None:
         return _under(stream, moe_paged_attention, cache, q, block_table, lengths, table_row, scale, window, out, want_lse, workspace)
     T, H = q.shape[:2]
