@@ -8,7 +8,8 @@
  * Conventions: those of brownout_moe.h (device pointers of the caller, caller's stream and workspace, no host
  * synchronisation, arguments checked on the host before any launch, a moe_status from every call).  Besides:
  *   - bf16 is rounded to nearest even; e4m3 is the 8-bit type with 4 exponent and 3 mantissa bits, no infinities and
- *     a largest value of 448, rounded to nearest even.  Sums, softmax statistics and scales are fp32.
+ *     a largest value of 448, rounded to nearest even.  Sums, softmax statistics and scales are fp32 (but for what the 8-bit matrix
+ *     instructions add up within 8 products: moe_linear_e4m3).
  *   - Strides are in elements of their tensor and may exceed what the shape needs (slices of wider tensors); the last
  *     dimension is contiguous.  Pointers are 16-byte aligned, and so is every row that a stride leads to (8 bytes where
  *     it says so); pointers to int32, fp32 and fp64 arrays need the alignment of their type.
@@ -75,9 +76,11 @@ moe_status moe_quantize_weight(const void *w, int32_t N, int32_t K, void *w8, fl
  *   x8 [M][K] e4m3, rows x_stride apart (a multiple of 16); x_scale [ceil(K/128)][x_scale_stride >= M] (as moe_rms_norm
  *   and moe_quantize_rows write them); w8 [N][K] e4m3 dense; w_scale [ceil(N/128)][ceil(K/128)];
  *   out [M][N] bf16, rows out_stride apart (any; 2-byte aligned).
- * Blocks are scaled and added up in fp32.  Within a block, K > 512 goes through the 8-bit matrix instructions, which add up products aligned
- * to the largest of them: of each, what lies below 2^-13 of that one is lost (around 1e-5 of sum |x||w| for values of like size; at worst,
- * one value among 127 that are 2^13 smaller, 127 * 2^-13).  Up to K = 512 products are exact and their sums fp32.
+ * Blocks are scaled and added up in fp32.  Up to K = 512, and for every K where `exact` is not 0, products are exact and their sums fp32.  Else a
+ * block goes through the 8-bit matrix instructions, which add up 8 neighbouring columns at a time: each product is cut off toward zero at 2^-13
+ * of 2^e, e the largest sum of two exponents among the 8, and what the groups give is added in fp32.  So at most 7 * 2^-13 of its largest
+ * product is lost of a group: around 1e-5 of sum |x||w| for values of like size, up to some 1e-4 of the largest where one column is
+ * hundreds of times larger than its neighbours.  `exact` takes up to 2.2 times as long (many rows), for up to 64 rows 1.05 to 1.2.
  * K a multiple of 16 (MOE_ERR_SHAPE); M <= MOE_MAX_ROWS, N, K <= 2^20, x_stride <= 2^23 (MOE_ERR_UNSUPPORTED).  out overlaps no
  * input.  The workspace holds partial sums where the work is split along K: moe_linear_workspace_size bytes (0 for many shapes) for
  * exactly this M, N, K, 256-byte aligned.
@@ -89,6 +92,7 @@ typedef struct moe_linear_args {
     const float *w_scale;
     void *out; int64_t out_stride;
     int32_t M, N, K;
+    int32_t exact;                            /* 0, or 1: exact products and fp32 sums for every K */
 } moe_linear_args;
 moe_status moe_linear_workspace_size(int32_t M, int32_t N, int32_t K, size_t *bytes);
 moe_status moe_linear_e4m3(const moe_linear_args *a, void *workspace, size_t workspace_bytes, void *stream);

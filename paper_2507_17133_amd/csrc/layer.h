@@ -86,7 +86,7 @@ hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, con
                             hipStream_t s);
 
 hipError_t init_linear_kernels();
-size_t linear_workspace_bytes(int M, int N, int K);
+size_t linear_workspace_bytes(int M, int N, int K, bool exact);
 hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s);
 
 }  // namespace bmoe

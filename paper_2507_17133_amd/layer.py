@@ -32,7 +32,7 @@ class moe_norm_args(C.Structure):
 class moe_linear_args(C.Structure):
     _fields_ = [("x8", C.c_void_p), ("x_stride", C.c_int64), ("x_scale", C.c_void_p), ("x_scale_stride", C.c_int64),
                 ("w8", C.c_void_p), ("w_scale", C.c_void_p), ("out", C.c_void_p), ("out_stride", C.c_int64),
-                ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32)]
+                ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("exact", C.c_int32)]
 
 
 class moe_kv_cache(C.Structure):
@@ -206,9 +206,11 @@ def alloc_linear_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tenso
 
 
 def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w_scale: torch.Tensor, out: Optional[torch.Tensor] = None,
-                    workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+                    workspace: Optional[torch.Tensor] = None, stream=None, exact: bool = False) -> torch.Tensor:
+    """x8 * x_scale times (w8 * w_scale) transposed, [M, N] bf16.  Beyond K = 512 the 8-bit matrix instructions cut products off at 2^-13 of the largest
+    of 8 neighbouring columns, which shows where a column is far larger than the rest; `exact`: products in full, sums in fp32, for up to 2.2 times the time."""
     if stream is not None:
-        return _under(stream, moe_linear_e4m3, x8, x_scale, w8, w_scale, out, workspace)
+        return _under(stream, moe_linear_e4m3, x8, x_scale, w8, w_scale, out, workspace, None, exact)
     M, K = x8.shape
     N = w8.shape[0]
     G = (K + 127) // 128
@@ -223,7 +225,7 @@ def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w
         need = linear_workspace_size(M, N, K)
         workspace = x8.new_empty(need, dtype=torch.uint8) if need else None
     a = moe_linear_args(x8.data_ptr(), _rows(x8, E4M3, M, K), x_scale.data_ptr(), _rows(x_scale, torch.float32, G, M), w8.data_ptr(),
-                        w_scale.data_ptr(), out.data_ptr(), out_stride, M, N, K)
+                        w_scale.data_ptr(), out.data_ptr(), out_stride, M, N, K, 1 if exact else 0)
     st = L.moe_linear_e4m3(C.byref(a), None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _on(x8))
     if st != MOE_OK:
         _check(st, "moe_linear_e4m3")
