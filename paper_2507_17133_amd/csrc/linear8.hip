@@ -197,14 +197,14 @@ static void rows_go(const LinearArgs& p, hipStream_t s)
 // ------------------------------------------------------------------------------------------------
 // Direct loads to LDS, 16 or 4 bytes per lane: base (wave-uniform) + off -> lds + 16 (4) lane.  Written as instructions because the compiler puts a
 // wait for every such load in flight before each LDS read (it cannot tell their targets apart).  They have no result register; the kernels
-// wait for them by count before the barrier that hands their target over.  Nothing else in these kernels uses m0.
+// wait for them by count before the barrier that hands their target over.
 __device__ __forceinline__ void load_lds16(const uint8_t* base, unsigned off, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "m0");
 }
 __device__ __forceinline__ void load_lds4(const uint8_t* base, unsigned off, unsigned lds)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(off), "s"(base) : "m0");
 }
 
 // What the kernels below have in common: a block's tile, its loads, fragments, scales and results.
