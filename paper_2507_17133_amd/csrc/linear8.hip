@@ -197,7 +197,10 @@ static void rows_go(const LinearArgs& p, hipStream_t s)
 // ------------------------------------------------------------------------------------------------
 // Direct loads to LDS, 16 or 4 bytes per lane: base (wave-uniform) + off -> lds + 16 (4) lane.  Written as instructions because the compiler puts a
 // wait for every such load in flight before each LDS read (it cannot tell their targets apart).  They have no result register; the kernels
-// wait for them by count before the barrier that hands their target over.
+// wait for them by count before the barrier that hands their target over.  m0 is reserved (nothing is kept there), which the compiler warns of where a
+// statement names it; named it must be, so that none comes between an instruction that reads m0 and what sets it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds16(const uint8_t* base, unsigned off, unsigned lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(off), "s"(base) : "m0");
@@ -206,6 +209,7 @@ __device__ __forceinline__ void load_lds4(const uint8_t* base, unsigned off, uns
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" : : "s"(lds), "v"(off), "s"(base) : "m0");
 }
+#pragma clang diagnostic pop
 
 // What the kernels below have in common: a block's tile, its loads, fragments, scales and results.
 template <int BM, int BN, int WM, int WN>
