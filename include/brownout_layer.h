@@ -83,7 +83,8 @@ moe_status moe_quantize_weight(const void *w, int32_t N, int32_t K, void *w8, fl
  * hundreds of times larger than its neighbours.  `exact` takes up to 2.2 times as long (many rows), for up to 64 rows 1.05 to 1.2.
  * K a multiple of 16 (MOE_ERR_SHAPE); M <= MOE_MAX_ROWS, N, K <= 2^20, x_stride <= 2^23 (MOE_ERR_UNSUPPORTED).  out overlaps no
  * input.  The workspace holds partial sums where the work is split along K: moe_linear_workspace_size bytes (0 for many shapes) for
- * exactly this M, N, K, 256-byte aligned.
+ * exactly this M, N, K, 256-byte aligned.  The size is not monotone in M (large products are not split): a workspace kept for
+ * batches of changing size has moe_linear_workspace_bound bytes, enough for every M up to M_max with this N and K.
  */
 typedef struct moe_linear_args {
     const void *x8; int64_t x_stride;
@@ -95,6 +96,7 @@ typedef struct moe_linear_args {
     int32_t exact;                            /* 0, or 1: exact products and fp32 sums for every K */
 } moe_linear_args;
 moe_status moe_linear_workspace_size(int32_t M, int32_t N, int32_t K, size_t *bytes);
+moe_status moe_linear_workspace_bound(int32_t M_max, int32_t N, int32_t K, size_t *bytes);
 moe_status moe_linear_e4m3(const moe_linear_args *a, void *workspace, size_t workspace_bytes, void *stream);
 
 /*

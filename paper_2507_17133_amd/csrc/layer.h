@@ -87,6 +87,7 @@ hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, con
 
 hipError_t init_linear_kernels();
 size_t linear_workspace_bytes(int M, int N, int K, bool exact);
+size_t linear_workspace_bound(int M_max, int N, int K);
 hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s);
 
 }  // namespace bmoe

@@ -151,6 +151,16 @@ moe_status moe_linear_workspace_size(int32_t M, int32_t N, int32_t K, size_t* by
     return MOE_OK;
 }
 
+moe_status moe_linear_workspace_bound(int32_t M_max, int32_t N, int32_t K, size_t* bytes)
+{
+    moe_status st = check_linear(M_max, N, K);
+    if (st != MOE_OK) return st;
+    if (!bytes) return MOE_ERR_INVALID_ARG;
+    *bytes = linear_workspace_bound(M_max, N, K);
+    if (ensure_device_init(nullptr) != hipSuccess) (void)hipGetLastError();      // as in moe_linear_workspace_size
+    return MOE_OK;
+}
+
 moe_status moe_linear_e4m3(const moe_linear_args* a, void* workspace, size_t workspace_bytes, void* stream)
 {
     if (!a) return MOE_ERR_INVALID_ARG;

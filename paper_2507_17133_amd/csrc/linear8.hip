@@ -705,6 +705,21 @@ size_t linear_workspace_bytes(int M, int N, int K, bool exact)
     return L.ksplit > 1 ? align_up((size_t)L.ksplit * (M - L.first_rows) * align_up(N, 4) * sizeof(float), 256) : 0;
 }
 
+// Enough for every M up to M_max.  The plan sees M in tiles of 64 rows, but for the partial sums' way, which makes fewer slices the better choice as M grows:
+// so the slices of the smallest M of a tile (33 of the first: fewer rows have a kernel of their own) are the most that its rows get.  Rows left
+// over by whole rounds of tiles are a product of fewer rows.
+size_t linear_workspace_bound(int M_max, int N, int K)
+{
+    if (K <= kShortK) return 0;
+    size_t rows = 0;                                      // slices x rows
+    double us;
+    for (int first = 33; first <= M_max; first = first == 33 ? 65 : first + 64) {
+        const int last = std::min(M_max, (first + 63) / 64 * 64), ks = one_way(first, N, K, false, us).ksplit;
+        if (ks > 1) rows = std::max(rows, (size_t)ks * last);
+    }
+    return align_up(rows * align_up(N, 4) * sizeof(float), 256);
+}
+
 hipError_t init_linear_kernels()
 {
     for (int way = kTile64; way < kWays; ++way) {

@@ -18,8 +18,8 @@ from .binding import MOE_OK, _check, _ptr, lib
 E4M3 = torch.float8_e4m3fn
 MOE_KV_BF16, MOE_KV_E4M3 = 0, 1
 ROPE_SCALINGS = ("none", "linear", "ntk", "yarn")
-EXPORTS = ("moe_rms_norm", "moe_quantize_rows", "moe_quantize_weight", "moe_linear_workspace_size", "moe_linear_e4m3",
-           "moe_rope_frequencies", "moe_rope_append", "moe_attention_workspace_size", "moe_paged_attention")
+EXPORTS = ("moe_rms_norm", "moe_quantize_rows", "moe_quantize_weight", "moe_linear_workspace_size", "moe_linear_workspace_bound",
+           "moe_linear_e4m3", "moe_rope_frequencies", "moe_rope_append", "moe_attention_workspace_size", "moe_paged_attention")
 
 
 class moe_norm_args(C.Structure):
@@ -68,6 +68,7 @@ def _lib():
             "moe_quantize_rows": [C.POINTER(moe_norm_args), p],
             "moe_quantize_weight": [p, i32, i32, p, p, p],
             "moe_linear_workspace_size": [i32, i32, i32, size],
+            "moe_linear_workspace_bound": [i32, i32, i32, size],
             "moe_linear_e4m3": [C.POINTER(moe_linear_args), p, C.c_size_t, p],
             "moe_rope_frequencies": [i32, C.c_double, C.POINTER(moe_rope_scaling), C.POINTER(C.c_double), C.POINTER(C.c_float)],
             "moe_rope_append": [C.POINTER(moe_kv_cache), C.POINTER(moe_block_table), C.POINTER(moe_rope), p, i64, p, i64, p, i64,
@@ -196,13 +197,22 @@ def moe_quantize_weight(w: torch.Tensor, stream=None):
 
 
 def linear_workspace_size(M: int, N: int, K: int) -> int:
+    """Bytes for exactly this product; not monotone in M."""
     n = C.c_size_t(0)
     _check(_lib().moe_linear_workspace_size(M, N, K, C.byref(n)), "moe_linear_workspace_size")
     return n.value
 
 
+def linear_workspace_bound(M_max: int, N: int, K: int) -> int:
+    """Bytes for every product of up to M_max rows."""
+    n = C.c_size_t(0)
+    _check(_lib().moe_linear_workspace_bound(M_max, N, K, C.byref(n)), "moe_linear_workspace_bound")
+    return n.value
+
+
 def alloc_linear_workspace(M: int, N: int, K: int, device="cuda") -> torch.Tensor:
-    return torch.empty(linear_workspace_size(M, N, K), dtype=torch.uint8, device=device)
+    """A workspace for every product of up to M rows with a weight [N, K]."""
+    return torch.empty(linear_workspace_bound(M, N, K), dtype=torch.uint8, device=device)
 
 
 def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w_scale: torch.Tensor, out: Optional[torch.Tensor] = None,
