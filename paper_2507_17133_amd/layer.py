@@ -4,6 +4,7 @@
 Like `binding`: argument marshalling only, no fallback path.  Tensors are on the current device; work goes to the
 current stream.  A call with `stream` is the same call under torch.cuda.stream(stream): what it allocates belongs to that stream.
 Tensors of other streams are the caller's to order before it, and to keep until it has run (Tensor.record_stream).
+There is no backward pass: a tensor that requires a gradient is refused unless gradients are off (torch.no_grad).
 """
 from __future__ import annotations
 
@@ -17,6 +18,7 @@ from .binding import MOE_OK, _check, _ptr, lib
 
 E4M3 = torch.float8_e4m3fn
 MOE_KV_BF16, MOE_KV_E4M3 = 0, 1
+NO_BACKWARD = "these operators have no backward pass: call them under torch.no_grad()"
 ROPE_SCALINGS = ("none", "linear", "ntk", "yarn")
 EXPORTS = ("moe_rms_norm", "moe_quantize_rows", "moe_quantize_weight", "moe_linear_workspace_size", "moe_linear_workspace_bound",
            "moe_linear_e4m3", "moe_rope_frequencies", "moe_rope_append", "moe_attention_workspace_size", "moe_paged_attention")
@@ -100,6 +102,7 @@ def _under(stream, call, *args):
 def _rows(t: torch.Tensor, dtype, rows: int, cols: int):
     """A [rows, cols] tensor whose rows are contiguous; returns its row stride."""
     assert t.is_cuda and t.dtype is dtype and t.shape == (rows, cols)
+    assert not (t.requires_grad and torch.is_grad_enabled()), NO_BACKWARD
     if t.is_contiguous():
         return cols
     assert cols == 1 or t.stride(1) == 1
@@ -141,6 +144,7 @@ def _norm(call, x, weight, eps, residual, want, out) -> NormOut:
         r, rs = residual.data_ptr(), _rows(residual, bf, T, d)
     if weight is not None:
         assert weight.is_cuda and weight.dtype is bf and weight.shape == (d,) and weight.is_contiguous()
+        assert not (weight.requires_grad and torch.is_grad_enabled()), NO_BACKWARD
         w = weight.data_ptr()
     if out is None:
         q = "y8" in want
@@ -190,6 +194,7 @@ def moe_quantize_weight(w: torch.Tensor, stream=None):
         return _under(stream, moe_quantize_weight, w)
     N, K = w.shape
     assert w.is_cuda and w.dtype is torch.bfloat16 and w.is_contiguous()
+    assert not (w.requires_grad and torch.is_grad_enabled()), NO_BACKWARD
     w8 = torch.empty((N, K), dtype=E4M3, device=w.device)
     scale = torch.empty((_groups(N), _groups(K)), dtype=torch.float32, device=w.device)
     _check(_lib().moe_quantize_weight(_ptr(w), N, K, _ptr(w8), _ptr(scale), _on(w)), "moe_quantize_weight")
@@ -226,6 +231,7 @@ def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w
     G = (K + 127) // 128
     assert w8.is_cuda and w8.dtype is E4M3 and w8.shape[1] == K and w8.is_contiguous()
     assert w_scale.is_cuda and w_scale.dtype is torch.float32 and w_scale.shape == (_groups(N), G) and w_scale.is_contiguous()
+    assert not ((w8.requires_grad or w_scale.requires_grad) and torch.is_grad_enabled()), NO_BACKWARD
     L = _ready or _lib()
     if out is None:
         out, out_stride = x8.new_empty((M, N), dtype=torch.bfloat16), N
@@ -252,6 +258,7 @@ class KvCache:
         e4m3 = k.dtype == E4M3
         assert k.is_cuda and v.is_cuda and k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
         assert k.stride(3) == 1 and (e4m3 or k.dtype == torch.bfloat16)
+        assert not ((k.requires_grad or v.requires_grad) and torch.is_grad_enabled()), NO_BACKWARD
         for s in (k_scale, v_scale):
             assert (s is not None) == e4m3, "scales belong to an e4m3 cache, and only to one"
             assert s is None or (s.is_cuda and s.dtype == torch.float32 and s.shape == (k.shape[2],) and s.is_contiguous())
@@ -312,6 +319,7 @@ def make_rope(rotary_dim: int, interleaved: bool = False, device="cuda", **frequ
 def _heads(t: torch.Tensor, T: int, heads: int, dim: int) -> int:
     """A [T, heads, dim] tensor whose heads are next to each other; returns its token stride."""
     assert t.is_cuda and t.dtype is torch.bfloat16 and t.shape == (T, heads, dim)
+    assert not (t.requires_grad and torch.is_grad_enabled()), NO_BACKWARD
     if t.is_contiguous():
         return heads * dim
     stride = t.stride()
