@@ -109,6 +109,12 @@ def _rows(t: torch.Tensor, dtype, rows: int, cols: int):
     return t.stride(0)
 
 
+def _bytes(workspace: torch.Tensor):
+    """Where a workspace is and how large."""
+    assert workspace.is_cuda and workspace.is_contiguous()
+    return workspace.data_ptr(), workspace.nbytes
+
+
 def _like(t: torch.Tensor, dtype=torch.bfloat16) -> torch.Tensor:
     return torch.empty_like(t, dtype=dtype) if t.is_contiguous() else t.new_empty(t.shape, dtype=dtype)
 
@@ -242,7 +248,7 @@ def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w
         workspace = x8.new_empty(need, dtype=torch.uint8) if need else None
     a = moe_linear_args(x8.data_ptr(), _rows(x8, E4M3, M, K), x_scale.data_ptr(), _rows(x_scale, torch.float32, G, M), w8.data_ptr(),
                         w_scale.data_ptr(), out.data_ptr(), out_stride, M, N, K, 1 if exact else 0)
-    st = L.moe_linear_e4m3(C.byref(a), None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _on(x8))
+    st = L.moe_linear_e4m3(C.byref(a), *((None, 0) if workspace is None else _bytes(workspace)), _on(x8))
     if st != MOE_OK:
         _check(st, "moe_linear_e4m3")
     return out
@@ -382,7 +388,7 @@ def moe_paged_attention(cache: KvCache, q: torch.Tensor, block_table: torch.Tens
     st = (_ready or _lib()).moe_paged_attention(
         cache.ref, C.byref(_table(block_table, table_row, T)), q.data_ptr(), _heads(q, T, H, D), H, T, _ints(lengths, T),
         D ** -0.5 if scale is None else scale, window, out.data_ptr(), out_stride, lse.data_ptr() if want_lse else None,
-        workspace.data_ptr(), workspace.numel(), _on(q))
+        *_bytes(workspace), _on(q))
     if st != MOE_OK:
         _check(st, "moe_paged_attention")
     return (out, lse) if want_lse else out
