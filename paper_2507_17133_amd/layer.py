@@ -133,6 +133,7 @@ class NormOut(NamedTuple):
 
 
 def alloc_norm_out(T: int, d: int, want=("y",), residual: bool = False, device="cuda") -> NormOut:
+    """What moe_rms_norm and moe_quantize_rows take as `out`: outputs that a program makes once."""
     bf, f32 = torch.bfloat16, torch.float32
     q = "y8" in want
     return NormOut(torch.empty((T, d), dtype=bf, device=device) if "y" in want else None,
