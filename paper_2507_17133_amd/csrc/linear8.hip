@@ -637,7 +637,9 @@ struct LinearPlan {
 //   128 x 128    0.65   1024 by 4096 x 7168 40.4, 40.7;     4096 by 4096 x 4096 93, 97
 //   128 x 256    1.06   2048 by 4096 x 4096 37.9, 40.3;     16384 by 7168 x 7168 861, 867
 //   256 x 256    1.72   4096 by 4096 x 4096 59, 62;         16384 by 7168 x 7168 690, 680
-// Up to 64 rows there is the rows kernel: its time goes with the weights, and from 33 rows on with the rows' trips as well.
+// Up to 64 rows there is the rows kernel: its time goes with the weights, and from 33 rows on with the rows' trips as well.  Its blocks take 32 columns where
+// blocks of 16 would be more than the CUs (16 and 32 columns, us, K = 4096: one row by 4096 6.0, 6.9, by 5120 8.6, 7.9, by 6144 8.7, 7.6, by 10240 11.8, 13.3, by 14336
+// 14.7, 14.3; 32 rows by 4096 8.6, 10.4, by 5120 15.0, 10.8, by 6144 15.3, 10.9, by 14336 28.4, 20.8; 64 rows, K = 512, by 4096 4.1, 4.2, by 6144 5.3, 4.4).
 // A last round that few CUs have a tile in costs as much as a full one, so the rows of whole rounds may go ahead, and the rest be cut in tiles
 // that suit it.
 static constexpr struct { int m, n; double block; } kTile[] = {
@@ -652,7 +654,7 @@ static double tile_rounds(int way, int64_t tiles, int blocks)
 static LinearPlan one_way(int M, int N, int K, bool wide, double& least)
 {
     LinearPlan best{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 0, 0, 0};
-    best.columns = ceil_div(N, 32) * ceil_div(M, best.rows) >= 192 ? 32 : 16;
+    best.columns = ceil_div(N, 16) * ceil_div(M, best.rows) > kCus ? 32 : 16;
     least = 4.0 + (M <= 16 ? 0.2e-6 : M <= 32 ? 0.28e-6 : 0.46e-6) * N * K;
     if (M <= 32 || (M <= 64 && wide)) return best;
     if (wide) {                                           // a tile is its loads and its store: large ones where they still fill the CUs

@@ -14,6 +14,7 @@ gpu = pytest.mark.gpu
 # rows kernel: (M, N, K, exact) -> row tiles, column tiles, blocks of K ahead, widened
 ROWS = [((10, 300, 640, 0), (1, 1, 4, 0)), ((16, 6144, 640, 0), (1, 2, 3, 0)), ((17, 300, 2064, 0), (2, 1, 4, 0)), ((32, 6144, 4096, 0), (2, 2, 3, 0)),
         ((20, 6150, 1040, 0), (2, 2, 3, 0)), ((50, 300, 640, 0), (4, 1, 2, 0)), ((50, 6160, 528, 0), (4, 2, 2, 0)), ((64, 6300, 528, 0), (4, 2, 2, 0)),
+        ((7, 4096, 640, 0), (1, 1, 4, 0)), ((7, 4100, 640, 0), (1, 2, 3, 0)), ((31, 5000, 1040, 0), (2, 2, 3, 0)), ((64, 5100, 512, 0), (4, 2, 1, 1)),
         ((10, 300, 512, 0), (1, 1, 1, 1)), ((3, 6144, 512, 0), (1, 2, 1, 1)), ((20, 300, 400, 0), (2, 1, 1, 1)), ((32, 6200, 272, 0), (2, 2, 1, 1)),
         ((64, 300, 512, 0), (4, 1, 1, 1)), ((50, 6144, 400, 0), (4, 2, 1, 1)), ((10, 300, 1040, 1), (1, 1, 4, 1)), ((10, 6144, 2064, 1), (1, 2, 3, 1)),
         ((20, 300, 4112, 1), (2, 1, 4, 1)), ((32, 6144, 4096, 1), (2, 2, 3, 1)), ((50, 300, 1040, 1), (4, 1, 2, 1)), ((64, 6200, 1552, 1), (4, 2, 2, 1))]
