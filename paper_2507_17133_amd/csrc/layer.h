@@ -20,10 +20,11 @@ __device__ __forceinline__ unsigned pack_e4m3(float a, float b, float c, float d
 
 // y / s to the last bit for the price of three multiplications: the product with the rounded 1 / s, corrected by its own remainder.  (Every pair of bf16
 // significands, of the value and of a group's largest, gives what the division gives; the product alone takes about one code in 1400 to its
-// neighbour.  The division itself: norm of 16384 x 7168 136 -> 145 us, its rows alone 63 -> 70, weight of 7168 x 7168 28 -> 34; this way 138, 64, 28.)
+// neighbour.  The division itself: norm of 16384 x 7168 136 -> 145 us, its rows alone 63 -> 70, weight of 7168 x 7168 28 -> 34; this way 137, 63, 28.)
 // An infinite s leaves y * 0; where y / s is beyond fp32's range the result is NaN.
 struct Divisor {
     float s, k;
+    __device__ __forceinline__ Divisor(float finite, float reciprocal) : s(finite), k(reciprocal) {}
     __device__ __forceinline__ explicit Divisor(float by) : s(by < __builtin_inff() ? by : 0.0f), k(1.0f / by) {}
     __device__ __forceinline__ float near(float y) const { return y * k; }                       // within 2 ulp
     __device__ __forceinline__ float exact(float y, float q) const { return __builtin_fmaf(-__builtin_fmaf(q, s, -y), k, q); }     // in this order -0 stays -0

@@ -26,7 +26,19 @@ struct NormArgs {
 // one says so in its scale.
 __device__ __forceinline__ unsigned abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
 
-__device__ __forceinline__ float group_scale(unsigned bits) { return __uint_as_float(max(bits, __float_as_uint(kLeastMagnitude))) / kE4m3Max; }
+// Its 448th part, rounded as the division rounds it (for every significand): a product, corrected by its remainder.
+__device__ __forceinline__ float group_scale(unsigned bits)
+{
+    const float m = __uint_as_float(max(bits, __float_as_uint(kLeastMagnitude))), q = m * (1.0f / kE4m3Max);
+    return m < __builtin_inff() ? __builtin_fmaf(-__builtin_fmaf(q, kE4m3Max, -m), 1.0f / kE4m3Max, q) : m;
+}
+
+// By a group's scale: at least 2^-64, infinite or NaN.  The hardware's reciprocal with one Newton step.
+__device__ __forceinline__ Divisor by_group_scale(float s)
+{
+    const float finite = s < __builtin_inff() ? s : 0.0f, r = __builtin_amdgcn_rcpf(s);
+    return Divisor(finite, __builtin_fmaf(__builtin_fmaf(-finite, r, 1.0f), r, r));
+}
 
 // A row's vectors of 8 columns are dealt out over `across` threads, NV each: vector v of thread i is columns 8 (v across + i) .., so 16 neighbouring lanes
 // hold one group of 128 columns.  ONE_ROW: the whole block, in as many waves as leave few lanes without a vector; else a wave per row, four to a block.
@@ -102,7 +114,7 @@ __global__ void __launch_bounds__(ONE_ROW ? 1024 : 256) norm_kernel(NormArgs p)
         for (int m = 8; m; m >>= 1) bits = max(bits, (unsigned)__shfl_xor((int)bits, m));
         const float s = group_scale(bits);
         if (c >= p.d) continue;
-        const Divisor div(lift_tiny(h[v], s));
+        const Divisor div = by_group_scale(lift_tiny(h[v], s));
         uint2 o;
         o.x = pack_e4m3(div(h[v][0]), div(h[v][1]), div(h[v][2]), div(h[v][3]));
         o.y = pack_e4m3(div(h[v][4]), div(h[v][5]), div(h[v][6]), div(h[v][7]));
@@ -169,7 +181,7 @@ __global__ void __launch_bounds__(256) quantize_weight_kernel(const bf16_t* __re
     for (int j = 0; j < 4; ++j) {
         const int n = n0 + 32 * j;
         if (n >= N || k0 >= K) continue;
-        const Divisor div(lift_tiny(v[j], s));
+        const Divisor div = by_group_scale(lift_tiny(v[j], s));
         uint4 o;
         o.x = pack_e4m3(div(v[j][0]), div(v[j][1]), div(v[j][2]), div(v[j][3]));
         o.y = pack_e4m3(div(v[j][4]), div(v[j][5]), div(v[j][6]), div(v[j][7]));

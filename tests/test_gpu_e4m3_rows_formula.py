@@ -56,3 +56,22 @@ def test_rows_of_the_norm(T, d):
     got = P.moe_rms_norm(x.cuda(), w.cuda(), 0.0, want=("y8",))
     assert torch.equal(got.scale.cpu(), s.t())
     assert torch.equal(got.y8.cpu().view(torch.uint8), want.contiguous().view(torch.uint8))
+
+
+def test_every_pair_of_significands():
+    """A group's largest value with each of the 128 significands that bf16 has, the other values with each of them and at many sizes below it."""
+    most, value = (1 + torch.arange(128) / 128.0 for _ in range(2))
+    below = [1, 2, 7, 8, 9, 13, 14, 15, 16, 17, 18, 19]
+    # rows: largest x size; columns: two groups of a largest value and half the significands
+    x = torch.zeros((128, len(below), 2, 128))
+    x[..., 0] = most[:, None, None]
+    for i, e in enumerate(below):
+        x[:, i, 0, 1:65], x[:, i, 1, 1:65] = value[:64] * 2.0 ** -e, value[64:] * 2.0 ** -e
+    x = x.reshape(-1, 256)
+    for size in (0, -90, -98, 100, 120):                   # whole rows scaled: the floor of a group's magnitude is 2^-100
+        rows = (x * 2.0 ** size).to(torch.bfloat16)
+        y = groups(rows.float())
+        s = y.abs().amax(2).clamp_min(FLOOR) / 448.0
+        got, scale = P.moe_quantize_rows(rows.cuda())
+        assert torch.equal(scale.cpu(), s.t())
+        assert torch.equal(got.cpu().view(torch.uint8), (y / s[:, :, None]).to(E4M3).reshape(-1, 256).view(torch.uint8))
