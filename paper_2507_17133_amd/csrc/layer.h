@@ -87,8 +87,15 @@ hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, con
                             hipStream_t s);
 
 hipError_t init_linear_kernels();
-size_t linear_workspace_bytes(int M, int N, int K, bool exact);
+// How a product is cut (linear8.hip).
+struct LinearPlan {
+    int way, ksplit, rows, columns;               // rows, columns: of the rows kernel's blocks
+    int first_way, first_rows;                    // rows that go ahead in tiles of their own (0: none)
+    bool wide;                                    // operands widened to bf16
+};
+LinearPlan linear_plan(int M, int N, int K, bool exact);
+size_t linear_workspace_bytes(const LinearPlan& plan, int M, int N);
 size_t linear_workspace_bound(int M_max, int N, int K);
-hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s);
+hipError_t launch_linear(const moe_linear_args& a, const LinearPlan& plan, void* ws, hipStream_t s);
 
 }  // namespace bmoe

@@ -145,7 +145,7 @@ moe_status moe_linear_workspace_size(int32_t M, int32_t N, int32_t K, size_t* by
     moe_status st = check_linear(M, N, K);
     if (st != MOE_OK) return st;
     if (!bytes) return MOE_ERR_INVALID_ARG;
-    *bytes = M > 0 ? linear_workspace_bytes(M, N, K, false) : 0;
+    *bytes = M > 0 ? linear_workspace_bytes(linear_plan(M, N, K, false), M, N) : 0;
     // a caller sizes its workspace before its first launch: the per-device set-up is done then, ahead of any stream capture
     if (ensure_device_init(nullptr) != hipSuccess) (void)hipGetLastError();
     return MOE_OK;
@@ -171,12 +171,13 @@ moe_status moe_linear_e4m3(const moe_linear_args* a, void* workspace, size_t wor
         return MOE_ERR_ALIGNMENT;
     if (a->x_scale_stride < a->M || a->out_stride < 0 || (a->M > 1 && a->out_stride < a->N)) return MOE_ERR_SHAPE;
     if (a->x_stride > kMaxRowBytes) return MOE_ERR_UNSUPPORTED;
-    const size_t need = linear_workspace_bytes(a->M, a->N, a->K, a->exact != 0);
+    const LinearPlan plan = linear_plan(a->M, a->N, a->K, a->exact != 0);
+    const size_t need = linear_workspace_bytes(plan, a->M, a->N);
     if (need > 0 && (!workspace || workspace_bytes < need)) return MOE_ERR_WORKSPACE;
     if (need > 0 && off(workspace, 256)) return MOE_ERR_ALIGNMENT;
     hipError_t e = ensure_device_init(nullptr);
     if (e != hipSuccess) return hip_fail(e, "moe_linear_e4m3/init");
-    e = launch_linear(*a, workspace, static_cast<hipStream_t>(stream));
+    e = launch_linear(*a, plan, workspace, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? MOE_OK : hip_fail(e, "moe_linear_e4m3");
 }
 

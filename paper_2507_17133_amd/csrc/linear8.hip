@@ -624,11 +624,6 @@ static auto with_tile(int way, F&& f)
     }
 }
 
-struct LinearPlan {
-    int way, ksplit, rows, columns;               // rows, columns: of the rows kernel's blocks
-    int first_way, first_rows;                    // rows that go ahead in tiles of their own (0: none)
-};
-
 // The way that should take the least time.  A CU works on one tile at a time, so a product takes rounds of tiles; a tile takes 2 us (its first loads,
 // its store) and for every block of K what is listed, from products of 2048 to 16384 rows; a launch takes 2 us.  Small tiles may be cut along K
 // as well, which costs a second launch and the partial sums' way to memory and back.  Foretold and measured (us), K blocks:
@@ -653,7 +648,7 @@ static double tile_rounds(int way, int64_t tiles, int blocks)
 
 static LinearPlan one_way(int M, int N, int K, bool wide, double& least)
 {
-    LinearPlan best{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 0, 0, 0};
+    LinearPlan best{kRows, 1, M <= 16 ? 16 : M <= 32 ? 32 : 64, 0, 0, 0, wide};
     best.columns = ceil_div(N, 16) * ceil_div(M, best.rows) > kCus ? 32 : 16;
     least = 4.0 + (M <= 16 ? 0.2e-6 : M <= 32 ? 0.28e-6 : 0.46e-6) * N * K;
     if (M <= 32 || (M <= 64 && wide)) return best;
@@ -673,14 +668,15 @@ static LinearPlan one_way(int M, int N, int K, bool wide, double& least)
             if (ks > 1) us += 2.5 + 2e-6 * M * N * ks;
             if (us < least) {
                 least = us;
-                best = {way, ks, 0, 0, 0, 0};
+                best = {way, ks, 0, 0, 0, 0, false};
             }
         }
     return best;
 }
 
-static LinearPlan linear_plan(int M, int N, int K, bool wide)
+LinearPlan linear_plan(int M, int N, int K, bool exact)
 {
+    const bool wide = exact || K <= kShortK;
     double least, rest;
     LinearPlan best = one_way(M, N, K, wide, least);
     if (wide || M <= 128) return best;
@@ -701,9 +697,8 @@ static LinearPlan linear_plan(int M, int N, int K, bool wide)
     return best;
 }
 
-size_t linear_workspace_bytes(int M, int N, int K, bool exact)
+size_t linear_workspace_bytes(const LinearPlan& L, int M, int N)
 {
-    const LinearPlan L = linear_plan(M, N, K, exact || K <= kShortK);
     return L.ksplit > 1 ? align_up((size_t)L.ksplit * (M - L.first_rows) * align_up(N, 4) * sizeof(float), 256) : 0;
 }
 
@@ -733,10 +728,8 @@ hipError_t init_linear_kernels()
     return hipSuccess;
 }
 
-hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s)
+hipError_t launch_linear(const moe_linear_args& a, const LinearPlan& L, void* ws, hipStream_t s)
 {
-    const bool wide = a.exact || a.K <= kShortK;
-    const LinearPlan L = linear_plan(a.M, a.N, a.K, wide);
     LinearArgs p;
     p.x = static_cast<const uint8_t*>(a.x8); p.w = static_cast<const uint8_t*>(a.w8);
     p.xs = a.x_scale; p.ws = a.w_scale;
@@ -745,7 +738,7 @@ hipError_t launch_linear(const moe_linear_args& a, void* ws, hipStream_t s)
     p.x_stride = a.x_stride; p.xs_stride = a.x_scale_stride; p.out_stride = a.out_stride;
     p.M = a.M; p.N = a.N; p.K = a.K; p.nk = ceil_div(a.K, kScaleGroup);
     p.part_stride = (int)align_up(a.N, 4);
-    p.wide = wide;
+    p.wide = L.wide;
     p.vec = (a.out_stride & 3) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 7u) == 0;
     p.vec16 = (a.out_stride & 7) == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0;
     auto tiles = [&](int way) {

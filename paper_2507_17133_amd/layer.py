@@ -18,6 +18,7 @@ from .binding import MOE_OK, _check, _ptr, lib
 
 E4M3 = torch.float8_e4m3fn
 MOE_KV_BF16, MOE_KV_E4M3 = 0, 1
+MOE_ERR_WORKSPACE = -4
 NO_BACKWARD = "these operators have no backward pass: call them under torch.no_grad()"
 ROPE_SCALINGS = ("none", "linear", "ntk", "yarn")
 EXPORTS = ("moe_rms_norm", "moe_quantize_rows", "moe_quantize_weight", "moe_linear_workspace_size", "moe_linear_workspace_bound",
@@ -244,12 +245,12 @@ def moe_linear_e4m3(x8: torch.Tensor, x_scale: torch.Tensor, w8: torch.Tensor, w
         out, out_stride = x8.new_empty((M, N), dtype=torch.bfloat16), N
     else:
         out_stride = _rows(out, torch.bfloat16, M, N)
-    if workspace is None:
-        need = linear_workspace_size(M, N, K)
-        workspace = x8.new_empty(need, dtype=torch.uint8) if need else None
     a = moe_linear_args(x8.data_ptr(), _rows(x8, E4M3, M, K), x_scale.data_ptr(), _rows(x_scale, torch.float32, G, M), w8.data_ptr(),
                         w_scale.data_ptr(), out.data_ptr(), out_stride, M, N, K, 1 if exact else 0)
     st = L.moe_linear_e4m3(C.byref(a), *((None, 0) if workspace is None else _bytes(workspace)), _on(x8))
+    if st == MOE_ERR_WORKSPACE and workspace is None:      # most products need none
+        workspace = x8.new_empty(linear_workspace_size(M, N, K), dtype=torch.uint8)
+        st = L.moe_linear_e4m3(C.byref(a), *_bytes(workspace), _on(x8))
     if st != MOE_OK:
         _check(st, "moe_linear_e4m3")
     return out
