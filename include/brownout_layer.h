@@ -181,7 +181,7 @@ moe_status moe_rope_append(const moe_kv_cache *cache, const moe_block_table *tab
  *   of out shares memory with one of q (MOE_ERR_INVALID_ARG)
  *   lse [T][n_heads] fp32 or NULL: log of the sum of exp(scale * q . k), to join attention over several caches
  * The tokens of a prompt's chunk are T rows with lengths position + 1, appended first.
- * Scores and sums are fp32; the probabilities are rounded to bf16 for the product with v (its sum is of the unrounded ones).
+ * Scores and sums are fp32; for the product with v a probability is two bf16 that add up to it within 2^-15 of it.
  * The workspace (moe_attention_workspace_size: for up to T_max tokens of n_heads heads on such a cache, 256-byte aligned) needs no
  * initialisation.  Every token's cache is cut into equal shares of the call's whole work, so one long sequence among
  * short ones is shared by the whole GPU.

@@ -4,8 +4,8 @@
 //
 // One pass: a row's vectors stay in the registers of the threads that share it between the sum of squares and the outputs, so every
 // input is read once and every output written once: HBM bound.  The norm's inputs and the residual, whose next reader is far off, pass by the caches, and so do large bf16
-// rows (16384 x 7168 with residual to e4m3 149 -> 137 us, 6.0 TB/s; 256 x 4096 5.1 -> 4.2); e4m3 rows stay for the product that reads them (8-byte
-// stores past the caches are slower besides: 142).  One row of 4096: 2.4 us, latency.
+// rows (16384 x 7168 with residual to e4m3 149 -> 137 us, 6.0 TB/s, in a graph over sets of inputs; 256 x 4096 5.1 -> 4.2); e4m3 rows stay for the product that reads them (8-byte
+// stores past the caches are slower besides: 142).  One row of 2048: 2.4 us, latency.
 #include "layer.h"
 
 #include <type_traits>
@@ -149,7 +149,7 @@ hipError_t launch_norm(const moe_norm_args& a, bool norm, hipStream_t s)
 }
 
 // One block per 128 x 128 block of the weight, whose values stay in registers between the maximum and the store (16 columns of four rows per
-// thread): one pass, HBM bound.  7168 x 7168 23 us (6.6 TB/s, part of it from the caches).
+// thread): one pass, HBM bound.  7168 x 7168 27 us (5.6 TB/s, six weights in turn).
 __global__ void __launch_bounds__(256) quantize_weight_kernel(const bf16_t* __restrict__ w, int N, int K, uint8_t* __restrict__ w8,
                                                               float* __restrict__ scale)
 {
