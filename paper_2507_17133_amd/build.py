@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libbrownout_moe.so")
 SOURCES = ["api.hip", "route.hip", "ffn.hip", "united.hip", "salc.hip", "distill.hip", "probe.hip", "norm.hip",
-           "rope.hip", "attention.hip", "linear8.hip", "layer_api.hip"]
+           "rope.hip", "attention.hip", "linear8.hip", "layer_api.hip", "chunk.hip", "move.hip", "logprob.hip", "draft_api.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

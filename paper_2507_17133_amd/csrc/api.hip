@@ -1,6 +1,6 @@
 // C ABI of libbrownout_moe.so: argument validation, workspace carving, kernel sequencing, profiling.
 #include "internal.h"
-#include "layer.h"
+#include "draft.h"
 #include "tiles.h"
 
 #include <algorithm>
@@ -63,6 +63,7 @@ hipError_t ensure_device_init(DeviceInfo* info)
         if ((e = init_distill_kernels()) != hipSuccess) return e;
         if ((e = init_attention_kernels()) != hipSuccess) return e;
         if ((e = init_linear_kernels()) != hipSuccess) return e;
+        if ((e = init_chunk_kernels()) != hipSuccess) return e;
         int n_cu = 0;
         if ((e = hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, dev)) != hipSuccess) return e;
         void* sp = nullptr;

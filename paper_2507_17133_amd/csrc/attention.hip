@@ -63,7 +63,7 @@ struct AttnArgs {
     int T, H, Hk, group, q_tiles, heads;          // heads: query heads of a key head that a wave takes (at most 16)
     int side, tile;                               // key heads side by side in a block; positions of its step
     float scale;
-    int window;
+    int window, sinks;                            // sinks: first positions that a window leaves visible
     bf16_t* out;
     int64_t out_stride;
     float* lse;
@@ -82,7 +82,12 @@ __device__ __forceinline__ int2 span_of(const AttnArgs& p, int t)
     const bool there = (unsigned)row < (unsigned)p.n_rows;
     return make_int2(p.window > 0 ? max(hi - p.window, 0) : 0, there ? hi : 0);
 }
-__device__ __forceinline__ int tiles_of(const AttnArgs& p, const int2 s) { return s.y > s.x ? (int)((unsigned)(s.y - s.x - 1) / (unsigned)p.tile) + 1 : 0; }
+// Positions below lo that it attends to besides: the first ones.
+__device__ __forceinline__ int sinks_of(const AttnArgs& p, const int2 s) { return min(p.sinks, s.x); }
+__device__ __forceinline__ int tiles_of(const AttnArgs& p, const int2 s)
+{
+    return s.y > s.x ? (int)((unsigned)(s.y - s.x + sinks_of(p, s) - 1) / (unsigned)p.tile) + 1 : 0;
+}
 __device__ __forceinline__ int items_of(const AttnArgs& p) { return p.Hk / p.side * p.q_tiles; }
 
 // The block's share of the line of tiles: its bounds, and where it begins.
@@ -146,7 +151,7 @@ __device__ __forceinline__ Share find_share(const AttnArgs& p, int64_t* lds)
 struct Place {
     int64_t at;                                   // its number in the line
     int t, item, tile, n;                         // n: tiles of the token's items
-    int lo, hi;                                   // positions that the token attends to
+    int lo, sinks, n_pos;                         // its positions: the first `sinks`, then those from lo on, n_pos in all
     int hk, h0, nh;                               // the wave's key head, its first query head and number of those
     const int32_t* row;                           // the token's row of the block table
 
@@ -154,7 +159,8 @@ struct Place {
     {
         const int2 s = span_of(p, t);
         lo = s.x;
-        hi = s.y;
+        sinks = sinks_of(p, s);
+        n_pos = s.y - s.x + sinks;
         n = tiles_of(p, s);
     }
     __device__ __forceinline__ void heads(const AttnArgs& p, int sub)
@@ -395,9 +401,10 @@ __global__ void __launch_bounds__(kAttnThreads, attention_resident(D, E4M3)) att
     unsigned koff[2], voff[8];
     // page of the lane's position (lanes 0..31) of the wave in a tile, -1 beyond the end
     auto page_of = [&](const Place& w, unsigned& in_page) -> int {
-        const unsigned pos = (unsigned)w.lo + (unsigned)w.tile * p.tile + behind * kStep + (lane & 31);
+        const unsigned nth = (unsigned)w.tile * p.tile + behind * kStep + (lane & 31);
         in_page = 0;
-        if (pos >= (unsigned)w.hi) return -1;
+        if (nth >= (unsigned)w.n_pos) return -1;
+        const unsigned pos = nth < (unsigned)w.sinks ? nth : nth - w.sinks + w.lo;
         const unsigned pg = (unsigned)((uint64_t)pos * p.page_magic >> p.page_shift);
         in_page = pos - pg * (unsigned)p.page_size;
         return w.row[pg];
@@ -718,7 +725,7 @@ static hipError_t attention_go(const AttnArgs& p, bool e4m3, int grid, hipStream
 }
 
 hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, const bf16_t* q, int64_t q_stride, int n_heads, int T,
-                            const int32_t* lengths, float scale, int window, bf16_t* out, int64_t out_stride, float* lse, void* ws,
+                            const int32_t* lengths, float scale, int window, int sinks, bf16_t* out, int64_t out_stride, float* lse, void* ws,
                             hipStream_t s)
 {
     AttnArgs p;
@@ -739,12 +746,12 @@ hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, con
     p.q = q; p.q_stride = q_stride; p.lengths = lengths;
     p.T = T; p.H = n_heads; p.Hk = c.n_kv_heads; p.group = n_heads / c.n_kv_heads;
     p.q_tiles = ceil_div(p.group, 16); p.heads = item_heads(p.group);
-    p.scale = scale; p.window = window;
+    p.scale = scale; p.window = window; p.sinks = sinks;
     p.out = out; p.out_stride = out_stride; p.lse = lse;
     p.cuts = static_cast<int4*>(ws);
     p.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(kAttnBlocks * sizeof(int4), 256));
     // no more shares than there can be tiles
-    const int64_t longest = window > 0 ? std::min(window, p.cap) : p.cap;
+    const int64_t longest = window > 0 ? std::min<int64_t>((int64_t)window + sinks, p.cap) : p.cap;
     p.side = heads_side_by_side(c, p.heads, T, longest);
     p.tile = kStep * kAttnWaves / p.side;
     const int64_t most = (int64_t)T * (p.Hk / p.side) * p.q_tiles * ((longest + p.tile - 1) / p.tile);

@@ -1,0 +1,791 @@
+// Attention of sequences' new tokens (a tree of drafted ones, a chunk of a prompt) over a paged key-value cache, each tile of it read once for all
+// the rows that share it.
+//
+//   out = sum_p softmax_p(scale q . k_p) v_p in one pass: running maximum m, running sum l and the running weighted sum O of v.
+//
+// A sequence's rows are its (new token, query head of a key head) pairs, token by token.  An item is a tile of up to ROWS rows of one key head; a block
+// goes through the item's positions STEP at a time.  K and V of a step lie in LDS as [64 columns][position], 16-byte pieces of a row exchanged so that
+// neither of the two ways they are read meets a bank twice; while one step is worked on the next is on its way to registers (e4m3 is widened
+// when it goes to LDS).  Each wave has 32 or 64 of the rows and, where rows are few, its part of the positions:
+//   S [32 positions][32 rows] = K Q^T,     O^T [D][32 rows] += V^T P^T          (32 x 32 x 16 MFMAs)
+// S leaves lane (g, c) = (lane / 32, lane % 32) with row c at positions 8 j + 4 g + 0..3: already the layout of P^T as the second operand, its 8
+// positions in the order {16 t + 4 g + 0..3, 16 t + 8 + 4 g + 0..3}; V^T is read in the same order by transposing LDS reads.  Maximum, sum and rescaling
+// are per row = per lane and its other half.  The maximum that exponentials refer to follows the true one at a distance of at most 2^kSlack, so O is
+// hardly ever rescaled.
+//
+// A position counts for some rows of an item and not for others; its probability is then 0 for these, but 0 times a NaN or an infinity of V is NaN.  A
+// part whose result is not finite is computed once more with the second product in fp32 lane by lane, which skips such places.
+#include "draft.h"
+
+#include <algorithm>
+#include <type_traits>
+
+namespace bmoe {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int kChunkWaves = 4, kChunkThreads = 64 * kChunkWaves;
+constexpr int kChunkShares = 512;                 // shares of the line of steps at most
+constexpr float kSlack = 4.0f;                    // how far (in powers of two) scores may exceed the maximum that they refer to
+constexpr int kMostContext = 0x7FFE0000;          // so that positions of new tokens stay in 32 bits
+
+// Rows per block 32 * RB * WM: WM waves with RB blocks of 32 rows each; WK waves share the positions of a step, PB blocks of 32 each.
+template <int D_, bool E4M3_, int RB_, int WM_, int WK_, int PB_>
+struct Shape {
+    static constexpr int D = D_, RB = RB_, WM = WM_, WK = WK_, PB = PB_;
+    static constexpr bool E4M3 = E4M3_;
+    static_assert(WM * WK == kChunkWaves, "four waves");
+    static constexpr int ROWS = 32 * RB * WM, STEP = 32 * PB * WK;
+    static constexpr int N64 = D / 64, N32 = D % 64 / 32;                     // panels of 64 columns, and one of 32
+    static constexpr int TILE = STEP * D * 2;                                 // bytes of K (of V) of a step in LDS
+    static constexpr int KS = D / 16, VS = D / 32;                            // products along D, blocks of 32 columns of V
+    static constexpr int SCRATCH = kChunkWaves * 32 * 32 * 4;                 // probabilities of the careful second product
+    static constexpr int JOIN = WK > 1 ? (WK - 1) * WM * 32 * RB * (D + 4) * 4 : 0;
+    static constexpr int LDS = (4 * TILE > JOIN ? 4 * TILE : JOIN) + SCRATCH;
+    static constexpr int RESIDENT = LDS <= 80 * 1024 && RB * D <= 128 ? 2 : 1;   // blocks of a CU
+    // floats of a part: [ROWS][D] O, [ROWS] m, [ROWS] l
+    static constexpr int64_t PART = (int64_t)ROWS * (D + 2);
+};
+
+struct ChunkArgs {
+    const char *kc, *vc;
+    int64_t head_stride;                          // bytes
+    unsigned page_step, token_step;               // a page's and a position's stride in 16-byte steps
+    const float *k_scale, *v_scale;
+    const int32_t *pages, *row_of;
+    int64_t row_stride;
+    int n_rows, n_pages, page_size;
+    unsigned page_magic;                          // position / page_size = position * page_magic >> page_shift
+    int page_shift;
+    int cap;                                      // positions that a row of the block table has
+    const bf16_t* q;
+    int64_t q_stride;
+    const int32_t *first, *context, *positions;
+    const uint32_t* seen;
+    int64_t seen_stride;
+    int words, n_seqs, T, H, Hk, group, window, sinks;
+    float scale;
+    bf16_t* out;
+    int64_t out_stride;
+    float* lse;
+    int whole;                                    // one block for each item; else shares of the line of steps
+    int4* cuts;                                   // per share: the item that it begins and does not end (sequence, tile, key head, shares)
+    float* parts;                                 // per share two parts
+};
+
+// A sequence's tokens, cut to what the call has.
+struct Seq {
+    int t0, n, context;
+    __device__ __forceinline__ Seq(const ChunkArgs& p, int b)
+    {
+        t0 = min(max(p.first[b], 0), p.T);
+        n = min(max(p.first[b + 1], t0), p.T) - t0;
+        context = min(max(p.context[b], 0), kMostContext);
+    }
+    __device__ __forceinline__ int row_tiles(const ChunkArgs& p, int rows) const { return (n * p.group + rows - 1) / rows; }
+};
+
+// The positions of a tile of rows: the first `sinks`, then those from lo on, n in all.
+struct Span {
+    int sinks, lo, n;
+    __device__ __forceinline__ Span(const ChunkArgs& p, const Seq& s, int tile, int rows, bool there)
+    {
+        const int j0 = tile * rows / p.group, j1 = min(s.n - 1, (tile * rows + rows - 1) / p.group);
+        const int hi = there ? min(s.context + (p.seen ? s.n : j1 + 1), p.cap) : 0;
+        lo = p.window > 0 ? min(max(s.context + (p.seen ? 0 : j0) + 1 - p.window, 0), hi) : 0;
+        sinks = min(p.sinks, lo);
+        n = hi - lo + sinks;
+    }
+    template <int STEP>
+    __device__ __forceinline__ int steps() const { return max(1, (n + STEP - 1) / STEP); }       // an item with nothing to see has its rows cleared
+};
+
+__device__ __forceinline__ int table_row(const ChunkArgs& p, int b) { return p.row_of ? p.row_of[b] : b; }
+
+// Steps of a sequence's items of one key head.
+template <class S>
+__device__ __forceinline__ int64_t steps_of(const ChunkArgs& p, int b)
+{
+    const Seq s(p, b);
+    const bool there = (unsigned)table_row(p, b) < (unsigned)p.n_rows;
+    const int tiles = s.row_tiles(p, S::ROWS);
+    if (tiles == 0) return 0;
+    if (p.seen) return (int64_t)tiles * Span(p, s, 0, S::ROWS, there).template steps<S::STEP>();
+    int64_t n = 0;
+    for (int i = 0; i < tiles; ++i) n += Span(p, s, i, S::ROWS, there).template steps<S::STEP>();
+    return n;
+}
+
+// Where a block begins in the line of steps, and how many it has.
+struct Begin {
+    int b, tile, hk, step;
+    int64_t at, end, per;
+};
+
+__device__ __forceinline__ int64_t sum_before(int64_t v, int lane, int64_t& total)
+{
+    int64_t x = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t y = __shfl_up(x, o);
+        if (lane >= o) x += y;
+    }
+    total = __shfl(x, 63);
+    return x - v;
+}
+
+template <class S>
+__device__ __forceinline__ bool find_share(const ChunkArgs& p, int64_t* lds, Begin& o)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int each = (p.n_seqs + kChunkThreads - 1) / kChunkThreads, b0 = min(p.n_seqs, tid * each), b1 = min(p.n_seqs, b0 + each);
+    int64_t mine = 0;
+    for (int b = b0; b < b1; ++b) mine += steps_of<S>(p, b) * p.Hk;
+    int64_t total;
+    int64_t before = sum_before(mine, lane, total);
+    if (lane == 0) lds[wave] = total;
+    __syncthreads();
+    int64_t all = 0;
+#pragma unroll
+    for (int w = 0; w < kChunkWaves; ++w) {
+        if (w < wave) before += lds[w];
+        all += lds[w];
+    }
+    o.per = (all + gridDim.x - 1) / gridDim.x;
+    o.at = min(all, o.per * (int64_t)blockIdx.x);
+    o.end = min(all, o.at + o.per);
+    if (o.at >= o.end) return false;
+    // the one thread whose sequences hold the first step looks for it
+    if (before <= o.at && o.at < before + mine) {
+        int b = b0;
+        for (;; ++b) {
+            const int64_t n = steps_of<S>(p, b) * p.Hk;
+            if (o.at < before + n) break;
+            before += n;
+        }
+        const Seq s(p, b);
+        const bool there = (unsigned)table_row(p, b) < (unsigned)p.n_rows;
+        int tile = 0, n = 0;
+        for (;; ++tile) {
+            n = Span(p, s, tile, S::ROWS, there).template steps<S::STEP>();
+            if (o.at < before + (int64_t)n * p.Hk) break;
+            before += (int64_t)n * p.Hk;
+        }
+        lds[kChunkWaves] = b;
+        lds[kChunkWaves + 1] = tile;
+        lds[kChunkWaves + 2] = (o.at - before) / n;
+        lds[kChunkWaves + 3] = (o.at - before) % n;
+    }
+    __syncthreads();
+    o.b = __builtin_amdgcn_readfirstlane((int)lds[kChunkWaves]);
+    o.tile = __builtin_amdgcn_readfirstlane((int)lds[kChunkWaves + 1]);
+    o.hk = __builtin_amdgcn_readfirstlane((int)lds[kChunkWaves + 2]);
+    o.step = __builtin_amdgcn_readfirstlane((int)lds[kChunkWaves + 3]);
+    __syncthreads();
+    return true;
+}
+
+// One block for each item.  Sequence b's tiles have the places from floor(first[b] * group / ROWS) + b on, which is room enough for them; the blocks
+// in between have none.  Late tiles of a chunk, which see the most, come first.
+template <class S>
+__device__ __forceinline__ bool find_item(const ChunkArgs& p, Begin& o)
+{
+    const int lane = threadIdx.x & 63, slots = gridDim.x / p.Hk, u = slots - 1 - (int)(blockIdx.x / p.Hk);
+    auto place = [&](int b) { return (int)((int64_t)min(max(p.first[b], 0), p.T) * p.group / S::ROWS) + b; };
+    // the last sequence whose place is not beyond u, 64 of a stride at a time
+    int lo = 0, n = p.n_seqs;
+    while (n > 1) {
+        const int stride = (n + 63) / 64, b = lo + lane * stride;
+        const bool is = lane * stride < n && place(b) <= u;
+        const uint64_t m = __ballot(is);
+        const int k = m ? 63 - __builtin_clzll(m) : 0;
+        lo = __builtin_amdgcn_readfirstlane(lo + k * stride);
+        n = __builtin_amdgcn_readfirstlane(min(stride, n - k * stride));
+    }
+    o.b = lo;
+    const Seq s(p, lo);
+    o.tile = u - place(lo);
+    o.hk = blockIdx.x % p.Hk;
+    o.step = 0;
+    return o.tile >= 0 && o.tile < s.row_tiles(p, S::ROWS);
+}
+
+template <bool E4M3>
+using pv8 = std::conditional_t<E4M3, f16x8, bf16x8>;
+
+template <bool HIGH>
+__device__ __forceinline__ unsigned to_bf16(unsigned w) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HIGH)); }
+template <bool HIGH>
+__device__ __forceinline__ unsigned to_f16(unsigned w) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH)); }
+
+// Byte of (row, 16-byte piece of the row's columns) in a step's K or V.
+template <class S>
+__device__ __forceinline__ int piece_at(int row, int piece)
+{
+    if (S::N32 == 0 || piece < 8 * S::N64) return (piece >> 3) * S::STEP * 128 + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+    return S::N64 * S::STEP * 128 + row * 64 + (((piece & 3) ^ (row >> 1 & 3)) << 4);
+}
+
+template <class S>
+__global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(ChunkArgs p)
+{
+    constexpr int D = S::D, RB = S::RB, WM = S::WM, WK = S::WK, PB = S::PB, STEP = S::STEP, POS = STEP / 64;
+    constexpr bool E4M3 = S::E4M3;
+    using Half = pv8<E4M3>;
+    // e4m3: probabilities as fp16, exactly enough for V's 4 bits; 2^kUp of them, so that small ones are not lost below fp16's range
+    constexpr float kUp = E4M3 ? 11.0f : 0.0f;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c = lane & 31, g = lane >> 5, wm = wave % WM, wk = wave / WM;
+    int64_t* found = reinterpret_cast<int64_t*>(smem + S::LDS - S::SCRATCH);      // at the kernel's start; flags of the waves later
+    float* scratch = reinterpret_cast<float*>(smem + S::LDS - S::SCRATCH) + wave * 32 * 32;
+
+    Begin at;
+    if (p.whole) {
+        if (!find_item<S>(p, at)) return;
+    } else {
+        if (tid == 0) p.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (!find_share<S>(p, found, at)) return;
+    }
+
+    for (;;) {
+        // ---------------- an item, or what the share has of it
+        const Seq seq(p, at.b);
+        const int row = table_row(p, at.b);
+        const Span span(p, seq, at.tile, S::ROWS, (unsigned)row < (unsigned)p.n_rows);
+        const int32_t* pages = p.pages + (int64_t)row * p.row_stride;
+        const int steps = span.template steps<STEP>(), begin = at.step;
+        const int end = p.whole ? steps : (int)min((int64_t)steps, at.step + (at.end - at.at));
+        const int n_rows = seq.n * p.group;
+        const char *kbase = p.kc + (int64_t)at.hk * p.head_stride, *vbase = p.vc + (int64_t)at.hk * p.head_stride;
+        float to_log2 = p.scale * 1.4426950408889634f * (E4M3 ? p.k_scale[at.hk] : 1.0f);
+        const unsigned flip = to_log2 < 0.0f ? 0x80008000u : 0u;              // the sign goes to q, so that the largest product is the largest score
+        to_log2 = to_log2 != to_log2 ? to_log2 : fmaxf(fabsf(to_log2), 1.17549435e-38f);       // above 0: 0 times a masked -infinity would be NaN
+
+        // rows of this lane: where their results go, what they see
+        int token[RB], head[RB], last[RB], from[RB];
+        bool real[RB];
+        bf16x8 q[RB][S::KS];
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+            const int i = at.tile * S::ROWS + (wm * RB + r) * 32 + c, j = min(i, n_rows - 1) / p.group;
+            real[r] = i < n_rows;
+            token[r] = seq.t0 + j;
+            head[r] = at.hk * p.group + (real[r] ? i - j * p.group : 0);
+            int pos = seq.context + j;
+            if (p.positions) pos = max(seq.context, p.positions[token[r]]);
+            last[r] = p.seen ? seq.context - 1 : pos;
+            from[r] = p.window > 0 ? pos - p.window + 1 : 0;                  // may be negative
+            const bf16_t* src = p.q + (int64_t)token[r] * p.q_stride + (int64_t)head[r] * D;
+#pragma unroll
+            for (int k = 0; k < S::KS; ++k) {
+                uint4 v = make_uint4(0, 0, 0, 0);
+                if (real[r]) v = *reinterpret_cast<const uint4*>(src + 16 * k + 8 * g);
+                v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
+                q[r][k] = __builtin_bit_cast(bf16x8, v);
+            }
+        }
+
+        f32x16 acc[RB][S::VS];
+        float m[RB], l[RB];
+
+        // ---------------- where a step's positions are: lane i has those of positions i, 64 + i, ...
+        unsigned off[POS];
+        uint64_t there[POS], there_next[POS];
+        int page[POS];
+        unsigned in_page[POS];
+        auto look = [&](int step) {
+#pragma unroll
+            for (int k = 0; k < POS; ++k) {
+                const int v = step * STEP + 64 * k + lane;
+                page[k] = -1;
+                in_page[k] = 0;
+                if (step < end && v < span.n) {
+                    const unsigned pos = v < span.sinks ? v : v - span.sinks + span.lo;
+                    const unsigned pg = (unsigned)((uint64_t)pos * p.page_magic >> p.page_shift);
+                    in_page[k] = pos - pg * (unsigned)p.page_size;
+                    page[k] = pages[pg];
+                }
+            }
+        };
+        auto resolve = [&]() {
+#pragma unroll
+            for (int k = 0; k < POS; ++k) {
+                const bool is = (unsigned)page[k] < (unsigned)p.n_pages;
+                off[k] = is ? (unsigned)page[k] * p.page_step + in_page[k] * p.token_step : 0;
+                there_next[k] = __ballot(is);
+            }
+        };
+        // ---------------- a step's K and V, to registers and from there to LDS
+        constexpr int ACROSS = E4M3 ? D / 16 : D / 8;                         // 16-byte pieces of a row in the cache
+        constexpr int PIECES = (STEP * ACROSS + kChunkThreads - 1) / kChunkThreads;
+        uint4 kraw[PIECES], vraw[PIECES];
+        auto issue = [&]() {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int id = i * kChunkThreads + tid, r = id / ACROSS, piece = id - r * ACROSS;
+                unsigned o = __shfl(off[0], r & 63);
+                bool is = there_next[0] >> (r & 63) & 1;
+                if constexpr (POS > 1) {
+                    const unsigned o1 = __shfl(off[POS - 1], r & 63);
+                    const bool is1 = there_next[POS - 1] >> (r & 63) & 1;
+                    o = r < 64 ? o : o1;
+                    is = r < 64 ? is : is1;
+                }
+                kraw[i] = vraw[i] = make_uint4(0, 0, 0, 0);
+                if (is && r < STEP) {
+                    kraw[i] = *reinterpret_cast<const uint4*>(kbase + (int64_t)o * 16 + 16 * piece);
+                    vraw[i] = *reinterpret_cast<const uint4*>(vbase + (int64_t)o * 16 + 16 * piece);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < POS; ++k) there[k] = there_next[k];
+        };
+        auto commit = [&](char* buf) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) {
+                const int id = i * kChunkThreads + tid, r = id / ACROSS, piece = id - r * ACROSS;
+                if (STEP * ACROSS % kChunkThreads != 0 && r >= STEP) continue;
+                const uint4 k = kraw[i], v = vraw[i];
+                if constexpr (E4M3) {
+                    *reinterpret_cast<uint4*>(buf + piece_at<S>(r, 2 * piece)) = make_uint4(to_bf16<false>(k.x), to_bf16<true>(k.x), to_bf16<false>(k.y), to_bf16<true>(k.y));
+                    *reinterpret_cast<uint4*>(buf + piece_at<S>(r, 2 * piece + 1)) = make_uint4(to_bf16<false>(k.z), to_bf16<true>(k.z), to_bf16<false>(k.w), to_bf16<true>(k.w));
+                    *reinterpret_cast<uint4*>(buf + S::TILE + piece_at<S>(r, 2 * piece)) = make_uint4(to_f16<false>(v.x), to_f16<true>(v.x), to_f16<false>(v.y), to_f16<true>(v.y));
+                    *reinterpret_cast<uint4*>(buf + S::TILE + piece_at<S>(r, 2 * piece + 1)) = make_uint4(to_f16<false>(v.z), to_f16<true>(v.z), to_f16<false>(v.w), to_f16<true>(v.w));
+                } else {
+                    *reinterpret_cast<uint4*>(buf + piece_at<S>(r, piece)) = k;
+                    *reinterpret_cast<uint4*>(buf + S::TILE + piece_at<S>(r, piece)) = v;
+                }
+            }
+        };
+
+        for (bool careful = false;; careful = true) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                m[r] = -__builtin_inff();
+                l[r] = 0.0f;
+#pragma unroll
+                for (int j = 0; j < S::VS; ++j) acc[r][j] = f32x16{};
+            }
+            uint64_t now[POS];
+            look(begin);
+            resolve();
+            look(begin + 1);
+            issue();
+            commit(smem);
+            for (int step = begin; step < end; ++step) {
+                char *buf = smem + ((step - begin) & 1) * 2 * S::TILE, *other = smem + ((step - begin + 1) & 1) * 2 * S::TILE;
+#pragma unroll
+                for (int k = 0; k < POS; ++k) now[k] = there[k];
+                resolve();                                    // of step + 1, asked for a step ago
+                __syncthreads();                              // this step's K and V are there, and nobody reads the other buffer any more
+                if (step + 1 < end) {
+                    issue();
+                    look(step + 2);
+                }
+                // ---- S = K Q^T of the wave's 32 * PB positions
+                const int v0 = step * STEP + wk * 32 * PB;        // the first of them, in the span's count
+                const char *kt = buf, *vt = buf + S::TILE;
+                f32x16 s[PB][RB];
+#pragma unroll
+                for (int b = 0; b < PB; ++b) {
+                    const int rowk = (wk * PB + b) * 32 + c;
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) s[b][r] = f32x16{};
+#pragma unroll
+                    for (int k = 0; k < S::KS; ++k) {
+                        const bf16x8 a = *reinterpret_cast<const bf16x8*>(kt + piece_at<S>(rowk, 2 * k + g));
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) s[b][r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[r][k], s[b][r], 0, 0, 0);
+                    }
+                }
+                // ---- what each row sees
+#pragma unroll
+                for (int b = 0; b < PB; ++b) {
+                    const int vb = v0 + 32 * b;
+                    const int in_step = (wk * PB + b) * 32;
+                    const unsigned is = (unsigned)(now[in_step / 64] >> (in_step & 63));
+                    const int first_pos = vb < span.sinks ? vb : vb - span.sinks + span.lo;
+                    const bool crosses = vb < span.sinks && vb + 32 > span.sinks;
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        const bool all = is == 0xFFFFFFFFu && !crosses && first_pos + 31 <= last[r] && (first_pos >= from[r] || first_pos + 31 < p.sinks);
+                        if (__all(all || !real[r])) continue;
+                        uint64_t bits = 0;                        // of the new tokens from position context + nth on
+                        const int nth = vb - span.sinks + span.lo - seq.context;
+                        if (p.seen && nth > -32) {
+                            const uint32_t* w = p.seen + (int64_t)token[r] * p.seen_stride;
+                            const int k = nth >> 5;
+                            const uint64_t lo = k >= 0 && k < p.words ? w[k] : 0, hi = k + 1 >= 0 && k + 1 < p.words ? w[k + 1] : 0;
+                            bits = (lo | hi << 32) >> (nth & 31);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int e = 8 * (i / 4) + 4 * g + i % 4, v = vb + e, pos = v < span.sinks ? v : v - span.sinks + span.lo;
+                            bool on = pos <= last[r] && (pos >= from[r] || pos < p.sinks);
+                            if (p.seen && pos >= seq.context) on = bits >> e & 1;
+                            if (!on || !(is >> e & 1)) s[b][r][i] = -__builtin_inff();
+                        }
+                    }
+                }
+                // ---- probabilities
+                Half pr[PB][RB][2];
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    float top = -__builtin_inff();
+#pragma unroll
+                    for (int b = 0; b < PB; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][r][i]);
+                    top = fmaxf(top, __shfl_xor(top, 32)) * to_log2;
+                    if (__any(top > m[r] + kSlack)) {
+                        const float m_new = fmaxf(m[r], top), f = m[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[r] - m_new);
+                        l[r] *= f;
+#pragma unroll
+                        for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) acc[r][j][i] *= f;
+                        m[r] = m_new;
+                    }
+                    const float ref = (m[r] == -__builtin_inff() ? 0.0f : m[r]) - kUp;
+#pragma unroll
+                    for (int b = 0; b < PB; ++b) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            s[b][r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r][i], to_log2, -ref));
+                            l[r] += s[b][r][i];
+                        }
+#pragma unroll
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) pr[b][r][t][i] = s[b][r][8 * t + i];
+                    }
+                }
+                // ---- O^T += V^T P^T
+                if (!careful) {
+                    const int q4 = lane >> 4, sub = (lane & 15) >> 2, quad = lane & 3;
+#pragma unroll
+                    for (int b = 0; b < PB; ++b)
+#pragma unroll
+                        for (int t = 0; t < 2; ++t) {
+                            const int r0 = (wk * PB + b) * 32 + 16 * t + 4 * g + sub;
+#pragma unroll
+                            for (int j = 0; j < S::VS; ++j) {
+                                const int piece = 4 * j + 2 * (q4 & 1) + (quad >> 1);
+                                union { s16x4 h[2]; Half v; } a;
+#pragma unroll
+                                for (int h = 0; h < 2; ++h)
+                                    a.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                        (__attribute__((address_space(3))) s16x4*)(vt + piece_at<S>(r0 + 8 * h, piece) + 8 * (quad & 1)));
+#pragma unroll
+                                for (int r = 0; r < RB; ++r) {
+                                    if constexpr (E4M3) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[b][r][t], acc[r][j], 0, 0, 0);
+                                    else acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[b][r][t], acc[r][j], 0, 0, 0);
+                                }
+                            }
+                        }
+                } else {
+#pragma unroll
+                    for (int b = 0; b < PB; ++b)
+#pragma unroll
+                        for (int r = 0; r < RB; ++r) {
+                            wave_lds_order();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) scratch[(8 * (i / 4) + 4 * g + i % 4) * 32 + c] = s[b][r][i];
+                            wave_lds_order();
+                            for (int e = 0; e < 32; ++e) {
+                                const float w = scratch[e * 32 + c];
+                                const int rowv = (wk * PB + b) * 32 + e;
+                                if (w == 0.0f) continue;
+#pragma unroll
+                                for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                                    for (int i4 = 0; i4 < 4; ++i4) {
+                                        const int col = 32 * j + 8 * i4 + 4 * g;
+                                        const uint2 raw = *reinterpret_cast<const uint2*>(vt + piece_at<S>(rowv, col >> 3) + 8 * g);
+                                        const unsigned u[2] = {raw.x, raw.y};
+#pragma unroll
+                                        for (int i = 0; i < 4; ++i) {
+                                            const unsigned short h = (unsigned short)(u[i / 2] >> 16 * (i & 1));
+                                            float val;
+                                            if constexpr (E4M3) val = (float)__builtin_bit_cast(_Float16, h);
+                                            else val = __uint_as_float((unsigned)h << 16);
+                                            acc[r][j][4 * i4 + i] = __builtin_fmaf(w, val, acc[r][j][4 * i4 + i]);
+                                        }
+                                    }
+                            }
+                        }
+                }
+                if (step + 1 < end) commit(other);
+            }
+            __syncthreads();                                  // all have read their last step
+            if (careful) break;
+            bool bad = false;
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+                if (real[r])
+#pragma unroll
+                    for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) bad = bad || !(fabsf(acc[r][j][i]) < __builtin_inff());
+            int* flags = reinterpret_cast<int*>(found);
+            const bool any = __any(bad);
+            if (lane == 0) flags[wave] = any ? 1 : 0;
+            __syncthreads();
+            bad = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+            __syncthreads();
+            if (!bad) break;
+        }
+
+        // ---------------- the end of the item, or of the share's part of it
+#pragma unroll
+        for (int r = 0; r < RB; ++r) l[r] += __shfl_xor(l[r], 32);
+        if constexpr (WK > 1) {
+            float* joined = reinterpret_cast<float*>(smem);   // [WK - 1][WM][32 RB][D + 4]: O, then m, l
+            auto slot = [&](int k, int r) { return joined + ((((k - 1) * WM + wm) * RB + r) * 32 + c) * (D + 4); };
+            if (wk > 0)
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    float* dst = slot(wk, r);
+#pragma unroll
+                    for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                        for (int i4 = 0; i4 < 4; ++i4)
+                            *reinterpret_cast<float4*>(dst + 32 * j + 8 * i4 + 4 * g) =
+                                make_float4(acc[r][j][4 * i4], acc[r][j][4 * i4 + 1], acc[r][j][4 * i4 + 2], acc[r][j][4 * i4 + 3]);
+                    if (g == 0) {
+                        dst[D] = m[r];
+                        dst[D + 1] = l[r];
+                    }
+                }
+            __syncthreads();
+            if (wk == 0)
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    float top = m[r];
+                    for (int k = 1; k < WK; ++k) top = fmaxf(top, slot(k, r)[D]);
+                    const float ref = top == -__builtin_inff() ? 0.0f : top;
+                    float f = __builtin_amdgcn_exp2f(m[r] - ref);
+                    l[r] *= f;
+#pragma unroll
+                    for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[r][j][i] *= f;
+                    for (int k = 1; k < WK; ++k) {
+                        const float* src = slot(k, r);
+                        f = __builtin_amdgcn_exp2f(src[D] - ref);
+                        l[r] += f * src[D + 1];
+#pragma unroll
+                        for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                            for (int i4 = 0; i4 < 4; ++i4) {
+                                const float4 v = *reinterpret_cast<const float4*>(src + 32 * j + 8 * i4 + 4 * g);
+                                acc[r][j][4 * i4] += f * v.x;
+                                acc[r][j][4 * i4 + 1] += f * v.y;
+                                acc[r][j][4 * i4 + 2] += f * v.z;
+                                acc[r][j][4 * i4 + 3] += f * v.w;
+                            }
+                    }
+                    m[r] = top;
+                }
+            __syncthreads();                                  // LDS is free for the next item
+        }
+        const bool begins = begin == 0, ends = end == steps;
+        if (!p.whole && begins && !ends && tid == 0)
+            p.cuts[blockIdx.x] = make_int4(at.b, at.tile, at.hk, (int)((at.at + steps - 1) / at.per - blockIdx.x) + 1);
+        if (wk == 0)
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                if (begins && ends) {
+                    if (!real[r]) continue;
+                    const float k = l[r] > 0.0f || l[r] != l[r] ? (E4M3 ? p.v_scale[at.hk] : 1.0f) / l[r] : 0.0f;
+                    bf16_t* dst = p.out + (int64_t)token[r] * p.out_stride + (int64_t)head[r] * D;
+#pragma unroll
+                    for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                        for (int i4 = 0; i4 < 4; ++i4)
+                            *reinterpret_cast<uint2*>(dst + 32 * j + 8 * i4 + 4 * g) =
+                                make_uint2(pack_bf16(acc[r][j][4 * i4] * k, acc[r][j][4 * i4 + 1] * k), pack_bf16(acc[r][j][4 * i4 + 2] * k, acc[r][j][4 * i4 + 3] * k));
+                    if (p.lse && g == 0) p.lse[(int64_t)token[r] * p.H + head[r]] = (m[r] - kUp + __log2f(l[r])) * 0.6931471805599453f;
+                } else {
+                    float* part = p.parts + (2 * (int64_t)blockIdx.x + (begins ? 1 : 0)) * S::PART;
+                    const int i = (wm * RB + r) * 32 + c;
+#pragma unroll
+                    for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                        for (int i4 = 0; i4 < 4; ++i4)
+                            *reinterpret_cast<float4*>(part + (int64_t)i * D + 32 * j + 8 * i4 + 4 * g) =
+                                make_float4(acc[r][j][4 * i4], acc[r][j][4 * i4 + 1], acc[r][j][4 * i4 + 2], acc[r][j][4 * i4 + 3]);
+                    if (g == 0) {
+                        part[S::ROWS * D + i] = m[r];
+                        part[S::ROWS * D + S::ROWS + i] = l[r];
+                    }
+                }
+            }
+        if (p.whole) return;
+        // ---------------- on to the next item of the share
+        at.at += end - begin;
+        if (at.at >= at.end) return;
+        at.step = 0;
+        if (++at.hk < p.Hk) continue;
+        at.hk = 0;
+        ++at.tile;
+        while (at.tile >= Seq(p, at.b).row_tiles(p, S::ROWS)) {       // ends: the share's steps belong to sequences that have some
+            at.tile = 0;
+            ++at.b;
+        }
+    }
+}
+
+// Joins the parts of the item that share x begins and does not end, a wave for each of its rows.
+template <int D>
+__global__ void __launch_bounds__(256) chunk_join(ChunkArgs p, int rows, float up)
+{
+    constexpr int LANES = D / 4;                          // lanes of a row of O, four columns each
+    const int4 cut = p.cuts[blockIdx.x];
+    const int n = cut.w, lane = threadIdx.x & 63, i = blockIdx.y * 4 + (threadIdx.x >> 6);
+    if (n == 0 || i >= rows) return;
+    const Seq seq(p, cut.x);
+    const int at = cut.y * rows + i;
+    if (at >= seq.n * p.group) return;
+    const int64_t size = (int64_t)rows * (D + 2);
+    auto part = [&](int k) { return p.parts + (2 * ((int64_t)blockIdx.x + k) + (k == 0 ? 1 : 0)) * size; };
+    float top = -__builtin_inff();
+    for (int k = lane; k < n; k += 64) top = fmaxf(top, part(k)[rows * D + i]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+    const float ref = top == -__builtin_inff() ? 0.0f : top;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.0f;
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+        const float* src = part(k);
+        const float f = __builtin_amdgcn_exp2f(src[rows * D + i] - ref);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (lane < LANES) v = *reinterpret_cast<const float4*>(src + (int64_t)i * D + 4 * lane);
+        o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+        sum += f * src[rows * D + rows + i];
+    }
+    const int j = at / p.group, head = cut.z * p.group + at - j * p.group, t = seq.t0 + j;
+    const float k = sum > 0.0f || sum != sum ? (p.v_scale ? p.v_scale[cut.z] : 1.0f) / sum : 0.0f;
+    if (lane < LANES)
+        *reinterpret_cast<uint2*>(p.out + (int64_t)t * p.out_stride + (int64_t)head * D + 4 * lane) = make_uint2(pack_bf16(o.x * k, o.y * k), pack_bf16(o.z * k, o.w * k));
+    if (p.lse && lane == 0) p.lse[(int64_t)t * p.H + head] = (top - up + __log2f(sum)) * 0.6931471805599453f;
+}
+
+// body(Shape): the shape that a call takes.
+template <int D, bool E4M3, typename F>
+auto pick(double rows, F&& body)
+{
+    if constexpr (D <= 128) {
+        if (rows <= 32) return body(Shape<D, E4M3, 1, 1, 4, 1>{});
+        if (rows <= 64) return body(Shape<D, E4M3, 1, 2, 2, 1>{});
+        if (rows <= 128) return body(Shape<D, E4M3, 1, 4, 1, 2>{});
+        return body(Shape<D, E4M3, 2, 4, 1, 2>{});
+    } else {
+        if (rows <= 64) return body(Shape<D, E4M3, 1, 2, 2, 1>{});
+        return body(Shape<D, E4M3, 1, 4, 1, 2>{});
+    }
+}
+template <typename F>
+auto pick(int D, bool e4m3, double rows, F&& body)
+{
+    auto of = [&](auto d) {
+        return e4m3 ? pick<decltype(d)::value, true>(rows, body) : pick<decltype(d)::value, false>(rows, body);
+    };
+    switch (D) {
+        case 64: return of(std::integral_constant<int, 64>{});
+        case 96: return of(std::integral_constant<int, 96>{});
+        case 128: return of(std::integral_constant<int, 128>{});
+        case 192: return of(std::integral_constant<int, 192>{});
+        default: return of(std::integral_constant<int, 256>{});
+    }
+}
+
+template <int D, bool E4M3>
+hipError_t init_of()
+{
+    hipError_t e = hipSuccess;
+    for (double rows : {32.0, 64.0, 128.0, 256.0}) {
+        e = pick<D, E4M3>(rows, [](auto s) {
+            using S = decltype(s);
+            return hipFuncSetAttribute(reinterpret_cast<const void*>(&chunk_kernel<S>), hipFuncAttributeMaxDynamicSharedMemorySize, S::LDS);
+        });
+        if (e != hipSuccess) return e;
+    }
+    return e;
+}
+
+}  // namespace
+
+hipError_t init_chunk_kernels()
+{
+    hipError_t e;
+    if ((e = init_of<64, false>()) != hipSuccess || (e = init_of<64, true>()) != hipSuccess || (e = init_of<96, false>()) != hipSuccess ||
+        (e = init_of<96, true>()) != hipSuccess || (e = init_of<128, false>()) != hipSuccess || (e = init_of<128, true>()) != hipSuccess ||
+        (e = init_of<192, false>()) != hipSuccess || (e = init_of<192, true>()) != hipSuccess || (e = init_of<256, false>()) != hipSuccess)
+        return e;
+    return init_of<256, true>();
+}
+
+// For every split of up to T tokens over up to n_seqs sequences: parts of the tallest tiles.
+size_t chunk_workspace_bytes(const moe_kv_cache& c, int n_seqs, int T, int n_heads)
+{
+    (void)n_seqs; (void)T; (void)n_heads;
+    const int rows = c.head_dim <= 128 ? 256 : 128;
+    return align_up(kChunkShares * sizeof(int4), 256) + align_up((size_t)2 * kChunkShares * rows * (c.head_dim + 2) * sizeof(float), 256);
+}
+
+hipError_t launch_chunk(const moe_kv_cache& c, const moe_block_table& t, const moe_chunk& ch, const bf16_t* q, int64_t q_stride, int n_heads, float scale,
+                        bf16_t* out, int64_t out_stride, float* lse, void* ws, hipStream_t s)
+{
+    const bool e4m3 = c.type == MOE_KV_E4M3;
+    const int size = e4m3 ? 1 : 2, per16 = 16 / size;
+    ChunkArgs p;
+    p.kc = static_cast<const char*>(c.k); p.vc = static_cast<const char*>(c.v);
+    p.head_stride = c.head_stride * size;
+    p.page_step = (unsigned)(c.page_stride / per16);
+    p.token_step = (unsigned)(c.token_stride / per16);
+    p.k_scale = e4m3 ? c.k_scale : nullptr; p.v_scale = e4m3 ? c.v_scale : nullptr;
+    p.pages = t.pages; p.row_of = t.token_row; p.row_stride = t.row_stride; p.n_rows = t.n_rows;
+    p.n_pages = c.n_pages; p.page_size = c.page_size;
+    // as in attention.hip: exact for every position below 2^31
+    int sh = 0;
+    while (((int64_t)1 << sh) < c.page_size) ++sh;
+    p.page_magic = (unsigned)((((uint64_t)1 << (31 + sh)) + c.page_size - 1) / c.page_size);
+    p.page_shift = 31 + sh;
+    p.cap = (int)std::min<int64_t>((int64_t)t.max_pages * c.page_size, 0x7FFFFFFF);
+    p.q = q; p.q_stride = q_stride;
+    p.first = ch.first; p.context = ch.context; p.positions = ch.seen ? ch.positions : nullptr;
+    p.seen = ch.seen; p.seen_stride = ch.seen_stride; p.words = ch.seen_words;
+    p.n_seqs = ch.n_seqs; p.T = ch.T; p.H = n_heads; p.Hk = c.n_kv_heads; p.group = n_heads / c.n_kv_heads;
+    p.window = ch.window; p.sinks = ch.window > 0 ? ch.sinks : 0;
+    p.scale = scale;
+    p.out = out; p.out_stride = out_stride; p.lse = lse;
+    p.cuts = static_cast<int4*>(ws);
+    p.parts = reinterpret_cast<float*>(static_cast<char*>(ws) + align_up(kChunkShares * sizeof(int4), 256));
+
+    const double rows = (double)ch.T * p.group / ch.n_seqs;       // of a sequence, on average
+    return pick(c.head_dim, e4m3, rows, [&](auto shape) {
+        using S = decltype(shape);
+        const int64_t slots = (int64_t)ch.T * p.group / S::ROWS + ch.n_seqs, items = slots * p.Hk;
+        p.whole = ch.n_seqs > 1024 || items >= 8 * 256 * S::RESIDENT;
+        if (p.whole) {
+            hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)items), dim3(kChunkThreads), S::LDS, s, p);
+            return hipGetLastError();
+        }
+        const int64_t most = items * (((int64_t)p.cap + S::STEP - 1) / S::STEP);
+        const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(most, 256 * S::RESIDENT));
+        hipLaunchKernelGGL((chunk_kernel<S>), dim3(grid), dim3(kChunkThreads), S::LDS, s, p);
+        hipError_t e = hipGetLastError();
+        if (e != hipSuccess || grid == 1) return e;
+        hipLaunchKernelGGL((chunk_join<S::D>), dim3(grid, S::ROWS / 4), dim3(256), 0, s, p, S::ROWS, S::E4M3 ? 11.0f : 0.0f);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace bmoe

@@ -78,12 +78,12 @@ hipError_t launch_quantize_weight(const bf16_t* w, int N, int K, uint8_t* w8, fl
 
 hipError_t launch_rope(const moe_kv_cache& c, const moe_block_table& t, const moe_rope& r, const bf16_t* q, int64_t q_stride,
                        const bf16_t* k, int64_t k_stride, const bf16_t* v, int64_t v_stride, int n_heads, int T,
-                       const int32_t* positions, bf16_t* q_out, int64_t q_out_stride, hipStream_t s);
+                       const int32_t* positions, const int32_t* places, bf16_t* q_out, int64_t q_out_stride, hipStream_t s);
 
 hipError_t init_attention_kernels();
 size_t attention_workspace_bytes(const moe_kv_cache& c, int T, int n_heads);
 hipError_t launch_attention(const moe_kv_cache& c, const moe_block_table& t, const bf16_t* q, int64_t q_stride, int n_heads, int T,
-                            const int32_t* lengths, float scale, int window, bf16_t* out, int64_t out_stride, float* lse, void* ws,
+                            const int32_t* lengths, float scale, int window, int sinks, bf16_t* out, int64_t out_stride, float* lse, void* ws,
                             hipStream_t s);
 
 hipError_t init_linear_kernels();

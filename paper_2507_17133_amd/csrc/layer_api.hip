@@ -1,5 +1,5 @@
 // C ABI of the operators around the MoE layer: argument checks, then the launch.
-#include "layer.h"
+#include "draft.h"
 
 #include <algorithm>
 #include <cmath>
@@ -9,6 +9,8 @@ namespace {
 
 constexpr int32_t kMaxColumns = 1 << 20;                         // with MOE_MAX_ROWS: tile counts and grids stay within what launches take
 constexpr int64_t kMaxRowBytes = (int64_t)1 << 23;               // a tile's offsets stay in 32 bits
+
+}  // namespace
 
 bool off(const void* p, unsigned bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
@@ -28,6 +30,8 @@ bool rows_meet(const void* a, int64_t a_stride, const void* b, int64_t b_stride,
     }
     return false;
 }
+
+namespace {
 
 moe_status check_norm(const moe_norm_args* a, bool norm)
 {
@@ -51,6 +55,8 @@ moe_status check_norm(const moe_norm_args* a, bool norm)
     if (a->y8 && a->scale_stride < a->T) return MOE_ERR_SHAPE;
     return MOE_OK;
 }
+
+}  // namespace
 
 moe_status check_cache(const moe_kv_cache* c)
 {
@@ -86,6 +92,8 @@ moe_status check_table(const moe_block_table* t, int32_t T)
     return MOE_OK;
 }
 
+namespace {
+
 moe_status check_linear(int32_t M, int32_t N, int32_t K)
 {
     if (M < 0) return MOE_ERR_INVALID_ARG;
@@ -95,6 +103,8 @@ moe_status check_linear(int32_t M, int32_t N, int32_t K)
 }
 
 bool attention_head_dim(int d) { return d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
+
+}  // namespace
 
 moe_status check_attention(const moe_kv_cache* c, int32_t n_heads, int32_t T)
 {
@@ -106,7 +116,54 @@ moe_status check_attention(const moe_kv_cache* c, int32_t n_heads, int32_t T)
     return MOE_OK;
 }
 
-}  // namespace
+moe_status attention_call(const moe_kv_cache* cache, const moe_block_table* table, const void* q, int64_t q_stride, int32_t n_heads, int32_t T,
+                          const int32_t* lengths, float scale, int32_t window, int32_t sinks, void* out, int64_t out_stride, float* lse, void* workspace,
+                          size_t workspace_bytes, void* stream, const char* name)
+{
+    moe_status st = check_attention(cache, n_heads, T);
+    if (st != MOE_OK) return st;
+    if (window < 0 || sinks < 0 || !std::isfinite(scale)) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;
+    if ((st = check_table(table, T)) != MOE_OK) return st;
+    if (!q || !lengths || !out) return MOE_ERR_INVALID_ARG;
+    if (off(q, 16) || off(lengths, 4) || off(out, 8) || off(lse, 4) || bad_stride(q_stride, 8) || bad_stride(out_stride, 4))
+        return MOE_ERR_ALIGNMENT;
+    if (T > 1 && out_stride < (int64_t)n_heads * cache->head_dim) return MOE_ERR_SHAPE;
+    if (!workspace || workspace_bytes < attention_workspace_bytes(*cache, T, n_heads)) return MOE_ERR_WORKSPACE;
+    if (off(workspace, 256)) return MOE_ERR_ALIGNMENT;
+    // blocks read a token's q where others have written its out
+    if (rows_meet(q, 2 * q_stride, out, 2 * out_stride, T, (int64_t)2 * n_heads * cache->head_dim)) return MOE_ERR_INVALID_ARG;
+    hipError_t e = ensure_device_init(nullptr);
+    if (e != hipSuccess) return hip_fail(e, name);
+    e = launch_attention(*cache, *table, static_cast<const bf16_t*>(q), q_stride, n_heads, T, lengths, scale, window, sinks,
+                         static_cast<bf16_t*>(out), out_stride, lse, workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOE_OK : hip_fail(e, name);
+}
+
+moe_status rope_call(const moe_kv_cache* cache, const moe_block_table* table, const moe_rope* rope, const void* q, int64_t q_stride, const void* k,
+                     int64_t k_stride, const void* v, int64_t v_stride, int32_t n_heads, int32_t T, const int32_t* positions, const int32_t* places,
+                     bool apart, void* q_out, int64_t q_out_stride, void* stream, const char* name)
+{
+    moe_status st = check_cache(cache);
+    if (st != MOE_OK) return st;
+    if (T < 0 || !rope) return MOE_ERR_INVALID_ARG;
+    const int D = cache->head_dim, R = rope->rotary_dim;
+    if (D % 16 != 0 || R < 0 || R > D || R % 16 != 0 || n_heads < 1) return MOE_ERR_SHAPE;
+    if (D > 256 || n_heads > MOE_MAX_HEADS || T > MOE_MAX_ROWS) return MOE_ERR_UNSUPPORTED;
+    if (R > 0 && !rope->turns) return MOE_ERR_INVALID_ARG;
+    if (T == 0) return MOE_OK;                            // an empty batch's table has no rows
+    if ((st = check_table(table, T)) != MOE_OK) return st;
+    if (!q || !k || !v || !positions || (apart && !places) || !q_out) return MOE_ERR_INVALID_ARG;
+    if (off(q, 16) || off(k, 16) || off(v, 16) || off(q_out, 16) || off(positions, 4) || off(places, 4) || off(rope->turns, 8) || bad_stride(q_stride, 8) ||
+        bad_stride(k_stride, 8) || bad_stride(v_stride, 8) || bad_stride(q_out_stride, 8))
+        return MOE_ERR_ALIGNMENT;
+    if (T > 1 && q_out_stride < (int64_t)n_heads * D) return MOE_ERR_SHAPE;
+    hipError_t e = launch_rope(*cache, *table, *rope, static_cast<const bf16_t*>(q), q_stride, static_cast<const bf16_t*>(k), k_stride,
+                               static_cast<const bf16_t*>(v), v_stride, n_heads, T, positions, places, static_cast<bf16_t*>(q_out), q_out_stride,
+                               static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? MOE_OK : hip_fail(e, name);
+}
+
 }  // namespace bmoe
 
 using namespace bmoe;
@@ -220,24 +277,8 @@ moe_status moe_rope_append(const moe_kv_cache* cache, const moe_block_table* tab
                            int32_t n_heads, int32_t T, const int32_t* positions, void* q_out, int64_t q_out_stride,
                            void* stream)
 {
-    moe_status st = check_cache(cache);
-    if (st != MOE_OK) return st;
-    if (T < 0 || !rope) return MOE_ERR_INVALID_ARG;
-    const int D = cache->head_dim, R = rope->rotary_dim;
-    if (D % 16 != 0 || R < 0 || R > D || R % 16 != 0 || n_heads < 1) return MOE_ERR_SHAPE;
-    if (D > 256 || n_heads > MOE_MAX_HEADS || T > MOE_MAX_ROWS) return MOE_ERR_UNSUPPORTED;
-    if (R > 0 && !rope->turns) return MOE_ERR_INVALID_ARG;
-    if (T == 0) return MOE_OK;                            // an empty batch's table has no rows
-    if ((st = check_table(table, T)) != MOE_OK) return st;
-    if (!q || !k || !v || !positions || !q_out) return MOE_ERR_INVALID_ARG;
-    if (off(q, 16) || off(k, 16) || off(v, 16) || off(q_out, 16) || off(positions, 4) || off(rope->turns, 8) || bad_stride(q_stride, 8) ||
-        bad_stride(k_stride, 8) || bad_stride(v_stride, 8) || bad_stride(q_out_stride, 8))
-        return MOE_ERR_ALIGNMENT;
-    if (T > 1 && q_out_stride < (int64_t)n_heads * D) return MOE_ERR_SHAPE;
-    hipError_t e = launch_rope(*cache, *table, *rope, static_cast<const bf16_t*>(q), q_stride, static_cast<const bf16_t*>(k), k_stride,
-                               static_cast<const bf16_t*>(v), v_stride, n_heads, T, positions, static_cast<bf16_t*>(q_out), q_out_stride,
-                               static_cast<hipStream_t>(stream));
-    return e == hipSuccess ? MOE_OK : hip_fail(e, "moe_rope_append");
+    return rope_call(cache, table, rope, q, q_stride, k, k_stride, v, v_stride, n_heads, T, positions, nullptr, false, q_out, q_out_stride, stream,
+                     "moe_rope_append");
 }
 
 moe_status moe_attention_workspace_size(const moe_kv_cache* cache, int32_t T_max, int32_t n_heads, size_t* bytes)
@@ -254,24 +295,8 @@ moe_status moe_paged_attention(const moe_kv_cache* cache, const moe_block_table*
                                int32_t n_heads, int32_t T, const int32_t* lengths, float scale, int32_t window, void* out,
                                int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream)
 {
-    moe_status st = check_attention(cache, n_heads, T);
-    if (st != MOE_OK) return st;
-    if (window < 0 || !std::isfinite(scale)) return MOE_ERR_INVALID_ARG;
-    if (T == 0) return MOE_OK;
-    if ((st = check_table(table, T)) != MOE_OK) return st;
-    if (!q || !lengths || !out) return MOE_ERR_INVALID_ARG;
-    if (off(q, 16) || off(lengths, 4) || off(out, 8) || off(lse, 4) || bad_stride(q_stride, 8) || bad_stride(out_stride, 4))
-        return MOE_ERR_ALIGNMENT;
-    if (T > 1 && out_stride < (int64_t)n_heads * cache->head_dim) return MOE_ERR_SHAPE;
-    if (!workspace || workspace_bytes < attention_workspace_bytes(*cache, T, n_heads)) return MOE_ERR_WORKSPACE;
-    if (off(workspace, 256)) return MOE_ERR_ALIGNMENT;
-    // blocks read a token's q where others have written its out
-    if (rows_meet(q, 2 * q_stride, out, 2 * out_stride, T, (int64_t)2 * n_heads * cache->head_dim)) return MOE_ERR_INVALID_ARG;
-    hipError_t e = ensure_device_init(nullptr);
-    if (e != hipSuccess) return hip_fail(e, "moe_paged_attention/init");
-    e = launch_attention(*cache, *table, static_cast<const bf16_t*>(q), q_stride, n_heads, T, lengths, scale, window,
-                         static_cast<bf16_t*>(out), out_stride, lse, workspace, static_cast<hipStream_t>(stream));
-    return e == hipSuccess ? MOE_OK : hip_fail(e, "moe_paged_attention");
+    return attention_call(cache, table, q, q_stride, n_heads, T, lengths, scale, window, 0, out, out_stride, lse, workspace, workspace_bytes, stream,
+                          "moe_paged_attention");
 }
 
 }  // extern "C"

@@ -1,0 +1,435 @@
+// What rows of logits say: log of the sum of exponentials, log probabilities and ranks of given tokens, entropy, the best alternatives.
+//
+//   m = max x,  S = sum e^(x - m),  U = sum e^(x - m) (x - m):      lse = m + log S,  log p_g = (x_g - m) - log S,  H = log S - U / S
+//   rank of g = #{x > x_g} + #{x = x_g, lower number};      the n_top first entries of the order (falling x, rising number)
+//
+// Both terms of H are at least 0, so nothing cancels.  A row is read once: a block takes a slice of it into registers, where the passes that follow
+// (maximum, sums, ranks, the best) find it; join_rows puts the slices of a row together by the same formulas.
+#include "draft.h"
+
+#include <algorithm>
+
+namespace bmoe {
+namespace {
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kEnough = 768;                      // blocks from which longer slices are taken: three for each CU
+constexpr int kCandidates = 512;                  // entries that a block sorts
+constexpr int kJoinMost = 32 * kThreads;          // entries that join_rows chooses from
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+struct LogprobArgs {
+    const char* logits;
+    int64_t stride;                               // in elements
+    const int32_t* tokens;
+    int64_t tokens_stride;
+    float* logprob;
+    int32_t* rank;
+    float *lse, *entropy;
+    int32_t* top_id;
+    float* top_logprob;
+    int T, V, G, N, slices;
+    float4* stats;                                // [T * slices]: m, S, U (U in powers of two)
+    int* before;                                  // [T * slices][G]
+    float2* best;                                 // [T * slices][N]: value, number (as bits)
+};
+
+// A value of the order (falling value, rising number).
+struct Entry {
+    float x;
+    int id;
+};
+__device__ __forceinline__ bool precedes(const Entry a, const Entry b) { return a.x > b.x || (a.x == b.x && a.id < b.id); }
+
+// Running sums about a maximum; joins as the exponentials do.
+struct Stats {
+    float m, s, u;
+    __device__ __forceinline__ void join(const Stats o)
+    {
+        const float top = fmaxf(m, o.m), ref = top == -__builtin_inff() ? 0.0f : top;
+        auto moved = [&](const Stats a, float& s2, float& u2) {
+            // e^(x - top) = e^(x - m) f; what has no finite maximum has no terms (or a NaN among them)
+            const float d = a.m == -__builtin_inff() ? 0.0f : (a.m - ref) * kLog2e, f = a.m == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(d);
+            s2 = f * a.s;
+            u2 = f == 0.0f ? f * a.u : f * (a.u + d * a.s);
+        };
+        float s1, u1, s2, u2;
+        moved(*this, s1, u1);
+        moved(o, s2, u2);
+        m = top;
+        s = s1 + s2;
+        u = u1 + u2;
+    }
+};
+
+// What is left to say about a row once its sums are known.
+struct Row {
+    float m, log_s, lse, entropy;
+    bool none;                                    // no distribution
+    __device__ __forceinline__ explicit Row(const Stats a) : m(a.m)
+    {
+        none = a.s != a.s;
+        log_s = __builtin_amdgcn_logf(a.s) * kLn2;
+        lse = none ? a.s : m == -__builtin_inff() ? m : m + log_s;
+        entropy = none ? a.s : m == -__builtin_inff() ? 0.0f : log_s - a.u * kLn2 / a.s;
+    }
+    __device__ __forceinline__ float of(float x) const { return none ? lse : x == -__builtin_inff() ? x : x - m - log_s; }
+};
+
+__device__ __forceinline__ float wave_max(float v)
+{
+#pragma unroll
+    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+    return v;
+}
+
+// Whole numbers in the order of floats.
+__device__ __forceinline__ unsigned order_of(float x)
+{
+    const unsigned b = __float_as_uint(x);
+    return b ^ ((unsigned)((int)b >> 31) | 0x80000000u);
+}
+__device__ __forceinline__ float of_order(unsigned u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
+
+// A bound that at least n of the wave's 64 values reach (n <= 64): the n-th largest one, cut off to the upper 16 bits of its order.
+__device__ __forceinline__ float nth_largest(float v, int n)
+{
+    const unsigned key = order_of(v) >> 16;
+    unsigned at = 0;
+#pragma unroll
+    for (int b = 15; b >= 0; --b) {
+        const unsigned higher = at | 1u << b;
+        if (__builtin_popcountll(__ballot(key >= higher)) >= n) at = higher;
+    }
+    return at < 0x0080u ? -__builtin_inff() : of_order(at << 16);
+}
+
+// LDS of the choice of a block's best entries.
+struct Choice {
+    float bound[kWaves];
+    int found;
+    Entry list[kCandidates];
+    Entry won[kWaves];
+};
+
+// The first n of the block's entries in order, to put(place, entry); a place that has none gets (-infinity, none).  `most`: the thread's largest value;
+// each(f): f(entry) for every entry of the thread.  Entries that reach the n-th largest of a wave's largest values hold the first n; where too many
+// do, as where all are alike, the entries are taken out one by one.
+template <typename Each, typename Put>
+__device__ __forceinline__ void choose(Choice& c, int n, float most, Each&& each, Put&& put)
+{
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const float mine = nth_largest(most, n);
+    if (lane == 0) c.bound[wave] = mine;
+    if (tid == 0) c.found = 0;
+    __syncthreads();
+    float bound = c.bound[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) bound = fmaxf(bound, c.bound[w]);
+    if (most >= bound)
+        each([&](const Entry e) {
+            if (e.x >= bound) {
+                const int at = atomicAdd(&c.found, 1);
+                if (at < kCandidates) c.list[at] = e;
+            }
+        });
+    __syncthreads();
+    const int found = c.found;
+    if (found <= kCandidates) {
+        for (int i = tid; i < max(found, n); i += kThreads) {
+            if (i >= found) {
+                put(i, Entry{-__builtin_inff(), 0x7FFFFFFF});
+                continue;
+            }
+            const Entry e = c.list[i];
+            int at = 0;
+            for (int j = 0; j < found; ++j) at += precedes(c.list[j], e) ? 1 : 0;
+            if (at < n) put(at, e);
+        }
+        return;
+    }
+    Entry last{__builtin_inff(), -1};
+    for (int i = 0; i < n; ++i) {
+        Entry top{-__builtin_inff(), 0x7FFFFFFF};
+        each([&](const Entry e) {
+            if (precedes(last, e) && precedes(e, top)) top = e;
+        });
+#pragma unroll
+        for (int o = 32; o; o >>= 1) {
+            const Entry e{__shfl_xor(top.x, o), __shfl_xor(top.id, o)};
+            if (precedes(e, top)) top = e;
+        }
+        if (lane == 0) c.won[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+            if (precedes(c.won[w], top)) top = c.won[w];
+        __syncthreads();
+        if (tid == 0) put(i, top);
+        last = top;
+    }
+}
+
+template <bool FP32>
+__device__ __forceinline__ float logit(const char* row, int i)
+{
+    if constexpr (FP32) return reinterpret_cast<const float*>(row)[i];
+    else return __uint_as_float((unsigned)reinterpret_cast<const uint16_t*>(row)[i] << 16);
+}
+
+// One slice of a row, EACH entries a thread.  HBM bounds it in large calls, beside the vector instructions (about 9 per entry, an exponential counts as 4, and one
+// more for each given token); the launches in small ones.
+template <bool FP32, int EACH>
+__global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
+{
+    constexpr int PER = FP32 ? 4 : 8, VECS = EACH / PER;          // entries of a 16-byte load
+    __shared__ Stats stats[kWaves];
+    __shared__ int counts[kWaves][MOE_MAX_GIVEN];
+    __shared__ Entry given[MOE_MAX_GIVEN];
+    __shared__ Choice choice;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int t = blockIdx.x / p.slices, slice = blockIdx.x - t * p.slices;
+    const char* row = p.logits + (int64_t)t * p.stride * (FP32 ? 4 : 2);
+    // slices begin on 16-byte lines, the first of them before the row where that begins inside one
+    const int begin = slice * EACH * kThreads - (int)((reinterpret_cast<uintptr_t>(row) & 15) / (FP32 ? 4 : 2));
+    float x[EACH];
+    uint4 raw[VECS];
+    bool whole[VECS];
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+        const int at = begin + (j * kThreads + tid) * PER;
+        whole[j] = at >= 0 && at + PER <= p.V;
+        if (whole[j]) raw[j] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + (int64_t)at * (FP32 ? 4 : 2))));
+    }
+    if (tid < p.G) {
+        const int id = p.tokens[(int64_t)t * p.tokens_stride + tid];
+        const bool real = (unsigned)id < (unsigned)p.V;
+        given[tid] = Entry{real ? logit<FP32>(row, id) : 0.0f, real ? id : -1};
+    }
+#pragma unroll
+    for (int j = 0; j < VECS; ++j) {
+        const int at = begin + (j * kThreads + tid) * PER;
+        if (whole[j]) {
+            if constexpr (FP32) {
+                x[4 * j] = __uint_as_float(raw[j].x); x[4 * j + 1] = __uint_as_float(raw[j].y);
+                x[4 * j + 2] = __uint_as_float(raw[j].z); x[4 * j + 3] = __uint_as_float(raw[j].w);
+            } else unpack_bf16(raw[j], x + 8 * j);
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) x[PER * j + e] = (unsigned)(at + e) < (unsigned)p.V ? logit<FP32>(row, at + e) : -__builtin_inff();
+        }
+    }
+    float most = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) most = fmaxf(most, x[i]);
+    Stats a;
+    a.m = wave_max(most);
+    const float ref = a.m == -__builtin_inff() ? 0.0f : a.m;
+    a.s = a.u = 0.0f;
+    // x log2 e - c in one instruction, c the rounded m log2 e.  All terms are off by the same factor 2^-g then, which is known.
+    const float c = ref * kLog2e, g = -__builtin_fmaf(ref, kLog2e, -c);
+    const bool small = fabsf(ref) <= 1048576.0f;
+    if (small) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const float d = __builtin_fmaf(x[i], kLog2e, -c), e = __builtin_amdgcn_exp2f(d);
+            a.s += e;
+            a.u = __builtin_fmaf(e, d, a.u);
+        }
+        const float f = __builtin_amdgcn_exp2f(g);
+        a.u = f * __builtin_fmaf(g, a.s, a.u);
+        a.s *= f;
+    }
+    if (!small || __any(a.u != a.u)) {            // large values, or -infinities (0 times one is NaN)
+        a.s = a.u = 0.0f;
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const float d = x[i] - ref, e = __builtin_amdgcn_exp2f(d * kLog2e);
+            a.s += e;
+            a.u = __builtin_fmaf(e, fmaxf(d, -1000.0f) * kLog2e, a.u);
+        }
+    }
+#pragma unroll
+    for (int o = 32; o; o >>= 1) {
+        a.s += __shfl_xor(a.s, o);
+        a.u += __shfl_xor(a.u, o);
+    }
+    if (lane == 0) stats[wave] = a;
+    __syncthreads();                              // given tokens, sums
+    for (int k = 0; k < p.G; ++k) {
+        const Entry e = given[k];
+        // at least x_g before its number, above it behind: above the value below x_g, or above x_g
+        const unsigned b = __float_as_uint(e.x + 0.0f);
+        const float below = b == 0 ? -1.401298464324817e-45f : __uint_as_float((int)b < 0 ? b + 1 : b - 1);
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < VECS; ++j) {
+            const int at = begin + (j * kThreads + tid) * PER;
+            const bool ahead = at + PER <= e.id, odd = !whole[j] || (!ahead && at <= e.id) || e.x == -__builtin_inff();
+            const float bound = ahead ? below : e.x;
+            if (__any(odd)) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    n += __builtin_popcountll(__ballot((unsigned)(at + i) < (unsigned)p.V && precedes(Entry{x[PER * j + i], at + i}, e)));
+            } else {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) n += __builtin_popcountll(__ballot(x[PER * j + i] > bound));
+            }
+        }
+        if (lane == 0) counts[wave][k] = n;
+    }
+    auto each = [&](auto&& f) {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int id = begin + (i / PER * kThreads + tid) * PER + i % PER;
+            if ((unsigned)id < (unsigned)p.V) f(Entry{x[i], id});
+        }
+    };
+    a = stats[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) a.join(stats[w]);
+    if (p.slices > 1) {
+        if (tid == 0) p.stats[blockIdx.x] = make_float4(a.m, a.s, a.u, 0.0f);
+        if (p.N) choose(choice, p.N, most, each, [&](int i, const Entry e) { p.best[(int64_t)blockIdx.x * p.N + i] = make_float2(e.x, __int_as_float(e.id)); });
+        if (p.G) __syncthreads();
+        if (tid < p.G) p.before[(int64_t)blockIdx.x * p.G + tid] = counts[0][tid] + counts[1][tid] + counts[2][tid] + counts[3][tid];
+        return;
+    }
+    const Row r(a);
+    if (tid == 0) {
+        if (p.lse) p.lse[t] = r.lse;
+        if (p.entropy) p.entropy[t] = r.entropy;
+    }
+    if (p.N)
+        choose(choice, p.N, most, each, [&](int i, const Entry e) {
+            if (p.top_id) p.top_id[(int64_t)t * p.N + i] = r.none ? -1 : e.id;
+            if (p.top_logprob) p.top_logprob[(int64_t)t * p.N + i] = r.of(e.x);
+        });
+    if (p.G) __syncthreads();
+    if (tid < p.G) {
+        const Entry e = given[tid];
+        if (p.logprob) p.logprob[(int64_t)t * p.G + tid] = e.id < 0 ? 0.0f : r.of(e.x);
+        if (p.rank) p.rank[(int64_t)t * p.G + tid] = e.id < 0 || r.none ? -1 : counts[0][tid] + counts[1][tid] + counts[2][tid] + counts[3][tid];
+    }
+}
+
+// A block for each row whose slices are joined; EACH of their best entries a thread.
+template <bool FP32, int EACH>
+__global__ void __launch_bounds__(kThreads) join_rows(LogprobArgs p)
+{
+    __shared__ Stats stats[kWaves];
+    __shared__ Choice choice;
+    const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t first = (int64_t)t * p.slices;
+    Entry entry[EACH];
+    float most = -__builtin_inff();
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int at = i * kThreads + tid;
+        entry[i] = Entry{-__builtin_inff(), 0x7FFFFFFF};
+        if (at < p.slices * p.N) {
+            const float2 v = p.best[first * p.N + at];
+            entry[i] = Entry{v.x, __float_as_int(v.y)};
+        }
+        most = fmaxf(most, entry[i].x);
+    }
+    Stats a{-__builtin_inff(), 0.0f, 0.0f};
+    for (int i = tid; i < p.slices; i += kThreads) {
+        const float4 v = p.stats[first + i];
+        a.join(Stats{v.x, v.y, v.z});
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        Stats b{__shfl_xor(a.m, o), __shfl_xor(a.s, o), __shfl_xor(a.u, o)};
+        a.join(b);
+    }
+    if (lane == 0) stats[wave] = a;
+    __syncthreads();
+    a = stats[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) a.join(stats[w]);
+    const Row r(a);
+    if (tid == 0) {
+        if (p.lse) p.lse[t] = r.lse;
+        if (p.entropy) p.entropy[t] = r.entropy;
+    }
+    if (tid < p.G) {
+        const int id = p.tokens[(int64_t)t * p.tokens_stride + tid];
+        const bool real = (unsigned)id < (unsigned)p.V;
+        const char* row = p.logits + (int64_t)t * p.stride * (FP32 ? 4 : 2);
+        if (p.logprob) p.logprob[(int64_t)t * p.G + tid] = real ? r.of(logit<FP32>(row, id)) : 0.0f;
+        if (p.rank) {
+            int n = 0;
+            for (int i = 0; i < p.slices; ++i) n += p.before[(first + i) * p.G + tid];
+            p.rank[(int64_t)t * p.G + tid] = real && !r.none ? n : -1;
+        }
+    }
+    if (p.N)
+        choose(choice, p.N, most,
+               [&](auto&& f) {
+#pragma unroll
+                   for (int i = 0; i < EACH; ++i)
+                       if (entry[i].id != 0x7FFFFFFF) f(entry[i]);
+               },
+               [&](int i, const Entry e) {
+                   if (p.top_id) p.top_id[(int64_t)t * p.N + i] = r.none ? -1 : e.id;
+                   if (p.top_logprob) p.top_logprob[(int64_t)t * p.N + i] = r.of(e.x);
+               });
+}
+
+int slices_of(int V, int each) { return ceil_div(V + 7, each * kThreads); }      // up to 7 places before the row
+
+// Entries of a thread: the longest slices that still make enough blocks, or the shortest ones.
+int entries_each(int64_t T, int V, int n_top)
+{
+    int each = 64;
+    while (each > 8 && T * slices_of(V, each) < kEnough && (int64_t)slices_of(V, each / 2) * n_top <= kJoinMost) each /= 2;
+    return each;
+}
+
+template <bool FP32>
+hipError_t go(const LogprobArgs& p, int each, hipStream_t s)
+{
+    const dim3 grid((unsigned)(p.T * p.slices)), threads(kThreads);
+    switch (each) {
+        case 8: hipLaunchKernelGGL((slice_kernel<FP32, 8>), grid, threads, 0, s, p); break;
+        case 16: hipLaunchKernelGGL((slice_kernel<FP32, 16>), grid, threads, 0, s, p); break;
+        case 32: hipLaunchKernelGGL((slice_kernel<FP32, 32>), grid, threads, 0, s, p); break;
+        default: hipLaunchKernelGGL((slice_kernel<FP32, 64>), grid, threads, 0, s, p); break;
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.slices == 1) return e;
+    if (p.slices * p.N <= 4 * kThreads) hipLaunchKernelGGL((join_rows<FP32, 4>), dim3(p.T), threads, 0, s, p);
+    else hipLaunchKernelGGL((join_rows<FP32, 32>), dim3(p.T), threads, 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t logprob_workspace_bytes(int64_t T, int V, int n_given, int n_top)
+{
+    // fewer rows may be cut into shorter slices, but then into fewer than twice kEnough of them
+    const int64_t parts = std::max(T * slices_of(V, 64), std::min<int64_t>(T * slices_of(V, 8), 2 * kEnough));
+    return align_up(parts * sizeof(float4), 256) + align_up(parts * sizeof(int) * n_given, 256) + align_up(parts * sizeof(float2) * n_top, 256);
+}
+
+hipError_t launch_logprobs(const moe_logprob_args& a, void* ws, hipStream_t s)
+{
+    LogprobArgs p;
+    p.logits = static_cast<const char*>(a.logits); p.stride = a.stride;
+    p.tokens = a.tokens; p.tokens_stride = a.tokens_stride;
+    p.logprob = a.logprob; p.rank = a.rank; p.lse = a.lse; p.entropy = a.entropy;
+    p.top_id = a.top_id; p.top_logprob = a.top_logprob;
+    p.T = a.T; p.V = a.V;
+    p.G = a.logprob || a.rank ? a.n_given : 0;
+    p.N = a.top_id || a.top_logprob ? a.n_top : 0;
+    const int each = entries_each(a.T, a.V, p.N);
+    p.slices = slices_of(a.V, each);
+    const size_t parts = (size_t)p.T * p.slices;
+    p.stats = static_cast<float4*>(ws);
+    p.before = reinterpret_cast<int*>(static_cast<char*>(ws) + align_up(parts * sizeof(float4), 256));
+    p.best = reinterpret_cast<float2*>(reinterpret_cast<char*>(p.before) + align_up(parts * sizeof(int) * p.G, 256));
+    return a.type == MOE_LOGITS_FP32 ? go<true>(p, each, s) : go<false>(p, each, s);
+}
+
+}  // namespace bmoe

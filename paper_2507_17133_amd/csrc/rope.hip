@@ -15,7 +15,7 @@ struct RopeArgs {
     const bf16_t *q, *k, *v;
     bf16_t* qo;
     int64_t qs, ks, vs, qos;
-    const int32_t* positions;
+    const int32_t *positions, *places;                    // places NULL: the positions
     const int32_t *pages, *token_row;
     int64_t row_stride;
     int n_rows, max_pages;
@@ -29,7 +29,7 @@ struct RopeArgs {
     int H, Hk, D, T;
 };
 
-// Where the token's k and v go, in elements from the cache's base; negative: nowhere.
+// Where k and v of a token that goes to position pos are, in elements from the cache's base; negative: nowhere.
 __device__ __forceinline__ int64_t cache_place(const RopeArgs& p, int t, int pos)
 {
     const int row = p.token_row ? p.token_row[t] : t, page_at = pos / p.page_size;
@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(512) rope_kernel(RopeArgs p)
         cs[i] = c * p.factor;
         sn[i] = s * p.factor;
     }
-    const int64_t place = cache_place(p, t, pos);
+    const int64_t place = pos < 0 ? -1 : cache_place(p, t, p.places ? p.places[t] : pos);
     __syncthreads();
     const int per_head = p.D >> 4, units = (p.H + 2 * p.Hk) * per_head, rot = p.R >> 4;
     for (int u = threadIdx.x; u < units; u += blockDim.x) {
@@ -127,12 +127,12 @@ __global__ void __launch_bounds__(512) rope_kernel(RopeArgs p)
 
 hipError_t launch_rope(const moe_kv_cache& c, const moe_block_table& t, const moe_rope& r, const bf16_t* q, int64_t q_stride,
                        const bf16_t* k, int64_t k_stride, const bf16_t* v, int64_t v_stride, int n_heads, int T,
-                       const int32_t* positions, bf16_t* q_out, int64_t q_out_stride, hipStream_t s)
+                       const int32_t* positions, const int32_t* places, bf16_t* q_out, int64_t q_out_stride, hipStream_t s)
 {
     RopeArgs p;
     p.q = q; p.k = k; p.v = v; p.qo = q_out;
     p.qs = q_stride; p.ks = k_stride; p.vs = v_stride; p.qos = q_out_stride;
-    p.positions = positions;
+    p.positions = positions; p.places = places;
     p.pages = t.pages; p.token_row = t.token_row; p.row_stride = t.row_stride; p.n_rows = t.n_rows; p.max_pages = t.max_pages;
     p.turns = r.turns; p.factor = r.factor; p.R = r.rotary_dim; p.interleaved = r.interleaved;
     p.kc = static_cast<uint8_t*>(c.k); p.vc = static_cast<uint8_t*>(c.v);
