@@ -43,9 +43,9 @@ struct Shape {
     static constexpr int N64 = D / 64, N32 = D % 64 / 32;                     // panels of 64 columns, and one of 32
     static constexpr int TILE = STEP * D * 2;                                 // bytes of K (of V) of a step in LDS
     static constexpr int KS = D / 16, VS = D / 32;                            // products along D, blocks of 32 columns of V
-    static constexpr int SCRATCH = kChunkWaves * 32 * 32 * 4;                 // probabilities of the careful second product
-    static constexpr int JOIN = WK > 1 ? (WK - 1) * WM * 32 * RB * (D + 4) * 4 : 0;
-    static constexpr int LDS = (4 * TILE > JOIN ? 4 * TILE : JOIN) + SCRATCH;
+    static constexpr int LEAD = 2 / PB;                                       // steps that K is ahead of V
+    static constexpr int LDS = 4 * TILE;                                      // two steps of K, two of V
+    static_assert(PB <= 2 && kChunkWaves * 32 * 32 * 4 <= 2 * TILE && (WK - 1) * WM * 32 * RB * (D + 4) * 4 <= LDS, "what else LDS holds");
     static constexpr int RESIDENT = LDS <= 80 * 1024 && RB * D <= 128 ? 2 : 1;   // blocks of a CU
     // floats of a part: [ROWS][D] O, [ROWS] m, [ROWS] l
     static constexpr int64_t PART = (int64_t)ROWS * (D + 2);
@@ -230,6 +230,9 @@ __device__ __forceinline__ int piece_at(int row, int piece)
     return S::N64 * S::STEP * 128 + row * 64 + (((piece & 3) ^ (row >> 1 & 3)) << 4);
 }
 
+// The n lowest bits (none for n <= 0, all from 32 on).
+__device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; }
+
 template <class S>
 __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(ChunkArgs p)
 {
@@ -241,8 +244,8 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, g = lane >> 5, wm = wave % WM, wk = wave / WM;
-    int64_t* found = reinterpret_cast<int64_t*>(smem + S::LDS - S::SCRATCH);      // at the kernel's start; flags of the waves later
-    float* scratch = reinterpret_cast<float*>(smem + S::LDS - S::SCRATCH) + wave * 32 * 32;
+    char *const kbuf = smem, *const vbuf = smem + 2 * S::TILE;
+    int64_t* found = reinterpret_cast<int64_t*>(smem);    // while no step is there
 
     Begin at;
     if (p.whole) {
@@ -279,7 +282,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             int pos = seq.context + j;
             if (p.positions) pos = max(seq.context, p.positions[token[r]]);
             last[r] = p.seen ? seq.context - 1 : pos;
-            from[r] = p.window > 0 ? pos - p.window + 1 : 0;                  // may be negative
+            from[r] = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
             const bf16_t* src = p.q + (int64_t)token[r] * p.q_stride + (int64_t)head[r] * D;
 #pragma unroll
             for (int k = 0; k < S::KS; ++k) {
@@ -290,80 +293,207 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             }
         }
 
+        // LDS offsets of a lane: its K row's pieces of a panel, and its V rows' pieces of even and odd blocks of 32 columns
+        int kat[4], kat32[2], vat[2], vat32;
+        {
+            const int sub = 4 * g + ((lane & 15) >> 2), piece = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), in = 8 * (lane & 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) kat[k] = (wk * PB * 32 + c) * 128 + (((2 * k + g) ^ (c & 7)) << 4);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                kat32[k] = S::N64 * STEP * 128 + (wk * PB * 32 + c) * 64 + (((2 * k + g) ^ (c >> 1 & 3)) << 4);
+                vat[k] = (wk * PB * 32 + sub) * 128 + (((4 * k + piece) ^ sub) << 4) + in;
+            }
+            vat32 = S::N64 * STEP * 128 + (wk * PB * 32 + sub) * 64 + ((piece ^ (sub >> 1 & 3)) << 4) + in;
+        }
+
         f32x16 acc[RB][S::VS];
         float m[RB], l[RB];
 
-        // ---------------- where a step's positions are: lane i has those of positions i, 64 + i, ...
-        unsigned off[POS];
-        uint64_t there[POS], there_next[POS];
-        int page[POS];
-        unsigned in_page[POS];
+        // ---------------- where a step's positions are: lane i has those of positions i, 64 + i, ...  Places behind the last position are read from that one.
+        struct Look {
+            int page[POS];
+            unsigned in_page[POS];
+            uint64_t counts[POS];
+        };
+        struct Where {
+            unsigned off[POS];                            // in 16-byte steps
+            uint64_t there[POS];
+        };
+        const int most = (int)min((int64_t)span.n, (int64_t)end * STEP);      // positions behind these are another share's, or nobody's
         auto look = [&](int step) {
+            Look o;
 #pragma unroll
             for (int k = 0; k < POS; ++k) {
-                const int v = step * STEP + 64 * k + lane;
-                page[k] = -1;
-                in_page[k] = 0;
-                if (step < end && v < span.n) {
-                    const unsigned pos = v < span.sinks ? v : v - span.sinks + span.lo;
+                const int v = step * STEP + 64 * k + lane, in = min(v, most - 1);
+                o.counts[k] = __ballot(v < most);
+                o.page[k] = -1;
+                o.in_page[k] = 0;
+                if (most > 0) {
+                    const unsigned pos = in < span.sinks ? in : in - span.sinks + span.lo;
                     const unsigned pg = (unsigned)((uint64_t)pos * p.page_magic >> p.page_shift);
-                    in_page[k] = pos - pg * (unsigned)p.page_size;
-                    page[k] = pages[pg];
+                    o.in_page[k] = pos - pg * (unsigned)p.page_size;
+                    o.page[k] = pages[pg];
                 }
             }
+            return o;
         };
-        auto resolve = [&]() {
+        auto resolve = [&](const Look& o) {
+            Where w;
 #pragma unroll
             for (int k = 0; k < POS; ++k) {
-                const bool is = (unsigned)page[k] < (unsigned)p.n_pages;
-                off[k] = is ? (unsigned)page[k] * p.page_step + in_page[k] * p.token_step : 0;
-                there_next[k] = __ballot(is);
+                const bool is = (unsigned)o.page[k] < (unsigned)p.n_pages;
+                w.off[k] = is ? (unsigned)o.page[k] * p.page_step + o.in_page[k] * p.token_step : 0;
+                w.there[k] = __ballot(is) & o.counts[k];
             }
+            return w;
         };
-        // ---------------- a step's K and V, to registers and from there to LDS
+        // ---------------- K or V of a step, to registers and from there to LDS
         constexpr int ACROSS = E4M3 ? D / 16 : D / 8;                         // 16-byte pieces of a row in the cache
         constexpr int PIECES = (STEP * ACROSS + kChunkThreads - 1) / kChunkThreads;
-        uint4 kraw[PIECES], vraw[PIECES];
-        auto issue = [&]() {
+        struct Raw {
+            uint4 w[PIECES];
+        };
+        auto fetch = [&](const char* base, const unsigned (&off)[POS], Raw& raw) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int id = i * kChunkThreads + tid, r = id / ACROSS, piece = id - r * ACROSS;
                 unsigned o = __shfl(off[0], r & 63);
-                bool is = there_next[0] >> (r & 63) & 1;
                 if constexpr (POS > 1) {
                     const unsigned o1 = __shfl(off[POS - 1], r & 63);
-                    const bool is1 = there_next[POS - 1] >> (r & 63) & 1;
                     o = r < 64 ? o : o1;
-                    is = r < 64 ? is : is1;
                 }
-                kraw[i] = vraw[i] = make_uint4(0, 0, 0, 0);
-                if (is && r < STEP) {
-                    kraw[i] = *reinterpret_cast<const uint4*>(kbase + (int64_t)o * 16 + 16 * piece);
-                    vraw[i] = *reinterpret_cast<const uint4*>(vbase + (int64_t)o * 16 + 16 * piece);
-                }
+                raw.w[i] = *reinterpret_cast<const uint4*>(base + 16 * piece + (uint64_t)o * 16);
             }
-#pragma unroll
-            for (int k = 0; k < POS; ++k) there[k] = there_next[k];
         };
-        auto commit = [&](char* buf) {
+        auto store = [&](char* tile, const Raw& raw, auto is_v) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int id = i * kChunkThreads + tid, r = id / ACROSS, piece = id - r * ACROSS;
                 if (STEP * ACROSS % kChunkThreads != 0 && r >= STEP) continue;
-                const uint4 k = kraw[i], v = vraw[i];
-                if constexpr (E4M3) {
-                    *reinterpret_cast<uint4*>(buf + piece_at<S>(r, 2 * piece)) = make_uint4(to_bf16<false>(k.x), to_bf16<true>(k.x), to_bf16<false>(k.y), to_bf16<true>(k.y));
-                    *reinterpret_cast<uint4*>(buf + piece_at<S>(r, 2 * piece + 1)) = make_uint4(to_bf16<false>(k.z), to_bf16<true>(k.z), to_bf16<false>(k.w), to_bf16<true>(k.w));
-                    *reinterpret_cast<uint4*>(buf + S::TILE + piece_at<S>(r, 2 * piece)) = make_uint4(to_f16<false>(v.x), to_f16<true>(v.x), to_f16<false>(v.y), to_f16<true>(v.y));
-                    *reinterpret_cast<uint4*>(buf + S::TILE + piece_at<S>(r, 2 * piece + 1)) = make_uint4(to_f16<false>(v.z), to_f16<true>(v.z), to_f16<false>(v.w), to_f16<true>(v.w));
+                const uint4 w = raw.w[i];
+                if constexpr (!E4M3) *reinterpret_cast<uint4*>(tile + piece_at<S>(r, piece)) = w;
+                else if constexpr (decltype(is_v)::value) {
+                    *reinterpret_cast<uint4*>(tile + piece_at<S>(r, 2 * piece)) = make_uint4(to_f16<false>(w.x), to_f16<true>(w.x), to_f16<false>(w.y), to_f16<true>(w.y));
+                    *reinterpret_cast<uint4*>(tile + piece_at<S>(r, 2 * piece + 1)) = make_uint4(to_f16<false>(w.z), to_f16<true>(w.z), to_f16<false>(w.w), to_f16<true>(w.w));
                 } else {
-                    *reinterpret_cast<uint4*>(buf + piece_at<S>(r, piece)) = k;
-                    *reinterpret_cast<uint4*>(buf + S::TILE + piece_at<S>(r, piece)) = v;
+                    *reinterpret_cast<uint4*>(tile + piece_at<S>(r, 2 * piece)) = make_uint4(to_bf16<false>(w.x), to_bf16<true>(w.x), to_bf16<false>(w.y), to_bf16<true>(w.y));
+                    *reinterpret_cast<uint4*>(tile + piece_at<S>(r, 2 * piece + 1)) = make_uint4(to_bf16<false>(w.z), to_bf16<true>(w.z), to_bf16<false>(w.w), to_bf16<true>(w.w));
                 }
             }
         };
-
-        for (bool careful = false;; careful = true) {
+        constexpr std::false_type of_k{};
+        constexpr std::true_type of_v{};
+        // ---------------- S of the wave's block b of a step
+        auto scores = [&](const char* kt, int b, f32x16 (&s)[RB]) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r) s[r] = f32x16{};
+#pragma unroll
+            for (int k = 0; k < S::KS; ++k) {
+                const bf16x8 a = *reinterpret_cast<const bf16x8*>(
+                    kt + (k < 4 * S::N64 ? kat[k & 3] + (k >> 2) * STEP * 128 + b * 32 * 128 : kat32[k & 1] + b * 32 * 64));
+#pragma unroll
+                for (int r = 0; r < RB; ++r) s[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[r][k], s[r], 0, 0, 0);
+            }
+        };
+        // ---------------- what each row sees of it: a bit for each of the 32 positions
+        auto cover = [&](int step, int b, const uint64_t (&there)[POS], f32x16 (&s)[RB]) {
+            const int in_step = (wk * PB + b) * 32, vb = step * STEP + in_step;
+            const uint64_t word = POS > 1 && in_step >= 64 ? there[POS - 1] : there[0];
+            const unsigned is = (unsigned)(word >> (in_step & 63));
+            // the first k of them are among the sinks, at positions vb on; the others at positions at on
+            const int k = min(max(span.sinks - vb, 0), 32), at = vb - span.sinks + span.lo;
+            bool all = is == 0xFFFFFFFFu && k == 0;
+#pragma unroll
+            for (int r = 0; r < RB; ++r) all = all && (!real[r] || (at + 31 <= last[r] && at >= from[r]));
+            if (__all(all)) return;
+            const unsigned sink = below(k);
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                unsigned on = below(last[r] - at + 1) & (~below(from[r] - at) | below(p.sinks - at));
+                const int nth = at - seq.context;         // of the new tokens, the one at position `at`
+                if (p.seen && nth > -32) {
+                    const uint32_t* w = p.seen + (int64_t)token[r] * p.seen_stride;
+                    const int i = nth >> 5;
+                    const uint64_t lo = i >= 0 && i < p.words ? w[i] : 0, hi = i + 1 < p.words ? w[i + 1] : 0;
+                    on |= (unsigned)((lo | hi << 32) >> (nth & 31)) & ~below(-nth);
+                }
+                on = ((sink & below(last[r] - vb + 1)) | (~sink & on)) & is;
+                on >>= 4 * g;
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (!(on >> (8 * (i / 4) + i % 4) & 1)) s[r][i] = -__builtin_inff();
+            }
+        };
+        // ---------------- probabilities in place of scores; f: what earlier sums are to be multiplied by.  Returns whether any of them are.
+        auto exponents = [&](f32x16 (&s)[RB], float (&f)[RB]) {
+            float top[RB];
+            bool moves = false;
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                top[r] = -__builtin_inff();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top[r] = fmaxf(top[r], s[r][i]);
+                const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[r]), __float_as_uint(top[r]), false, false);
+                top[r] = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * to_log2;
+                moves = moves || top[r] > m[r] + kSlack;
+            }
+            moves = __any(moves);
+            if (moves)
+#pragma unroll
+                for (int r = 0; r < RB; ++r) {
+                    const float m_new = fmaxf(m[r], top[r]);
+                    f[r] = m[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[r] - m_new);
+                    l[r] *= f[r];
+                    m[r] = m_new;
+                }
+#pragma unroll
+            for (int r = 0; r < RB; ++r) {
+                const float ref = (m[r] == -__builtin_inff() ? 0.0f : m[r]) - kUp;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i], to_log2, -ref));
+                    l[r] += s[r][i];
+                }
+            }
+            return moves;
+        };
+        auto rescale = [&](const float (&f)[RB]) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[r][j][i] *= f[r];
+        };
+        auto rounded = [&](const f32x16 (&s)[RB], Half (&pr)[RB][2]) {
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pr[r][t][i] = s[r][8 * t + i];
+        };
+        // ---------------- O^T += V^T P^T
+        auto weigh = [&](const char* vt, int b, const Half (&pr)[RB][2]) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int j = 0; j < S::VS; ++j) {
+                    union { s16x4 h[2]; Half v; } a;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        a.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (__attribute__((address_space(3))) s16x4*)(vt + (j < 2 * S::N64 ? vat[j & 1] + (j >> 1) * STEP * 128 + (32 * b + 16 * t + 8 * h) * 128
+                                                                                             : vat32 + (32 * b + 16 * t + 8 * h) * 64)));
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        if constexpr (E4M3) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
+                        else acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
+                    }
+                }
+        };
+        auto clear = [&]() {
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 m[r] = -__builtin_inff();
@@ -371,174 +501,158 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
 #pragma unroll
                 for (int j = 0; j < S::VS; ++j) acc[r][j] = f32x16{};
             }
-            uint64_t now[POS];
-            look(begin);
-            resolve();
-            look(begin + 1);
-            issue();
-            commit(smem);
+        };
+
+        // ---------------- the pipeline: block n of a wave is weighed while n + 1 has its exponentials taken and n + 2 its scores.  In step j V of step j and K
+        // of step j + LEAD are in LDS, the next ones in registers, those after them on their way to there.
+        {
+            constexpr int LEAD = S::LEAD;
+            Raw kraw, vraw;
+            Where way[LEAD + 1];                          // of steps j + 2 .. j + LEAD + 2
+            uint64_t there[LEAD + 3][POS];                // of steps j ..
+            Look asked;
+            f32x16 s0[RB], s1[RB];
+            Half p0[RB][2], p1[RB][2];
+            float f[RB];
+            {
+                Look first[LEAD + 2];
+                Where w[LEAD + 2];
+                Raw kr[LEAD];
+#pragma unroll
+                for (int i = 0; i < LEAD + 2; ++i) first[i] = look(begin + i);
+                asked = look(begin + LEAD + 2);
+#pragma unroll
+                for (int i = 0; i < LEAD + 2; ++i) {
+                    w[i] = resolve(first[i]);
+#pragma unroll
+                    for (int k = 0; k < POS; ++k) there[i][k] = w[i].there[k];
+                    if (i < LEAD) fetch(kbase, w[i].off, kr[i]);
+                    if (i == 0) fetch(vbase, w[0].off, vraw);
+                }
+                fetch(kbase, w[LEAD].off, kraw);
+#pragma unroll
+                for (int i = 0; i < LEAD; ++i) store(kbuf + i * S::TILE, kr[i], of_k);
+                store(vbuf, vraw, of_v);
+                if constexpr (LEAD == 1) store(kbuf + S::TILE, kraw, of_k);
+                __syncthreads();
+                clear();
+                scores(kbuf, 0, s0);
+                scores(LEAD == 1 ? kbuf : kbuf + S::TILE, LEAD == 1 ? 1 : 0, s1);
+                if constexpr (LEAD == 2) {
+                    __syncthreads();
+                    store(kbuf, kraw, of_k);
+                }
+                fetch(kbase, w[LEAD + 1].off, kraw);
+                fetch(vbase, w[1].off, vraw);
+                cover(begin, 0, there[0], s0);
+                exponents(s0, f);
+                rounded(s0, p0);
+#pragma unroll
+                for (int i = 0; i < LEAD; ++i) way[i] = w[i + 2];
+            }
             for (int step = begin; step < end; ++step) {
-                char *buf = smem + ((step - begin) & 1) * 2 * S::TILE, *other = smem + ((step - begin + 1) & 1) * 2 * S::TILE;
+                const int odd = (step - begin) & 1;
+                __syncthreads();                          // V of this step and K of step + LEAD are there, and nobody reads the other buffers any more
+                store(kbuf + ((odd + LEAD + 1) & 1) * S::TILE, kraw, of_k);
+                store(vbuf + (odd ^ 1) * S::TILE, vraw, of_v);
+                way[LEAD] = resolve(asked);
 #pragma unroll
-                for (int k = 0; k < POS; ++k) now[k] = there[k];
-                resolve();                                    // of step + 1, asked for a step ago
-                __syncthreads();                              // this step's K and V are there, and nobody reads the other buffer any more
-                if (step + 1 < end) {
-                    issue();
-                    look(step + 2);
+                for (int k = 0; k < POS; ++k) there[LEAD + 2][k] = way[LEAD].there[k];
+                if (step + 2 < end) {
+                    fetch(kbase, way[LEAD].off, kraw);
+                    fetch(vbase, way[0].off, vraw);
+                    asked = look(step + LEAD + 3);
                 }
-                // ---- S = K Q^T of the wave's 32 * PB positions
-                const int v0 = step * STEP + wk * 32 * PB;        // the first of them, in the span's count
-                const char *kt = buf, *vt = buf + S::TILE;
-                f32x16 s[PB][RB];
-#pragma unroll
-                for (int b = 0; b < PB; ++b) {
-                    const int rowk = (wk * PB + b) * 32 + c;
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) s[b][r] = f32x16{};
-#pragma unroll
-                    for (int k = 0; k < S::KS; ++k) {
-                        const bf16x8 a = *reinterpret_cast<const bf16x8*>(kt + piece_at<S>(rowk, 2 * k + g));
-#pragma unroll
-                        for (int r = 0; r < RB; ++r) s[b][r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[r][k], s[b][r], 0, 0, 0);
-                    }
-                }
-                // ---- what each row sees
-#pragma unroll
-                for (int b = 0; b < PB; ++b) {
-                    const int vb = v0 + 32 * b;
-                    const int in_step = (wk * PB + b) * 32;
-                    const unsigned is = (unsigned)(now[in_step / 64] >> (in_step & 63));
-                    const int first_pos = vb < span.sinks ? vb : vb - span.sinks + span.lo;
-                    const bool crosses = vb < span.sinks && vb + 32 > span.sinks;
+                const char *kt = kbuf + ((odd + LEAD) & 1) * S::TILE, *vt = vbuf + odd * S::TILE;
+                auto part = [&](int b, f32x16 (&cur)[RB], f32x16 (&next)[RB], Half (&pr)[RB][2], Half (&pn)[RB][2]) {
+                    cover(step + (b + 1) / PB, (b + 1) % PB, there[(b + 1) / PB], cur);
+                    scores(kt, b, next);
+                    weigh(vt, b, pr);
+                    const bool moves = exponents(cur, f);
+                    rounded(cur, pn);
+                    if (moves) rescale(f);
+                };
+                part(0, s1, s0, p0, p1);
+                if constexpr (PB == 2) part(1, s0, s1, p1, p0);
+                else {
 #pragma unroll
                     for (int r = 0; r < RB; ++r) {
-                        const bool all = is == 0xFFFFFFFFu && !crosses && first_pos + 31 <= last[r] && (first_pos >= from[r] || first_pos + 31 < p.sinks);
-                        if (__all(all || !real[r])) continue;
-                        uint64_t bits = 0;                        // of the new tokens from position context + nth on
-                        const int nth = vb - span.sinks + span.lo - seq.context;
-                        if (p.seen && nth > -32) {
-                            const uint32_t* w = p.seen + (int64_t)token[r] * p.seen_stride;
-                            const int k = nth >> 5;
-                            const uint64_t lo = k >= 0 && k < p.words ? w[k] : 0, hi = k + 1 >= 0 && k + 1 < p.words ? w[k + 1] : 0;
-                            bits = (lo | hi << 32) >> (nth & 31);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int e = 8 * (i / 4) + 4 * g + i % 4, v = vb + e, pos = v < span.sinks ? v : v - span.sinks + span.lo;
-                            bool on = pos <= last[r] && (pos >= from[r] || pos < p.sinks);
-                            if (p.seen && pos >= seq.context) on = bits >> e & 1;
-                            if (!on || !(is >> e & 1)) s[b][r][i] = -__builtin_inff();
-                        }
+                        s1[r] = s0[r];
+                        p0[r][0] = p1[r][0];
+                        p0[r][1] = p1[r][1];
                     }
                 }
-                // ---- probabilities
-                Half pr[PB][RB][2];
 #pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    float top = -__builtin_inff();
+                for (int i = 0; i < LEAD; ++i) way[i] = way[i + 1];
 #pragma unroll
-                    for (int b = 0; b < PB; ++b)
+                for (int i = 0; i < LEAD + 2; ++i)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][r][i]);
-                    top = fmaxf(top, __shfl_xor(top, 32)) * to_log2;
-                    if (__any(top > m[r] + kSlack)) {
-                        const float m_new = fmaxf(m[r], top), f = m[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[r] - m_new);
-                        l[r] *= f;
-#pragma unroll
-                        for (int j = 0; j < S::VS; ++j)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) acc[r][j][i] *= f;
-                        m[r] = m_new;
-                    }
-                    const float ref = (m[r] == -__builtin_inff() ? 0.0f : m[r]) - kUp;
-#pragma unroll
-                    for (int b = 0; b < PB; ++b) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            s[b][r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][r][i], to_log2, -ref));
-                            l[r] += s[b][r][i];
-                        }
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) pr[b][r][t][i] = s[b][r][8 * t + i];
-                    }
-                }
-                // ---- O^T += V^T P^T
-                if (!careful) {
-                    const int q4 = lane >> 4, sub = (lane & 15) >> 2, quad = lane & 3;
-#pragma unroll
-                    for (int b = 0; b < PB; ++b)
-#pragma unroll
-                        for (int t = 0; t < 2; ++t) {
-                            const int r0 = (wk * PB + b) * 32 + 16 * t + 4 * g + sub;
-#pragma unroll
-                            for (int j = 0; j < S::VS; ++j) {
-                                const int piece = 4 * j + 2 * (q4 & 1) + (quad >> 1);
-                                union { s16x4 h[2]; Half v; } a;
-#pragma unroll
-                                for (int h = 0; h < 2; ++h)
-                                    a.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                        (__attribute__((address_space(3))) s16x4*)(vt + piece_at<S>(r0 + 8 * h, piece) + 8 * (quad & 1)));
-#pragma unroll
-                                for (int r = 0; r < RB; ++r) {
-                                    if constexpr (E4M3) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[b][r][t], acc[r][j], 0, 0, 0);
-                                    else acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[b][r][t], acc[r][j], 0, 0, 0);
-                                }
-                            }
-                        }
-                } else {
-#pragma unroll
-                    for (int b = 0; b < PB; ++b)
-#pragma unroll
-                        for (int r = 0; r < RB; ++r) {
-                            wave_lds_order();
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) scratch[(8 * (i / 4) + 4 * g + i % 4) * 32 + c] = s[b][r][i];
-                            wave_lds_order();
-                            for (int e = 0; e < 32; ++e) {
-                                const float w = scratch[e * 32 + c];
-                                const int rowv = (wk * PB + b) * 32 + e;
-                                if (w == 0.0f) continue;
-#pragma unroll
-                                for (int j = 0; j < S::VS; ++j)
-#pragma unroll
-                                    for (int i4 = 0; i4 < 4; ++i4) {
-                                        const int col = 32 * j + 8 * i4 + 4 * g;
-                                        const uint2 raw = *reinterpret_cast<const uint2*>(vt + piece_at<S>(rowv, col >> 3) + 8 * g);
-                                        const unsigned u[2] = {raw.x, raw.y};
-#pragma unroll
-                                        for (int i = 0; i < 4; ++i) {
-                                            const unsigned short h = (unsigned short)(u[i / 2] >> 16 * (i & 1));
-                                            float val;
-                                            if constexpr (E4M3) val = (float)__builtin_bit_cast(_Float16, h);
-                                            else val = __uint_as_float((unsigned)h << 16);
-                                            acc[r][j][4 * i4 + i] = __builtin_fmaf(w, val, acc[r][j][4 * i4 + i]);
-                                        }
-                                    }
-                            }
-                        }
-                }
-                if (step + 1 < end) commit(other);
+                    for (int k = 0; k < POS; ++k) there[i][k] = there[i + 1][k];
             }
-            __syncthreads();                                  // all have read their last step
-            if (careful) break;
-            bool bad = false;
+            __syncthreads();                              // all have read their last step
+        }
+
+        bool bad = false;
 #pragma unroll
-            for (int r = 0; r < RB; ++r)
-                if (real[r])
+        for (int r = 0; r < RB; ++r)
+            if (real[r])
 #pragma unroll
-                    for (int j = 0; j < S::VS; ++j)
+                for (int j = 0; j < S::VS; ++j)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) bad = bad || !(fabsf(acc[r][j][i]) < __builtin_inff());
-            int* flags = reinterpret_cast<int*>(found);
-            const bool any = __any(bad);
-            if (lane == 0) flags[wave] = any ? 1 : 0;
-            __syncthreads();
-            bad = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
-            __syncthreads();
-            if (!bad) break;
+                    for (int i = 0; i < 16; ++i) bad = bad || !(fabsf(acc[r][j][i]) < __builtin_inff());
+        int* flags = reinterpret_cast<int*>(smem);
+        const bool any = __any(bad);
+        if (lane == 0) flags[wave] = any ? 1 : 0;
+        __syncthreads();
+        bad = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+        __syncthreads();
+        if (bad) {                                        // once more, with care and no haste
+            float* scratch = reinterpret_cast<float*>(smem + S::TILE) + wave * 32 * 32;      // one step of K is at kbuf, of V at its end
+            char* vt = smem + 3 * S::TILE;
+            clear();
+            for (int step = begin; step < end; ++step) {
+                const Where w = resolve(look(step));
+                Raw raw;
+                fetch(kbase, w.off, raw);
+                store(kbuf, raw, of_k);
+                fetch(vbase, w.off, raw);
+                store(vt, raw, of_v);
+                __syncthreads();
+                for (int b = 0; b < PB; ++b) {
+                    f32x16 s[RB];
+                    float f[RB];
+                    scores(kbuf, b, s);
+                    cover(step, b, w.there, s);
+                    if (exponents(s, f)) rescale(f);
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) {
+                        wave_lds_order();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) scratch[(8 * (i / 4) + 4 * g + i % 4) * 32 + c] = s[r][i];
+                        wave_lds_order();
+                        for (int e = 0; e < 32; ++e) {
+                            const float weight = scratch[e * 32 + c];
+                            if (weight == 0.0f) continue;
+#pragma unroll
+                            for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                                for (int i4 = 0; i4 < 4; ++i4) {
+                                    const uint2 raw2 = *reinterpret_cast<const uint2*>(vt + piece_at<S>((wk * PB + b) * 32 + e, 4 * j + i4) + 8 * g);
+                                    const unsigned u[2] = {raw2.x, raw2.y};
+#pragma unroll
+                                    for (int i = 0; i < 4; ++i) {
+                                        const unsigned short h = (unsigned short)(u[i / 2] >> 16 * (i & 1));
+                                        float val;
+                                        if constexpr (E4M3) val = (float)__builtin_bit_cast(_Float16, h);
+                                        else val = __uint_as_float((unsigned)h << 16);
+                                        acc[r][j][4 * i4 + i] = __builtin_fmaf(weight, val, acc[r][j][4 * i4 + i]);
+                                    }
+                                }
+                        }
+                    }
+                }
+                __syncthreads();
+            }
         }
 
         // ---------------- the end of the item, or of the share's part of it
