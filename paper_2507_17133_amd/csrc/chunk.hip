@@ -230,6 +230,16 @@ __device__ __forceinline__ int piece_at(int row, int piece)
     return S::N64 * S::STEP * 128 + row * 64 + (((piece & 3) ^ (row >> 1 & 3)) << 4);
 }
 
+// body(integral_constant 0), ... , body(integral_constant N - 1)
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void unrolled(F&& body)
+{
+    if constexpr (I < N) {
+        body(std::integral_constant<int, I>{});
+        unrolled<N, I + 1>(body);
+    }
+}
+
 // The n lowest bits (none for n <= 0, all from 32 on).
 __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; }
 
@@ -260,7 +270,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         const Seq seq(p, at.b);
         const int row = table_row(p, at.b);
         const Span span(p, seq, at.tile, S::ROWS, (unsigned)row < (unsigned)p.n_rows);
-        const int32_t* pages = p.pages + (int64_t)row * p.row_stride;
+        const int32_t* pages = p.pages + (span.n > 0 ? (int64_t)row * p.row_stride : 0);          // where there is nothing to see, any row will do
         const int steps = span.template steps<STEP>(), begin = at.step;
         const int end = p.whole ? steps : (int)min((int64_t)steps, at.step + (at.end - at.at));
         const int n_rows = seq.n * p.group;
@@ -269,27 +279,36 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         const unsigned flip = to_log2 < 0.0f ? 0x80008000u : 0u;              // the sign goes to q, so that the largest product is the largest score
         to_log2 = to_log2 != to_log2 ? to_log2 : fmaxf(fabsf(to_log2), 1.17549435e-38f);       // above 0: 0 times a masked -infinity would be NaN
 
-        // rows of this lane: where their results go, what they see
-        int token[RB], head[RB], last[RB], from[RB];
-        bool real[RB];
+        // rows of this lane: which they are, and what they see: the positions from `from` to `last` and the sinks
+        struct Row {
+            bool real;
+            int token, head, nth;                         // nth: the token's number in the sequence
+        };
+        auto row_of = [&](int r) {
+            const int i = at.tile * S::ROWS + (wm * RB + r) * 32 + c, j = min(i, n_rows - 1) / p.group;
+            return Row{i < n_rows, seq.t0 + j, at.hk * p.group + (i < n_rows ? i - j * p.group : 0), j};
+        };
+        int last[RB], from[RB];
         bf16x8 q[RB][S::KS];
 #pragma unroll
         for (int r = 0; r < RB; ++r) {
-            const int i = at.tile * S::ROWS + (wm * RB + r) * 32 + c, j = min(i, n_rows - 1) / p.group;
-            real[r] = i < n_rows;
-            token[r] = seq.t0 + j;
-            head[r] = at.hk * p.group + (real[r] ? i - j * p.group : 0);
-            int pos = seq.context + j;
-            if (p.positions) pos = max(seq.context, p.positions[token[r]]);
+            const Row o = row_of(r);
+            int pos = seq.context + o.nth;
+            if (p.positions) pos = max(seq.context, p.positions[o.token]);
             last[r] = p.seen ? seq.context - 1 : pos;
             from[r] = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
-            const bf16_t* src = p.q + (int64_t)token[r] * p.q_stride + (int64_t)head[r] * D;
+            if (!o.real) {                                // whatever it sees, nobody looks at it
+                last[r] = 0x7FFFFFFF;
+                from[r] = 0;
+            }
+            const bf16_t* src = p.q + (int64_t)o.token * p.q_stride + (int64_t)o.head * D;
 #pragma unroll
             for (int k = 0; k < S::KS; ++k) {
                 uint4 v = make_uint4(0, 0, 0, 0);
-                if (real[r]) v = *reinterpret_cast<const uint4*>(src + 16 * k + 8 * g);
+                if (o.real) v = *reinterpret_cast<const uint4*>(src + 16 * k + 8 * g);
                 v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
                 q[r][k] = __builtin_bit_cast(bf16x8, v);
+                if constexpr (S::RESIDENT == 1) asm volatile("" : "+a"(q[r][k]));      // operands may stay in accumulation registers
             }
         }
 
@@ -325,16 +344,12 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             Look o;
 #pragma unroll
             for (int k = 0; k < POS; ++k) {
-                const int v = step * STEP + 64 * k + lane, in = min(v, most - 1);
+                const int v = step * STEP + 64 * k + lane, in = max(min(v, most - 1), 0);
                 o.counts[k] = __ballot(v < most);
-                o.page[k] = -1;
-                o.in_page[k] = 0;
-                if (most > 0) {
-                    const unsigned pos = in < span.sinks ? in : in - span.sinks + span.lo;
-                    const unsigned pg = (unsigned)((uint64_t)pos * p.page_magic >> p.page_shift);
-                    o.in_page[k] = pos - pg * (unsigned)p.page_size;
-                    o.page[k] = pages[pg];
-                }
+                const unsigned pos = in < span.sinks ? in : in - span.sinks + span.lo;
+                const unsigned pg = (unsigned)((uint64_t)pos * p.page_magic >> p.page_shift);
+                o.in_page[k] = pos - pg * (unsigned)p.page_size;
+                o.page[k] = pages[pg];
             }
             return o;
         };
@@ -351,16 +366,22 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         // ---------------- K or V of a step, to registers and from there to LDS
         constexpr int ACROSS = E4M3 ? D / 16 : D / 8;                         // 16-byte pieces of a row in the cache
         constexpr int PIECES = (STEP * ACROSS + kChunkThreads - 1) / kChunkThreads;
+        constexpr bool SAME = kChunkThreads % ACROSS == 0;                    // a thread's pieces are of the same columns, rows apart
+        auto row_and_piece = [&](int i) {
+            const int id = i * kChunkThreads + tid;
+            return SAME ? make_int2(i * (kChunkThreads / ACROSS) + tid / ACROSS, tid % ACROSS) : make_int2(id / ACROSS, id % ACROSS);
+        };
         struct Raw {
             uint4 w[PIECES];
         };
         auto fetch = [&](const char* base, const unsigned (&off)[POS], Raw& raw) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const int id = i * kChunkThreads + tid, r = id / ACROSS, piece = id - r * ACROSS;
-                unsigned o = __shfl(off[0], r & 63);
+                const int r = row_and_piece(i).x, piece = row_and_piece(i).y;
+                // the lane is taken modulo 64
+                unsigned o = __builtin_amdgcn_ds_bpermute(4 * r, off[0]);
                 if constexpr (POS > 1) {
-                    const unsigned o1 = __shfl(off[POS - 1], r & 63);
+                    const unsigned o1 = __builtin_amdgcn_ds_bpermute(4 * r, off[POS - 1]);
                     o = r < 64 ? o : o1;
                 }
                 raw.w[i] = *reinterpret_cast<const uint4*>(base + 16 * piece + (uint64_t)o * 16);
@@ -369,7 +390,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         auto store = [&](char* tile, const Raw& raw, auto is_v) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const int id = i * kChunkThreads + tid, r = id / ACROSS, piece = id - r * ACROSS;
+                const int r = row_and_piece(i).x, piece = row_and_piece(i).y;
                 if (STEP * ACROSS % kChunkThreads != 0 && r >= STEP) continue;
                 const uint4 w = raw.w[i];
                 if constexpr (!E4M3) *reinterpret_cast<uint4*>(tile + piece_at<S>(r, piece)) = w;
@@ -405,7 +426,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             const int k = min(max(span.sinks - vb, 0), 32), at = vb - span.sinks + span.lo;
             bool all = is == 0xFFFFFFFFu && k == 0;
 #pragma unroll
-            for (int r = 0; r < RB; ++r) all = all && (!real[r] || (at + 31 <= last[r] && at >= from[r]));
+            for (int r = 0; r < RB; ++r) all = all && at + 31 <= last[r] && at >= from[r];
             if (__all(all)) return;
             const unsigned sink = below(k);
 #pragma unroll
@@ -413,7 +434,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                 unsigned on = below(last[r] - at + 1) & (~below(from[r] - at) | below(p.sinks - at));
                 const int nth = at - seq.context;         // of the new tokens, the one at position `at`
                 if (p.seen && nth > -32) {
-                    const uint32_t* w = p.seen + (int64_t)token[r] * p.seen_stride;
+                    const uint32_t* w = p.seen + (int64_t)row_of(r).token * p.seen_stride;
                     const int i = nth >> 5;
                     const uint64_t lo = i >= 0 && i < p.words ? w[i] : 0, hi = i + 1 < p.words ? w[i + 1] : 0;
                     on |= (unsigned)((lo | hi << 32) >> (nth & 31)) & ~below(-nth);
@@ -425,37 +446,44 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                     if (!(on >> (8 * (i / 4) + i % 4) & 1)) s[r][i] = -__builtin_inff();
             }
         };
-        // ---------------- probabilities in place of scores; f: what earlier sums are to be multiplied by.  Returns whether any of them are.
-        auto exponents = [&](f32x16 (&s)[RB], float (&f)[RB]) {
-            float top[RB];
+        // ---------------- probabilities in place of scores, in three steps: the maximum, what it changes, the exponentials.
+        auto largest = [&](const f32x16 (&s)[RB], float (&top)[RB], int i) {
+            const int r = i / 16;
+            top[r] = i % 16 ? fmaxf(top[r], s[r][i % 16]) : s[r][0];
+        };
+        // f: what earlier sums are to be multiplied by.  Returns whether any of them are; no branch, so that products go on around it.
+        auto refer = [&](float (&top)[RB], float (&f)[RB], float (&ref)[RB]) {
             bool moves = false;
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
-                top[r] = -__builtin_inff();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top[r] = fmaxf(top[r], s[r][i]);
                 const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[r]), __float_as_uint(top[r]), false, false);
                 top[r] = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * to_log2;
                 moves = moves || top[r] > m[r] + kSlack;
             }
             moves = __any(moves);
-            if (moves)
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    const float m_new = fmaxf(m[r], top[r]);
-                    f[r] = m[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[r] - m_new);
-                    l[r] *= f[r];
-                    m[r] = m_new;
-                }
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
-                const float ref = (m[r] == -__builtin_inff() ? 0.0f : m[r]) - kUp;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[r][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i], to_log2, -ref));
-                    l[r] += s[r][i];
-                }
+                const float m_new = moves ? fmaxf(m[r], top[r]) : m[r];
+                f[r] = m[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[r] - m_new);
+                l[r] *= f[r];
+                m[r] = m_new;
+                ref[r] = (m_new == -__builtin_inff() ? 0.0f : m_new) - kUp;
             }
+            return moves;
+        };
+        auto exponent = [&](f32x16 (&s)[RB], const float (&ref)[RB], int i) {
+            const int r = i / 16;
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i % 16], to_log2, -ref[r]));
+            l[r] += e;
+            s[r][i % 16] = e;
+        };
+        auto exponents = [&](f32x16 (&s)[RB], float (&f)[RB]) {
+            float top[RB], ref[RB];
+#pragma unroll
+            for (int i = 0; i < 16 * RB; ++i) largest(s, top, i);
+            const bool moves = refer(top, f, ref);
+#pragma unroll
+            for (int i = 0; i < 16 * RB; ++i) exponent(s, ref, i);
             return moves;
         };
         auto rescale = [&](const float (&f)[RB]) {
@@ -474,24 +502,33 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
 #pragma unroll
                     for (int i = 0; i < 8; ++i) pr[r][t][i] = s[r][8 * t + i];
         };
-        // ---------------- O^T += V^T P^T
-        auto weigh = [&](const char* vt, int b, const Half (&pr)[RB][2]) {
+        // ---------------- a block's products in slots of RB: KS of S = K Q^T, then 2 * VS of O^T += V^T P^T; their operand from K or V
+        union Operand {
+            bf16x8 k;
+            s16x4 h[2];
+            Half v;
+        };
+        auto operand = [&](auto slot, const char* kt, const char* vt, int b, Operand& a) {
+            constexpr int k = decltype(slot)::value, t = (k - S::KS) / S::VS, j = (k - S::KS) % S::VS;
+            if constexpr (k < S::KS)
+                a.k = *reinterpret_cast<const bf16x8*>(
+                    kt + (k < 4 * S::N64 ? kat[k & 3] + (k >> 2) * STEP * 128 + b * 32 * 128 : kat32[k & 1] + b * 32 * 64));
+            else {
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+                for (int h = 0; h < 2; ++h)
+                    a.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4*)(vt + (j < 2 * S::N64 ? vat[j & 1] + (j >> 1) * STEP * 128 + (32 * b + 16 * t + 8 * h) * 128
+                                                                                         : vat32 + (32 * b + 16 * t + 8 * h) * 64)));
+            }
+        };
+        auto product = [&](auto slot, const Operand& a, f32x16 (&s)[RB], const Half (&pr)[RB][2]) {
+            constexpr int k = decltype(slot)::value, t = (k - S::KS) / S::VS, j = (k - S::KS) % S::VS;
 #pragma unroll
-                for (int j = 0; j < S::VS; ++j) {
-                    union { s16x4 h[2]; Half v; } a;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        a.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (__attribute__((address_space(3))) s16x4*)(vt + (j < 2 * S::N64 ? vat[j & 1] + (j >> 1) * STEP * 128 + (32 * b + 16 * t + 8 * h) * 128
-                                                                                             : vat32 + (32 * b + 16 * t + 8 * h) * 64)));
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        if constexpr (E4M3) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
-                        else acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
-                    }
-                }
+            for (int r = 0; r < RB; ++r) {
+                if constexpr (k < S::KS) s[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.k, q[r][k], k == 0 ? f32x16{} : s[r], 0, 0, 0);
+                else if constexpr (E4M3) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
+                else acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
+            }
         };
         auto clear = [&]() {
 #pragma unroll
@@ -553,27 +590,56 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             for (int step = begin; step < end; ++step) {
                 const int odd = (step - begin) & 1;
                 __syncthreads();                          // V of this step and K of step + LEAD are there, and nobody reads the other buffers any more
-                store(kbuf + ((odd + LEAD + 1) & 1) * S::TILE, kraw, of_k);
-                store(vbuf + (odd ^ 1) * S::TILE, vraw, of_v);
-                way[LEAD] = resolve(asked);
-#pragma unroll
-                for (int k = 0; k < POS; ++k) there[LEAD + 2][k] = way[LEAD].there[k];
-                if (step + 2 < end) {
-                    fetch(kbase, way[LEAD].off, kraw);
-                    fetch(vbase, way[0].off, vraw);
-                    asked = look(step + LEAD + 3);
-                }
                 const char *kt = kbuf + ((odd + LEAD) & 1) * S::TILE, *vt = vbuf + odd * S::TILE;
-                auto part = [&](int b, f32x16 (&cur)[RB], f32x16 (&next)[RB], Half (&pr)[RB][2], Half (&pn)[RB][2]) {
-                    cover(step + (b + 1) / PB, (b + 1) % PB, there[(b + 1) / PB], cur);
-                    scores(kt, b, next);
-                    weigh(vt, b, pr);
-                    const bool moves = exponents(cur, f);
-                    rounded(cur, pn);
-                    if (moves) rescale(f);
+                // what a step has to do besides, one thing behind each of the first slots
+                auto beside = [&](auto slot) {
+                    constexpr int k = decltype(slot)::value;
+                    if constexpr (k == 0) store(kbuf + ((odd + LEAD + 1) & 1) * S::TILE, kraw, of_k);
+                    if constexpr (k == 1) store(vbuf + (odd ^ 1) * S::TILE, vraw, of_v);
+                    if constexpr (k == 2) {
+                        way[LEAD] = resolve(asked);
+#pragma unroll
+                        for (int i = 0; i < POS; ++i) there[LEAD + 2][i] = way[LEAD].there[i];
+                    }
+                    if constexpr (k == 3) fetch(kbase, way[LEAD].off, kraw);
+                    if constexpr (k == 4) fetch(vbase, way[0].off, vraw);
+                    if constexpr (k == 5) asked = look(step + LEAD + 3);
                 };
-                part(0, s1, s0, p0, p1);
-                if constexpr (PB == 2) part(1, s0, s1, p1, p0);
+                auto part = [&](auto b_, f32x16 (&cur)[RB], f32x16 (&next)[RB], Half (&pr)[RB][2], Half (&pn)[RB][2]) {
+                    constexpr int b = decltype(b_)::value, SLOTS = S::KS + 2 * S::VS, FIRST = SLOTS / 4, AHEAD = 2, ALL = 16 * RB;
+                    Operand a[AHEAD + 1];
+                    unrolled<AHEAD>([&](auto i) { operand(i, kt, vt, b, a[i]); });
+                    cover(step + (b + 1) / PB, (b + 1) % PB, there[(b + 1) / PB], cur);
+                    float top[RB], ref[RB];
+                    bool moves = false;
+                    unrolled<SLOTS>([&](auto i) {
+                        constexpr int k = decltype(i)::value;
+                        if constexpr (k + AHEAD < SLOTS) operand(std::integral_constant<int, k + AHEAD>{}, kt, vt, b, a[(k + AHEAD) % (AHEAD + 1)]);
+                        product(i, a[k % (AHEAD + 1)], next, pr);
+                        if constexpr (k < FIRST) {
+#pragma unroll
+                            for (int e = ALL * k / FIRST; e < ALL * (k + 1) / FIRST; ++e) largest(cur, top, e);
+                            if constexpr (k == FIRST - 1) moves = refer(top, f, ref);
+                        } else {
+                            constexpr int N = SLOTS - FIRST, e0 = ALL * (k - FIRST) / N / 2 * 2, e1 = k == SLOTS - 1 ? ALL : ALL * (k - FIRST + 1) / N / 2 * 2;
+#pragma unroll
+                            for (int e = e0; e < e1; ++e) {
+                                exponent(cur, ref, e);
+                                pn[e / 16][e % 16 / 8][e % 8] = cur[e / 16][e % 16];
+                            }
+                        }
+                        if constexpr (b == 0) beside(i);
+                        __builtin_amdgcn_sched_barrier(0);
+                    });
+#pragma unroll
+                    for (int r = 0; r < RB; ++r) asm volatile("" : "+v"(pn[r][0]), "+v"(pn[r][1]), "+v"(l[r]), "+v"(next[r]));        // here, and not where they are needed
+                    if (__builtin_expect(moves, 0)) {
+                        asm volatile("");                 // seldom: a branch, not a product with one
+                        rescale(f);
+                    }
+                };
+                part(std::integral_constant<int, 0>{}, s1, s0, p0, p1);
+                if constexpr (PB == 2) part(std::integral_constant<int, 1>{}, s0, s1, p1, p0);
                 else {
 #pragma unroll
                     for (int r = 0; r < RB; ++r) {
@@ -595,7 +661,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         bool bad = false;
 #pragma unroll
         for (int r = 0; r < RB; ++r)
-            if (real[r])
+            if (row_of(r).real)
 #pragma unroll
                 for (int j = 0; j < S::VS; ++j)
 #pragma unroll
@@ -715,16 +781,17 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
 #pragma unroll
             for (int r = 0; r < RB; ++r) {
                 if (begins && ends) {
-                    if (!real[r]) continue;
+                    const Row o = row_of(r);
+                    if (!o.real) continue;
                     const float k = l[r] > 0.0f || l[r] != l[r] ? (E4M3 ? p.v_scale[at.hk] : 1.0f) / l[r] : 0.0f;
-                    bf16_t* dst = p.out + (int64_t)token[r] * p.out_stride + (int64_t)head[r] * D;
+                    bf16_t* dst = p.out + (int64_t)o.token * p.out_stride + (int64_t)o.head * D;
 #pragma unroll
                     for (int j = 0; j < S::VS; ++j)
 #pragma unroll
                         for (int i4 = 0; i4 < 4; ++i4)
                             *reinterpret_cast<uint2*>(dst + 32 * j + 8 * i4 + 4 * g) =
                                 make_uint2(pack_bf16(acc[r][j][4 * i4] * k, acc[r][j][4 * i4 + 1] * k), pack_bf16(acc[r][j][4 * i4 + 2] * k, acc[r][j][4 * i4 + 3] * k));
-                    if (p.lse && g == 0) p.lse[(int64_t)token[r] * p.H + head[r]] = (m[r] - kUp + __log2f(l[r])) * 0.6931471805599453f;
+                    if (p.lse && g == 0) p.lse[(int64_t)o.token * p.H + o.head] = (m[r] - kUp + __log2f(l[r])) * 0.6931471805599453f;
                 } else {
                     float* part = p.parts + (2 * (int64_t)blockIdx.x + (begins ? 1 : 0)) * S::PART;
                     const int i = (wm * RB + r) * 32 + c;
