@@ -44,6 +44,7 @@ struct Shape {
     static constexpr int TILE = STEP * D * 2;                                 // bytes of K (of V) of a step in LDS
     static constexpr int KS = D / 16, VS = D / 32;                            // products along D, blocks of 32 columns of V
     static constexpr int LEAD = 2 / PB;                                       // steps that K is ahead of V
+    static constexpr int AHEAD = 4;                                           // slots that LDS reads are ahead of the products
     static constexpr int LDS = 4 * TILE;                                      // two steps of K, two of V
     static_assert(PB <= 2 && kChunkWaves * 32 * 32 * 4 <= 2 * TILE && (WK - 1) * WM * 32 * RB * (D + 4) * 4 <= LDS, "what else LDS holds");
     static constexpr int RESIDENT = LDS <= 80 * 1024 && RB * D <= 128 ? 2 : 1;   // blocks of a CU
@@ -222,13 +223,20 @@ __device__ __forceinline__ unsigned to_bf16(unsigned w) { return __builtin_bit_c
 template <bool HIGH>
 __device__ __forceinline__ unsigned to_f16(unsigned w) { return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, HIGH)); }
 
+// Where a panel's 16-byte pieces of a row are: exchanged so that 16 rows' same piece (K's operand) and 4 rows' four neighbours (V's) lie in different banks.
+__device__ __forceinline__ int turn64(int row) { return (row & 2) << 1 | (row & 4) >> 1 | (row & 8) >> 3; }
+__device__ __forceinline__ int turn32(int row) { return row >> 2 & 3; }
+
 // Byte of (row, 16-byte piece of the row's columns) in a step's K or V.
 template <class S>
 __device__ __forceinline__ int piece_at(int row, int piece)
 {
-    if (S::N32 == 0 || piece < 8 * S::N64) return (piece >> 3) * S::STEP * 128 + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
-    return S::N64 * S::STEP * 128 + row * 64 + (((piece & 3) ^ (row >> 1 & 3)) << 4);
+    if (S::N32 == 0 || piece < 8 * S::N64) return (piece >> 3) * S::STEP * 128 + row * 128 + (((piece & 7) ^ turn64(row)) << 4);
+    return S::N64 * S::STEP * 128 + row * 64 + (((piece & 3) ^ turn32(row)) << 4);
 }
+
+template <typename T>
+__device__ __forceinline__ __attribute__((address_space(3))) T* at_lds(unsigned byte) { return (__attribute__((address_space(3))) T*)(uintptr_t)byte; }
 
 // body(integral_constant 0), ... , body(integral_constant N - 1)
 template <int N, int I = 0, typename F>
@@ -312,19 +320,10 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             }
         }
 
-        // LDS offsets of a lane: its K row's pieces of a panel, and its V rows' pieces of even and odd blocks of 32 columns
-        int kat[4], kat32[2], vat[2], vat32;
-        {
-            const int sub = 4 * g + ((lane & 15) >> 2), piece = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), in = 8 * (lane & 1);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) kat[k] = (wk * PB * 32 + c) * 128 + (((2 * k + g) ^ (c & 7)) << 4);
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                kat32[k] = S::N64 * STEP * 128 + (wk * PB * 32 + c) * 64 + (((2 * k + g) ^ (c >> 1 & 3)) << 4);
-                vat[k] = (wk * PB * 32 + sub) * 128 + (((4 * k + piece) ^ sub) << 4) + in;
-            }
-            vat32 = S::N64 * STEP * 128 + (wk * PB * 32 + sub) * 64 + ((piece ^ (sub >> 1 & 3)) << 4) + in;
-        }
+        // LDS offsets of a lane: its K row's first piece of a panel, its V row's; the others are these with a few bits turned
+        const int rk = wk * PB * 32 + c, sub = 4 * g + ((lane & 15) >> 2), rv = wk * PB * 32 + sub, piece = 2 * (lane >> 4 & 1) + (lane >> 1 & 1), in = 8 * (lane & 1);
+        const int kat = rk * 128 + ((g ^ turn64(c)) << 4), kat32 = S::N64 * STEP * 128 + rk * 64 + ((g ^ turn32(c)) << 4);
+        const int vat = rv * 128 + ((piece ^ turn64(sub)) << 4) + in, vat32 = S::N64 * STEP * 128 + rv * 64 + ((piece ^ turn32(sub)) << 4) + in;
 
         f32x16 acc[RB][S::VS];
         float m[RB], l[RB];
@@ -374,18 +373,25 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         struct Raw {
             uint4 w[PIECES];
         };
-        auto fetch = [&](const char* base, const unsigned (&off)[POS], Raw& raw) {
+        auto spread = [&](const unsigned (&off)[POS], unsigned (&o)[PIECES]) {          // to the threads that read there
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
-                const int r = row_and_piece(i).x, piece = row_and_piece(i).y;
-                // the lane is taken modulo 64
-                unsigned o = __builtin_amdgcn_ds_bpermute(4 * r, off[0]);
+                const int r = row_and_piece(i).x;
+                o[i] = __builtin_amdgcn_ds_bpermute(4 * r, off[0]);                      // the lane is taken modulo 64
                 if constexpr (POS > 1) {
                     const unsigned o1 = __builtin_amdgcn_ds_bpermute(4 * r, off[POS - 1]);
-                    o = r < 64 ? o : o1;
+                    o[i] = r < 64 ? o[i] : o1;
                 }
-                raw.w[i] = *reinterpret_cast<const uint4*>(base + 16 * piece + (uint64_t)o * 16);
             }
+        };
+        auto read = [&](const char* base, const unsigned (&o)[PIECES], Raw& raw) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) raw.w[i] = *reinterpret_cast<const uint4*>(base + 16 * row_and_piece(i).y + (uint64_t)o[i] * 16);
+        };
+        auto fetch = [&](const char* base, const unsigned (&off)[POS], Raw& raw) {
+            unsigned o[PIECES];
+            spread(off, o);
+            read(base, o, raw);
         };
         auto store = [&](char* tile, const Raw& raw, auto is_v) {
 #pragma unroll
@@ -405,18 +411,6 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         };
         constexpr std::false_type of_k{};
         constexpr std::true_type of_v{};
-        // ---------------- S of the wave's block b of a step
-        auto scores = [&](const char* kt, int b, f32x16 (&s)[RB]) {
-#pragma unroll
-            for (int r = 0; r < RB; ++r) s[r] = f32x16{};
-#pragma unroll
-            for (int k = 0; k < S::KS; ++k) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8*>(
-                    kt + (k < 4 * S::N64 ? kat[k & 3] + (k >> 2) * STEP * 128 + b * 32 * 128 : kat32[k & 1] + b * 32 * 64));
-#pragma unroll
-                for (int r = 0; r < RB; ++r) s[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[r][k], s[r], 0, 0, 0);
-            }
-        };
         // ---------------- what each row sees of it: a bit for each of the 32 positions
         auto cover = [&](int step, int b, const uint64_t (&there)[POS], f32x16 (&s)[RB]) {
             const int in_step = (wk * PB + b) * 32, vb = step * STEP + in_step;
@@ -508,18 +502,25 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             s16x4 h[2];
             Half v;
         };
-        auto operand = [&](auto slot, const char* kt, const char* vt, int b, Operand& a) {
+        struct Lds {
+            unsigned k, k32, v, v32;                      // of a lane in this step's K and V
+        };
+        auto operand = [&](auto slot, const Lds& o, int b, Operand& a) {
             constexpr int k = decltype(slot)::value, t = (k - S::KS) / S::VS, j = (k - S::KS) % S::VS;
-            if constexpr (k < S::KS)
-                a.k = *reinterpret_cast<const bf16x8*>(
-                    kt + (k < 4 * S::N64 ? kat[k & 3] + (k >> 2) * STEP * 128 + b * 32 * 128 : kat32[k & 1] + b * 32 * 64));
+            if constexpr (k < 4 * S::N64) a.k = *at_lds<bf16x8>((o.k ^ (k & 3) << 5) + (k >> 2) * STEP * 128 + b * 32 * 128);
+            else if constexpr (k < S::KS) a.k = *at_lds<bf16x8>((o.k32 ^ (k & 1) << 5) + b * 32 * 64);
             else {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    a.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4*)(vt + (j < 2 * S::N64 ? vat[j & 1] + (j >> 1) * STEP * 128 + (32 * b + 16 * t + 8 * h) * 128
-                                                                                         : vat32 + (32 * b + 16 * t + 8 * h) * 64)));
+                for (int h = 0; h < 2; ++h) {             // row r + 8 h
+                    const unsigned at = j < 2 * S::N64 ? (o.v ^ ((j & 1) << 6 | h << 4)) + (j >> 1) * STEP * 128 + (32 * b + 16 * t + 8 * h) * 128
+                                                       : (o.v32 ^ h << 5) + (32 * b + 16 * t + 8 * h) * 64;
+                    a.h[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at_lds<s16x4>(at));
+                }
             }
+        };
+        auto lds_of = [&](const char* kt, const char* vt) {
+            const unsigned k = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)kt, v = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)vt;
+            return Lds{k + kat, k + kat32, v + vat, v + vat32};
         };
         auto product = [&](auto slot, const Operand& a, f32x16 (&s)[RB], const Half (&pr)[RB][2]) {
             constexpr int k = decltype(slot)::value, t = (k - S::KS) / S::VS, j = (k - S::KS) % S::VS;
@@ -529,6 +530,19 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                 else if constexpr (E4M3) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
                 else acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
             }
+        };
+        auto scores = [&](const Lds& o, int b, f32x16 (&s)[RB]) {
+            const Half none[RB][2] = {};
+            unrolled<S::KS>([&](auto k) {
+                Operand a;
+                operand(k, o, b, a);
+                product(k, a, s, none);
+            });
+        };
+        // loads from memory stay on their way across it
+        auto lds_sync = [&]() {
+            __builtin_amdgcn_s_waitcnt(0xC07F);           // lgkmcnt(0)
+            lds_barrier();
         };
         auto clear = [&]() {
 #pragma unroll
@@ -573,8 +587,8 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                 if constexpr (LEAD == 1) store(kbuf + S::TILE, kraw, of_k);
                 __syncthreads();
                 clear();
-                scores(kbuf, 0, s0);
-                scores(LEAD == 1 ? kbuf : kbuf + S::TILE, LEAD == 1 ? 1 : 0, s1);
+                scores(lds_of(kbuf, vbuf), 0, s0);
+                scores(lds_of(LEAD == 1 ? kbuf : kbuf + S::TILE, vbuf), LEAD == 1 ? 1 : 0, s1);
                 if constexpr (LEAD == 2) {
                     __syncthreads();
                     store(kbuf, kraw, of_k);
@@ -589,8 +603,9 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             }
             for (int step = begin; step < end; ++step) {
                 const int odd = (step - begin) & 1;
-                __syncthreads();                          // V of this step and K of step + LEAD are there, and nobody reads the other buffers any more
-                const char *kt = kbuf + ((odd + LEAD) & 1) * S::TILE, *vt = vbuf + odd * S::TILE;
+                lds_sync();                               // V of this step and K of step + LEAD are there, and nobody reads the other buffers any more
+                unsigned ko[PIECES], vo[PIECES];
+                const Lds tiles = lds_of(kbuf + ((odd + LEAD) & 1) * S::TILE, vbuf + odd * S::TILE);
                 // what a step has to do besides, one thing behind each of the first slots
                 auto beside = [&](auto slot) {
                     constexpr int k = decltype(slot)::value;
@@ -601,20 +616,22 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
 #pragma unroll
                         for (int i = 0; i < POS; ++i) there[LEAD + 2][i] = way[LEAD].there[i];
                     }
-                    if constexpr (k == 3) fetch(kbase, way[LEAD].off, kraw);
-                    if constexpr (k == 4) fetch(vbase, way[0].off, vraw);
+                    if constexpr (k == 2) spread(way[LEAD].off, ko);
+                    if constexpr (k == 3) spread(way[0].off, vo);
+                    if constexpr (k == 4) read(kbase, ko, kraw);
+                    if constexpr (k == 5) read(vbase, vo, vraw);
                     if constexpr (k == 5) asked = look(step + LEAD + 3);
                 };
                 auto part = [&](auto b_, f32x16 (&cur)[RB], f32x16 (&next)[RB], Half (&pr)[RB][2], Half (&pn)[RB][2]) {
-                    constexpr int b = decltype(b_)::value, SLOTS = S::KS + 2 * S::VS, FIRST = SLOTS / 4, AHEAD = 2, ALL = 16 * RB;
+                    constexpr int b = decltype(b_)::value, SLOTS = S::KS + 2 * S::VS, FIRST = SLOTS / 4, AHEAD = S::AHEAD, ALL = 16 * RB;
                     Operand a[AHEAD + 1];
-                    unrolled<AHEAD>([&](auto i) { operand(i, kt, vt, b, a[i]); });
+                    unrolled<AHEAD>([&](auto i) { operand(i, tiles, b, a[i]); });
                     cover(step + (b + 1) / PB, (b + 1) % PB, there[(b + 1) / PB], cur);
                     float top[RB], ref[RB];
                     bool moves = false;
                     unrolled<SLOTS>([&](auto i) {
                         constexpr int k = decltype(i)::value;
-                        if constexpr (k + AHEAD < SLOTS) operand(std::integral_constant<int, k + AHEAD>{}, kt, vt, b, a[(k + AHEAD) % (AHEAD + 1)]);
+                        if constexpr (k + AHEAD < SLOTS) operand(std::integral_constant<int, k + AHEAD>{}, tiles, b, a[(k + AHEAD) % (AHEAD + 1)]);
                         product(i, a[k % (AHEAD + 1)], next, pr);
                         if constexpr (k < FIRST) {
 #pragma unroll
@@ -687,7 +704,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                 for (int b = 0; b < PB; ++b) {
                     f32x16 s[RB];
                     float f[RB];
-                    scores(kbuf, b, s);
+                    scores(lds_of(kbuf, vt), b, s);
                     cover(step, b, w.there, s);
                     if (exponents(s, f)) rescale(f);
 #pragma unroll
