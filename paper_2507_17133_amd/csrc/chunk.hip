@@ -28,7 +28,6 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kChunkWaves = 4, kChunkThreads = 64 * kChunkWaves;
 constexpr int kChunkShares = 512;                 // shares of the line of steps at most
 constexpr float kSlack = 4.0f;                    // how far (in powers of two) scores may exceed the maximum that they refer to
 constexpr int kMostContext = 0x7FFE0000;          // so that positions of new tokens stay in 32 bits
@@ -38,16 +37,18 @@ template <int D_, bool E4M3_, int RB_, int WM_, int WK_, int PB_>
 struct Shape {
     static constexpr int D = D_, RB = RB_, WM = WM_, WK = WK_, PB = PB_;
     static constexpr bool E4M3 = E4M3_;
-    static_assert(WM * WK == kChunkWaves, "four waves");
+    static constexpr int WAVES = WM * WK, THREADS = 64 * WAVES;
+    static_assert(WAVES == 4 || WAVES == 8, "waves of a block");
     static constexpr int ROWS = 32 * RB * WM, STEP = 32 * PB * WK;
     static constexpr int N64 = D / 64, N32 = D % 64 / 32;                     // panels of 64 columns, and one of 32
     static constexpr int TILE = STEP * D * 2;                                 // bytes of K (of V) of a step in LDS
     static constexpr int KS = D / 16, VS = D / 32;                            // products along D, blocks of 32 columns of V
     static constexpr int LEAD = 2 / PB;                                       // steps that K is ahead of V
-    static constexpr int AHEAD = 4;                                           // slots that LDS reads are ahead of the products
-    static constexpr int LDS = 4 * TILE;                                      // two steps of K, two of V
-    static_assert(PB <= 2 && kChunkWaves * 32 * 32 * 4 <= 2 * TILE && (WK - 1) * WM * 32 * RB * (D + 4) * 4 <= LDS, "what else LDS holds");
-    static constexpr int RESIDENT = LDS <= 80 * 1024 && RB * D <= 128 ? 2 : 1;   // blocks of a CU
+    static constexpr int AHEAD = 2;                                           // slots that LDS reads are ahead of the products
+    static constexpr int SCRATCH = WAVES * 32 * 32 * 4;                       // probabilities of the careful second product
+    static constexpr int LDS = 4 * TILE > 2 * TILE + SCRATCH ? 4 * TILE : 2 * TILE + SCRATCH;                                      // two steps of K, two of V
+    static_assert(PB <= 2 && (WK - 1) * WM * 32 * RB * (D + 4) * 4 <= LDS, "what else LDS holds");
+    static constexpr int RESIDENT = WAVES == 4 && LDS <= 80 * 1024 && RB * D <= 128 ? 2 : 1;   // blocks of a CU
     // floats of a part: [ROWS][D] O, [ROWS] m, [ROWS] l
     static constexpr int64_t PART = (int64_t)ROWS * (D + 2);
 };
@@ -143,7 +144,7 @@ template <class S>
 __device__ __forceinline__ bool find_share(const ChunkArgs& p, int64_t* lds, Begin& o)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = (p.n_seqs + kChunkThreads - 1) / kChunkThreads, b0 = min(p.n_seqs, tid * each), b1 = min(p.n_seqs, b0 + each);
+    const int each = (p.n_seqs + S::THREADS - 1) / S::THREADS, b0 = min(p.n_seqs, tid * each), b1 = min(p.n_seqs, b0 + each);
     int64_t mine = 0;
     for (int b = b0; b < b1; ++b) mine += steps_of<S>(p, b) * p.Hk;
     int64_t total;
@@ -152,7 +153,7 @@ __device__ __forceinline__ bool find_share(const ChunkArgs& p, int64_t* lds, Beg
     __syncthreads();
     int64_t all = 0;
 #pragma unroll
-    for (int w = 0; w < kChunkWaves; ++w) {
+    for (int w = 0; w < S::WAVES; ++w) {
         if (w < wave) before += lds[w];
         all += lds[w];
     }
@@ -176,16 +177,16 @@ __device__ __forceinline__ bool find_share(const ChunkArgs& p, int64_t* lds, Beg
             if (o.at < before + (int64_t)n * p.Hk) break;
             before += (int64_t)n * p.Hk;
         }
-        lds[kChunkWaves] = b;
-        lds[kChunkWaves + 1] = tile;
-        lds[kChunkWaves + 2] = (o.at - before) / n;
-        lds[kChunkWaves + 3] = (o.at - before) % n;
+        lds[S::WAVES] = b;
+        lds[S::WAVES + 1] = tile;
+        lds[S::WAVES + 2] = (o.at - before) / n;
+        lds[S::WAVES + 3] = (o.at - before) % n;
     }
     __syncthreads();
-    o.b = __builtin_amdgcn_readfirstlane((int)lds[kChunkWaves]);
-    o.tile = __builtin_amdgcn_readfirstlane((int)lds[kChunkWaves + 1]);
-    o.hk = __builtin_amdgcn_readfirstlane((int)lds[kChunkWaves + 2]);
-    o.step = __builtin_amdgcn_readfirstlane((int)lds[kChunkWaves + 3]);
+    o.b = __builtin_amdgcn_readfirstlane((int)lds[S::WAVES]);
+    o.tile = __builtin_amdgcn_readfirstlane((int)lds[S::WAVES + 1]);
+    o.hk = __builtin_amdgcn_readfirstlane((int)lds[S::WAVES + 2]);
+    o.step = __builtin_amdgcn_readfirstlane((int)lds[S::WAVES + 3]);
     __syncthreads();
     return true;
 }
@@ -252,7 +253,7 @@ __device__ __forceinline__ void unrolled(F&& body)
 __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; }
 
 template <class S>
-__global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(ChunkArgs p)
+__global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArgs p)
 {
     constexpr int D = S::D, RB = S::RB, WM = S::WM, WK = S::WK, PB = S::PB, STEP = S::STEP, POS = STEP / 64;
     constexpr bool E4M3 = S::E4M3;
@@ -296,6 +297,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
             const int i = at.tile * S::ROWS + (wm * RB + r) * 32 + c, j = min(i, n_rows - 1) / p.group;
             return Row{i < n_rows, seq.t0 + j, at.hk * p.group + (i < n_rows ? i - j * p.group : 0), j};
         };
+        const bool idle = at.tile * S::ROWS + wm * RB * 32 >= n_rows;         // a wave without rows only brings K and V
         int last[RB], from[RB];
         bf16x8 q[RB][S::KS];
 #pragma unroll
@@ -316,7 +318,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                 if (o.real) v = *reinterpret_cast<const uint4*>(src + 16 * k + 8 * g);
                 v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
                 q[r][k] = __builtin_bit_cast(bf16x8, v);
-                if constexpr (S::RESIDENT == 1) asm volatile("" : "+a"(q[r][k]));      // operands may stay in accumulation registers
+                if constexpr (S::WAVES == 4 && S::RESIDENT == 1) asm volatile("" : "+a"(q[r][k]));      // operands may stay in accumulation registers
             }
         }
 
@@ -364,11 +366,11 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         };
         // ---------------- K or V of a step, to registers and from there to LDS
         constexpr int ACROSS = E4M3 ? D / 16 : D / 8;                         // 16-byte pieces of a row in the cache
-        constexpr int PIECES = (STEP * ACROSS + kChunkThreads - 1) / kChunkThreads;
-        constexpr bool SAME = kChunkThreads % ACROSS == 0;                    // a thread's pieces are of the same columns, rows apart
+        constexpr int PIECES = (STEP * ACROSS + S::THREADS - 1) / S::THREADS;
+        constexpr bool SAME = S::THREADS % ACROSS == 0;                    // a thread's pieces are of the same columns, rows apart
         auto row_and_piece = [&](int i) {
-            const int id = i * kChunkThreads + tid;
-            return SAME ? make_int2(i * (kChunkThreads / ACROSS) + tid / ACROSS, tid % ACROSS) : make_int2(id / ACROSS, id % ACROSS);
+            const int id = i * S::THREADS + tid;
+            return SAME ? make_int2(i * (S::THREADS / ACROSS) + tid / ACROSS, tid % ACROSS) : make_int2(id / ACROSS, id % ACROSS);
         };
         struct Raw {
             uint4 w[PIECES];
@@ -397,7 +399,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) {
                 const int r = row_and_piece(i).x, piece = row_and_piece(i).y;
-                if (STEP * ACROSS % kChunkThreads != 0 && r >= STEP) continue;
+                if (STEP * ACROSS % S::THREADS != 0 && r >= STEP) continue;
                 const uint4 w = raw.w[i];
                 if constexpr (!E4M3) *reinterpret_cast<uint4*>(tile + piece_at<S>(r, piece)) = w;
                 else if constexpr (decltype(is_v)::value) {
@@ -559,7 +561,7 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         {
             constexpr int LEAD = S::LEAD;
             Raw kraw, vraw;
-            Where way[LEAD + 1];                          // of steps j + 2 .. j + LEAD + 2
+            unsigned spots[LEAD][PIECES];                 // where the thread reads, of steps j + 2 .. j + LEAD + 1
             uint64_t there[LEAD + 3][POS];                // of steps j ..
             Look asked;
             f32x16 s0[RB], s1[RB];
@@ -599,12 +601,18 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                 exponents(s0, f);
                 rounded(s0, p0);
 #pragma unroll
-                for (int i = 0; i < LEAD; ++i) way[i] = w[i + 2];
+                for (int i = 0; i < LEAD; ++i) spread(w[i + 2].off, spots[i]);
             }
             for (int step = begin; step < end; ++step) {
                 const int odd = (step - begin) & 1;
                 lds_sync();                               // V of this step and K of step + LEAD are there, and nobody reads the other buffers any more
-                unsigned ko[PIECES], vo[PIECES];
+                unsigned vo[PIECES];
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i) vo[i] = spots[0][i];
+#pragma unroll
+                for (int n = 0; n + 1 < LEAD; ++n)
+#pragma unroll
+                    for (int i = 0; i < PIECES; ++i) spots[n][i] = spots[n + 1][i];
                 const Lds tiles = lds_of(kbuf + ((odd + LEAD) & 1) * S::TILE, vbuf + odd * S::TILE);
                 // what a step has to do besides, one thing behind each of the first slots
                 auto beside = [&](auto slot) {
@@ -612,14 +620,13 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                     if constexpr (k == 0) store(kbuf + ((odd + LEAD + 1) & 1) * S::TILE, kraw, of_k);
                     if constexpr (k == 1) store(vbuf + (odd ^ 1) * S::TILE, vraw, of_v);
                     if constexpr (k == 2) {
-                        way[LEAD] = resolve(asked);
+                        const Where w = resolve(asked);
 #pragma unroll
-                        for (int i = 0; i < POS; ++i) there[LEAD + 2][i] = way[LEAD].there[i];
+                        for (int i = 0; i < POS; ++i) there[LEAD + 2][i] = w.there[i];
+                        spread(w.off, spots[LEAD - 1]);
                     }
-                    if constexpr (k == 2) spread(way[LEAD].off, ko);
-                    if constexpr (k == 3) spread(way[0].off, vo);
-                    if constexpr (k == 4) read(kbase, ko, kraw);
-                    if constexpr (k == 5) read(vbase, vo, vraw);
+                    if constexpr (k == 3) read(vbase, vo, vraw);
+                    if constexpr (k == 4) read(kbase, spots[LEAD - 1], kraw);
                     if constexpr (k == 5) asked = look(step + LEAD + 3);
                 };
                 auto part = [&](auto b_, f32x16 (&cur)[RB], f32x16 (&next)[RB], Half (&pr)[RB][2], Half (&pn)[RB][2]) {
@@ -655,9 +662,13 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                         rescale(f);
                     }
                 };
-                part(std::integral_constant<int, 0>{}, s1, s0, p0, p1);
-                if constexpr (PB == 2) part(std::integral_constant<int, 1>{}, s0, s1, p1, p0);
-                else {
+                if (idle) {
+                    unrolled<6>(beside);
+                } else if constexpr (PB == 2) {
+                    part(std::integral_constant<int, 0>{}, s1, s0, p0, p1);
+                    part(std::integral_constant<int, 1>{}, s0, s1, p1, p0);
+                } else {
+                    part(std::integral_constant<int, 0>{}, s1, s0, p0, p1);
 #pragma unroll
                     for (int r = 0; r < RB; ++r) {
                         s1[r] = s0[r];
@@ -665,8 +676,6 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
                         p0[r][1] = p1[r][1];
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < LEAD; ++i) way[i] = way[i + 1];
 #pragma unroll
                 for (int i = 0; i < LEAD + 2; ++i)
 #pragma unroll
@@ -687,11 +696,13 @@ __global__ void __launch_bounds__(kChunkThreads, S::RESIDENT) chunk_kernel(Chunk
         const bool any = __any(bad);
         if (lane == 0) flags[wave] = any ? 1 : 0;
         __syncthreads();
-        bad = (flags[0] | flags[1] | flags[2] | flags[3]) != 0;
+        bad = false;
+#pragma unroll
+        for (int w = 0; w < S::WAVES; ++w) bad = bad || flags[w] != 0;
         __syncthreads();
         if (bad) {                                        // once more, with care and no haste
-            float* scratch = reinterpret_cast<float*>(smem + S::TILE) + wave * 32 * 32;      // one step of K is at kbuf, of V at its end
-            char* vt = smem + 3 * S::TILE;
+            float* scratch = reinterpret_cast<float*>(smem + S::TILE) + wave * 32 * 32;      // one step of K before it, of V behind
+            char* vt = smem + S::TILE + S::SCRATCH;
             clear();
             for (int step = begin; step < end; ++step) {
                 const Where w = resolve(look(step));
@@ -883,7 +894,7 @@ auto pick(double rows, F&& body)
         if (rows <= 32) return body(Shape<D, E4M3, 1, 1, 4, 1>{});
         if (rows <= 64) return body(Shape<D, E4M3, 1, 2, 2, 1>{});
         if (rows <= 128) return body(Shape<D, E4M3, 1, 4, 1, 2>{});
-        return body(Shape<D, E4M3, 2, 4, 1, 2>{});
+        return body(Shape<D, E4M3, 1, 8, 1, 2>{});
     } else {
         if (rows <= 64) return body(Shape<D, E4M3, 1, 2, 2, 1>{});
         return body(Shape<D, E4M3, 1, 4, 1, 2>{});
@@ -973,12 +984,12 @@ hipError_t launch_chunk(const moe_kv_cache& c, const moe_block_table& t, const m
         const int64_t slots = (int64_t)ch.T * p.group / S::ROWS + ch.n_seqs, items = slots * p.Hk;
         p.whole = ch.n_seqs > 1024 || items >= 8 * 256 * S::RESIDENT;
         if (p.whole) {
-            hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)items), dim3(kChunkThreads), S::LDS, s, p);
+            hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)items), dim3(S::THREADS), S::LDS, s, p);
             return hipGetLastError();
         }
         const int64_t most = items * (((int64_t)p.cap + S::STEP - 1) / S::STEP);
         const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(most, 256 * S::RESIDENT));
-        hipLaunchKernelGGL((chunk_kernel<S>), dim3(grid), dim3(kChunkThreads), S::LDS, s, p);
+        hipLaunchKernelGGL((chunk_kernel<S>), dim3(grid), dim3(S::THREADS), S::LDS, s, p);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || grid == 1) return e;
         hipLaunchKernelGGL((chunk_join<S::D>), dim3(grid, S::ROWS / 4), dim3(256), 0, s, p, S::ROWS, S::E4M3 ? 11.0f : 0.0f);
