@@ -5,6 +5,14 @@
 
 namespace bmoe {
 
+// The largest of three, in one instruction (fmaxf first makes sure that what it is given is no signalling NaN, an instruction each).  NaN only if all are.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
 // layer_api.hip
 bool off(const void* p, unsigned bytes);                           // not aligned to so many bytes
 bool bad_stride(int64_t stride, int unit);

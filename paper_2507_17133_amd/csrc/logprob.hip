@@ -15,7 +15,8 @@ namespace {
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kEnough = 768;                      // blocks from which longer slices are taken: three for each CU
 constexpr int kCandidates = 512;                  // entries that a block sorts
-constexpr int kJoinMost = 32 * kThreads;          // entries that join_rows chooses from
+constexpr int kLongest = 32;                      // entries of a thread at most: slices of 8192
+constexpr int kJoinEach = 36, kJoinMost = kJoinEach * kThreads;        // entries that join_rows chooses from
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 struct LogprobArgs {
@@ -76,12 +77,40 @@ struct Row {
     __device__ __forceinline__ float of(float x) const { return none ? lse : x == -__builtin_inff() ? x : x - m - log_s; }
 };
 
-__device__ __forceinline__ float wave_max(float v)
+// The value of the lane that is STEP on in a butterfly whose earlier steps have made groups of STEP lanes alike (so a mirrored order serves as well).
+template <int STEP>
+__device__ __forceinline__ int across_bits(int i)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
+    if constexpr (STEP == 1) return __builtin_amdgcn_update_dpp(i, i, 0xB1, 0xF, 0xF, false);          // quad_perm 1 0 3 2
+    else if constexpr (STEP == 2) return __builtin_amdgcn_update_dpp(i, i, 0x4E, 0xF, 0xF, false);     // quad_perm 2 3 0 1
+    else if constexpr (STEP == 4) return __builtin_amdgcn_update_dpp(i, i, 0x141, 0xF, 0xF, false);    // row_half_mirror
+    else if constexpr (STEP == 8) return __builtin_amdgcn_update_dpp(i, i, 0x140, 0xF, 0xF, false);    // row_mirror
+    else {
+        static_assert(STEP == 16 || STEP == 32, "steps of a wave");
+        const auto two = STEP == 16 ? __builtin_amdgcn_permlane16_swap((unsigned)i, (unsigned)i, false, false)
+                                    : __builtin_amdgcn_permlane32_swap((unsigned)i, (unsigned)i, false, false);
+        // one of the two is the lane's own
+        const bool upper = (threadIdx.x & STEP) != 0;
+        return (int)(upper ? two[0] : two[1]);
+    }
 }
+template <int STEP>
+__device__ __forceinline__ float across(float v) { return __int_as_float(across_bits<STEP>(__float_as_int(v))); }
+template <int STEP>
+__device__ __forceinline__ unsigned across(unsigned v) { return (unsigned)across_bits<STEP>((int)v); }
+template <typename T, typename F>
+__device__ __forceinline__ T wave_fold(T v, F&& f)
+{
+    v = f(v, across<1>(v));
+    v = f(v, across<2>(v));
+    v = f(v, across<4>(v));
+    v = f(v, across<8>(v));
+    v = f(v, across<16>(v));
+    return f(v, across<32>(v));
+}
+__device__ __forceinline__ float wave_max(float v) { return wave_fold(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v) { return wave_fold(v, [](T a, T b) { return a + b; }); }
 
 // Whole numbers in the order of floats.
 __device__ __forceinline__ unsigned order_of(float x)
@@ -91,8 +120,9 @@ __device__ __forceinline__ unsigned order_of(float x)
 }
 __device__ __forceinline__ float of_order(unsigned u) { return __uint_as_float(u & 0x80000000u ? u ^ 0x80000000u : ~u); }
 
-// A bound that at least n of the wave's 64 values reach (n <= 64): the n-th largest one, cut off to the upper 16 bits of its order.
-__device__ __forceinline__ float nth_largest(float v, int n)
+// A bound that at least n of the wave's 64 values reach (n <= 64): the n-th largest one, cut off to the upper 16 bits of its order.  (The least of the largest
+// values of n groups costs a third, but ten times as many entries reach it: 67 x 50021, 20 alternatives 119 us instead of 21.)
+__device__ __forceinline__ float reached_by(float v, int n)
 {
     const unsigned key = order_of(v) >> 16;
     unsigned at = 0;
@@ -113,45 +143,43 @@ struct Choice {
 };
 
 // The first n of the block's entries in order, to put(place, entry); a place that has none gets (-infinity, none).  `most`: the thread's largest value;
-// each(f): f(entry) for every entry of the thread.  Entries that reach the n-th largest of a wave's largest values hold the first n; where too many
+// each(bound, f): f(entry) for every entry of the thread that reaches bound.  Entries that reach a bound that n of them are known to reach hold the first n; where too many
 // do, as where all are alike, the entries are taken out one by one.
 template <typename Each, typename Put>
 __device__ __forceinline__ void choose(Choice& c, int n, float most, Each&& each, Put&& put)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const float mine = nth_largest(most, n);
+    const float mine = reached_by(most, n);
     if (lane == 0) c.bound[wave] = mine;
     if (tid == 0) c.found = 0;
     __syncthreads();
     float bound = c.bound[0];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) bound = fmaxf(bound, c.bound[w]);
-    if (most >= bound)
-        each([&](const Entry e) {
-            if (e.x >= bound) {
-                const int at = atomicAdd(&c.found, 1);
-                if (at < kCandidates) c.list[at] = e;
-            }
-        });
+    each(bound, [&](const Entry e) {
+        const int at = atomicAdd(&c.found, 1);
+        if (at < kCandidates) c.list[at] = e;
+    });
     __syncthreads();
     const int found = c.found;
     if (found <= kCandidates) {
-        for (int i = tid; i < max(found, n); i += kThreads) {
-            if (i >= found) {
-                put(i, Entry{-__builtin_inff(), 0x7FFFFFFF});
-                continue;
-            }
-            const Entry e = c.list[i];
+        // an entry's place: how many of the others precede it, counted by four neighbouring lanes
+        for (int i0 = 0; i0 < max(found, n); i0 += kThreads / 4) {
+            const int i = i0 + tid / 4;
+            const Entry e = i < found ? c.list[i] : Entry{-__builtin_inff(), 0x7FFFFFFF};
             int at = 0;
-            for (int j = 0; j < found; ++j) at += precedes(c.list[j], e) ? 1 : 0;
-            if (at < n) put(at, e);
+#pragma unroll 4
+            for (int j = tid & 3; j < found; j += 4) at += precedes(c.list[j], e) ? 1 : 0;
+            at += __shfl_xor(at, 1);
+            at += __shfl_xor(at, 2);
+            if ((tid & 3) == 0 && (i < found ? at : i) < n) put(i < found ? at : i, e);
         }
         return;
     }
     Entry last{__builtin_inff(), -1};
     for (int i = 0; i < n; ++i) {
         Entry top{-__builtin_inff(), 0x7FFFFFFF};
-        each([&](const Entry e) {
+        each(-__builtin_inff(), [&](const Entry e) {
             if (precedes(last, e) && precedes(e, top)) top = e;
         });
 #pragma unroll
@@ -177,6 +205,14 @@ __device__ __forceinline__ float logit(const char* row, int i)
     else return __uint_as_float((unsigned)reinterpret_cast<const uint16_t*>(row)[i] << 16);
 }
 
+template <bool FP32>
+__device__ __forceinline__ Entry given_token(const LogprobArgs& p, const char* row, int t, int k)
+{
+    const int id = p.tokens[(int64_t)t * p.tokens_stride + k];
+    const bool real = (unsigned)id < (unsigned)p.V;
+    return Entry{real ? logit<FP32>(row, id) : 0.0f, real ? id : -1};
+}
+
 // One slice of a row, EACH entries a thread.  HBM bounds it in large calls, beside the vector instructions (about 9 per entry, an exponential counts as 4, and one
 // more for each given token); the launches in small ones.
 template <bool FP32, int EACH>
@@ -184,44 +220,55 @@ __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
 {
     constexpr int PER = FP32 ? 4 : 8, VECS = EACH / PER;          // entries of a 16-byte load
     __shared__ Stats stats[kWaves];
-    __shared__ int counts[kWaves][MOE_MAX_GIVEN];
+    __shared__ int counts[kWaves][MOE_MAX_GIVEN + 1];      // given tokens come in twos
     __shared__ Entry given[MOE_MAX_GIVEN];
     __shared__ Choice choice;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int t = blockIdx.x / p.slices, slice = blockIdx.x - t * p.slices;
     const char* row = p.logits + (int64_t)t * p.stride * (FP32 ? 4 : 2);
     // slices begin on 16-byte lines, the first of them before the row where that begins inside one
-    const int begin = slice * EACH * kThreads - (int)((reinterpret_cast<uintptr_t>(row) & 15) / (FP32 ? 4 : 2));
+    const int begin = slice * EACH * kThreads - (int)((reinterpret_cast<uintptr_t>(row) & 15) / (FP32 ? 4 : 2)), end = begin + EACH * kThreads;
+    const bool inner = begin >= 0 && end <= p.V;
     float x[EACH];
-    uint4 raw[VECS];
-    bool whole[VECS];
+    if (inner) {
+        uint4 raw[VECS];
 #pragma unroll
-    for (int j = 0; j < VECS; ++j) {
-        const int at = begin + (j * kThreads + tid) * PER;
-        whole[j] = at >= 0 && at + PER <= p.V;
-        if (whole[j]) raw[j] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(row + (int64_t)at * (FP32 ? 4 : 2))));
-    }
-    if (tid < p.G) {
-        const int id = p.tokens[(int64_t)t * p.tokens_stride + tid];
-        const bool real = (unsigned)id < (unsigned)p.V;
-        given[tid] = Entry{real ? logit<FP32>(row, id) : 0.0f, real ? id : -1};
-    }
+        for (int j = 0; j < VECS; ++j)
+            raw[j] = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(
+                                                   row + (int64_t)(begin + (j * kThreads + tid) * PER) * (FP32 ? 4 : 2))));
+        if (tid < p.G) given[tid] = given_token<FP32>(p, row, t, tid);
 #pragma unroll
-    for (int j = 0; j < VECS; ++j) {
-        const int at = begin + (j * kThreads + tid) * PER;
-        if (whole[j]) {
+        for (int j = 0; j < VECS; ++j) {
             if constexpr (FP32) {
                 x[4 * j] = __uint_as_float(raw[j].x); x[4 * j + 1] = __uint_as_float(raw[j].y);
                 x[4 * j + 2] = __uint_as_float(raw[j].z); x[4 * j + 3] = __uint_as_float(raw[j].w);
             } else unpack_bf16(raw[j], x + 8 * j);
-        } else {
+        }
+    } else {
+        if (tid < p.G) given[tid] = given_token<FP32>(p, row, t, tid);
 #pragma unroll
-            for (int e = 0; e < PER; ++e) x[PER * j + e] = (unsigned)(at + e) < (unsigned)p.V ? logit<FP32>(row, at + e) : -__builtin_inff();
+        for (int j = 0; j < VECS; ++j) {
+            const int at = begin + (j * kThreads + tid) * PER;
+            if (at >= 0 && at + PER <= p.V) {
+                const uint4 raw = *reinterpret_cast<const uint4*>(row + (int64_t)at * (FP32 ? 4 : 2));
+                if constexpr (FP32) {
+                    x[4 * j] = __uint_as_float(raw.x); x[4 * j + 1] = __uint_as_float(raw.y);
+                    x[4 * j + 2] = __uint_as_float(raw.z); x[4 * j + 3] = __uint_as_float(raw.w);
+                } else unpack_bf16(raw, x + 8 * j);
+            } else {
+#pragma unroll
+                for (int e = 0; e < PER; ++e) x[PER * j + e] = (unsigned)(at + e) < (unsigned)p.V ? logit<FP32>(row, at + e) : -__builtin_inff();
+            }
         }
     }
-    float most = -__builtin_inff();
+    float most = -__builtin_inff(), best[VECS];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) most = fmaxf(most, x[i]);
+    for (int j = 0; j < VECS; ++j) {
+        best[j] = max3(x[PER * j], x[PER * j + 1], x[PER * j + 2]);
+        if constexpr (PER == 8) best[j] = max3(max3(best[j], x[8 * j + 3], x[8 * j + 4]), x[8 * j + 5], x[8 * j + 6]);
+        best[j] = max3(best[j], x[PER * j + PER - 1], -__builtin_inff());       // a number, if only that one
+        most = fmaxf(most, best[j]);
+    }
     Stats a;
     a.m = wave_max(most);
     const float ref = a.m == -__builtin_inff() ? 0.0f : a.m;
@@ -249,41 +296,55 @@ __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
             a.u = __builtin_fmaf(e, fmaxf(d, -1000.0f) * kLog2e, a.u);
         }
     }
-#pragma unroll
-    for (int o = 32; o; o >>= 1) {
-        a.s += __shfl_xor(a.s, o);
-        a.u += __shfl_xor(a.u, o);
-    }
+    a.s = wave_sum(a.s);
+    a.u = wave_sum(a.u);
     if (lane == 0) stats[wave] = a;
     __syncthreads();                              // given tokens, sums
-    for (int k = 0; k < p.G; ++k) {
-        const Entry e = given[k];
-        // at least x_g before its number, above it behind: above the value below x_g, or above x_g
-        const unsigned b = __float_as_uint(e.x + 0.0f);
-        const float below = b == 0 ? -1.401298464324817e-45f : __uint_as_float((int)b < 0 ? b + 1 : b - 1);
-        int n = 0;
+    // ranks, two given tokens at a time (a lane's two counts in one number)
+    const Entry held = p.G ? given[min(lane, p.G - 1)] : Entry{0.0f, -1};
+    for (int k = 0; k < p.G; k += 2) {
+        int n[2] = {0, 0};
+        unsigned mine = 0;
 #pragma unroll
-        for (int j = 0; j < VECS; ++j) {
-            const int at = begin + (j * kThreads + tid) * PER;
-            const bool ahead = at + PER <= e.id, odd = !whole[j] || (!ahead && at <= e.id) || e.x == -__builtin_inff();
-            const float bound = ahead ? below : e.x;
-            if (__any(odd)) {
+        for (int h = 0; h < 2; ++h) {
+            const int from = min(k + h, p.G - 1);
+            const Entry e{__int_as_float(__builtin_amdgcn_readlane(__float_as_int(held.x), from)), __builtin_amdgcn_readlane(held.id, from)};
+            if (inner && (e.id < begin || e.id >= end) && e.x > -__builtin_inff()) {
+                // a slice before its number: what is at least x_g, that is above the value below it; behind: what is above x_g
+                const unsigned b = __float_as_uint(e.x + 0.0f);
+                const float below = b == 0 ? -1.401298464324817e-45f : __uint_as_float((int)b < 0 ? b + 1 : b - 1), bound = e.id >= end ? below : e.x;
+                unsigned m = 0;
 #pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    n += __builtin_popcountll(__ballot((unsigned)(at + i) < (unsigned)p.V && precedes(Entry{x[PER * j + i], at + i}, e)));
+                for (int j = 0; j < VECS; ++j)
+                    if (__any(best[j] > bound)) {         // for a likely token hardly ever
+#pragma unroll
+                        for (int i = 0; i < PER; ++i) m += x[PER * j + i] > bound ? 1 : 0;
+                    }
+                mine |= m << (16 * h);
             } else {
+                int b = begin;
+                asm volatile("" : "+v"(b));               // numbers are made here each time, not kept for all entries
 #pragma unroll
-                for (int i = 0; i < PER; ++i) n += __builtin_popcountll(__ballot(x[PER * j + i] > bound));
+                for (int i = 0; i < EACH; ++i) {
+                    const int id = b + (i / PER * kThreads + tid) * PER + i % PER;
+                    n[h] += __builtin_popcountll(__ballot((unsigned)id < (unsigned)p.V && precedes(Entry{x[i], id}, e)));
+                }
             }
         }
-        if (lane == 0) counts[wave][k] = n;
+        mine = wave_sum(mine);
+        if (lane < 2) counts[wave][k + lane] = (lane ? n[1] + (mine >> 16) : n[0] + (mine & 0xFFFFu));
     }
-    auto each = [&](auto&& f) {
+    auto each = [&](float bound, auto&& f) {
 #pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            const int id = begin + (i / PER * kThreads + tid) * PER + i % PER;
-            if ((unsigned)id < (unsigned)p.V) f(Entry{x[i], id});
-        }
+        for (int j = 0; j < VECS; ++j)
+            {
+#pragma unroll
+                for (int i = PER * j; i < PER * j + PER; ++i)
+                    if (x[i] >= bound) {
+                        const int id = begin + (j * kThreads + tid) * PER + i % PER;
+                        if ((unsigned)id < (unsigned)p.V) f(Entry{x[i], id});
+                    }
+            }
     };
     a = stats[0];
 #pragma unroll
@@ -366,10 +427,10 @@ __global__ void __launch_bounds__(kThreads) join_rows(LogprobArgs p)
     }
     if (p.N)
         choose(choice, p.N, most,
-               [&](auto&& f) {
+               [&](float bound, auto&& f) {
 #pragma unroll
                    for (int i = 0; i < EACH; ++i)
-                       if (entry[i].id != 0x7FFFFFFF) f(entry[i]);
+                       if (entry[i].x >= bound && entry[i].id != 0x7FFFFFFF) f(entry[i]);
                },
                [&](int i, const Entry e) {
                    if (p.top_id) p.top_id[(int64_t)t * p.N + i] = r.none ? -1 : e.id;
@@ -377,12 +438,14 @@ __global__ void __launch_bounds__(kThreads) join_rows(LogprobArgs p)
                });
 }
 
-int slices_of(int V, int each) { return ceil_div(V + 7, each * kThreads); }      // up to 7 places before the row
+constexpr int slices_of(int V, int each, int ahead = 7) { return (V + ahead + each * kThreads - 1) / (each * kThreads); }      // up to 7 places before a row that begins inside a line
+
+static_assert(slices_of(MOE_MAX_ENTRIES, kLongest) * MOE_MAX_TOP <= kJoinMost, "the best of all slices of a row");
 
 // Entries of a thread: the longest slices that still make enough blocks, or the shortest ones.
 int entries_each(int64_t T, int V, int n_top)
 {
-    int each = 64;
+    int each = kLongest;
     while (each > 8 && T * slices_of(V, each) < kEnough && (int64_t)slices_of(V, each / 2) * n_top <= kJoinMost) each /= 2;
     return each;
 }
@@ -394,13 +457,12 @@ hipError_t go(const LogprobArgs& p, int each, hipStream_t s)
     switch (each) {
         case 8: hipLaunchKernelGGL((slice_kernel<FP32, 8>), grid, threads, 0, s, p); break;
         case 16: hipLaunchKernelGGL((slice_kernel<FP32, 16>), grid, threads, 0, s, p); break;
-        case 32: hipLaunchKernelGGL((slice_kernel<FP32, 32>), grid, threads, 0, s, p); break;
-        default: hipLaunchKernelGGL((slice_kernel<FP32, 64>), grid, threads, 0, s, p); break;
+        default: hipLaunchKernelGGL((slice_kernel<FP32, kLongest>), grid, threads, 0, s, p); break;
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.slices == 1) return e;
     if (p.slices * p.N <= 4 * kThreads) hipLaunchKernelGGL((join_rows<FP32, 4>), dim3(p.T), threads, 0, s, p);
-    else hipLaunchKernelGGL((join_rows<FP32, 32>), dim3(p.T), threads, 0, s, p);
+    else hipLaunchKernelGGL((join_rows<FP32, kJoinEach>), dim3(p.T), threads, 0, s, p);
     return hipGetLastError();
 }
 
@@ -409,7 +471,7 @@ hipError_t go(const LogprobArgs& p, int each, hipStream_t s)
 size_t logprob_workspace_bytes(int64_t T, int V, int n_given, int n_top)
 {
     // fewer rows may be cut into shorter slices, but then into fewer than twice kEnough of them
-    const int64_t parts = std::max(T * slices_of(V, 64), std::min<int64_t>(T * slices_of(V, 8), 2 * kEnough));
+    const int64_t parts = std::max(T * slices_of(V, kLongest), std::min<int64_t>(T * slices_of(V, 8), 2 * kEnough));
     return align_up(parts * sizeof(float4), 256) + align_up(parts * sizeof(int) * n_given, 256) + align_up(parts * sizeof(float2) * n_top, 256);
 }
 
@@ -423,8 +485,9 @@ hipError_t launch_logprobs(const moe_logprob_args& a, void* ws, hipStream_t s)
     p.T = a.T; p.V = a.V;
     p.G = a.logprob || a.rank ? a.n_given : 0;
     p.N = a.top_id || a.top_logprob ? a.n_top : 0;
-    const int each = entries_each(a.T, a.V, p.N);
-    p.slices = slices_of(a.V, each);
+    const int each = entries_each(a.T, a.V, p.N), size = a.type == MOE_LOGITS_FP32 ? 4 : 2;
+    const bool aligned = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && (a.T == 1 || a.stride * size % 16 == 0);
+    p.slices = slices_of(a.V, each, aligned ? 0 : 16 / size - 1);
     const size_t parts = (size_t)p.T * p.slices;
     p.stats = static_cast<float4*>(ws);
     p.before = reinterpret_cast<int*>(static_cast<char*>(ws) + align_up(parts * sizeof(float4), 256));
