@@ -29,26 +29,29 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kChunkShares = 512;                 // shares of the line of steps at most
+constexpr int kBetween = 5;                         // what an item costs besides its steps, in steps
+constexpr int kMostShared = 1024;                 // sequences of a call whose steps are dealt out in shares
 constexpr float kSlack = 4.0f;                    // how far (in powers of two) scores may exceed the maximum that they refer to
 constexpr int kMostContext = 0x7FFE0000;          // so that positions of new tokens stay in 32 bits
 
-// Rows per block 32 * RB * WM: WM waves with RB blocks of 32 rows each; WK waves share the positions of a step, PB blocks of 32 each.
-template <int D_, bool E4M3_, int RB_, int WM_, int WK_, int PB_>
+// Rows of a block 32 * WM, one of WM waves each; WK waves share the positions of a step, PB blocks of 32 each.
+template <int D_, bool E4M3_, int WM_, int WK_, int PB_, int DEPTH_>
 struct Shape {
-    static constexpr int D = D_, RB = RB_, WM = WM_, WK = WK_, PB = PB_;
+    static constexpr int D = D_, WM = WM_, WK = WK_, PB = PB_, DEPTH = DEPTH_;       // DEPTH: steps on their way to registers
     static constexpr bool E4M3 = E4M3_;
     static constexpr int WAVES = WM * WK, THREADS = 64 * WAVES;
-    static_assert(WAVES == 4 || WAVES == 8, "waves of a block");
-    static constexpr int ROWS = 32 * RB * WM, STEP = 32 * PB * WK;
+    static_assert(WAVES == 2 || WAVES == 4 || WAVES == 8, "waves of a block");
+    static constexpr int ROWS = 32 * WM, STEP = 32 * PB * WK;
     static constexpr int N64 = D / 64, N32 = D % 64 / 32;                     // panels of 64 columns, and one of 32
     static constexpr int TILE = STEP * D * 2;                                 // bytes of K (of V) of a step in LDS
     static constexpr int KS = D / 16, VS = D / 32;                            // products along D, blocks of 32 columns of V
     static constexpr int LEAD = 2 / PB;                                       // steps that K is ahead of V
     static constexpr int AHEAD = 2;                                           // slots that LDS reads are ahead of the products
     static constexpr int SCRATCH = WAVES * 32 * 32 * 4;                       // probabilities of the careful second product
-    static constexpr int LDS = 4 * TILE > 2 * TILE + SCRATCH ? 4 * TILE : 2 * TILE + SCRATCH;                                      // two steps of K, two of V
-    static_assert(PB <= 2 && (WK - 1) * WM * 32 * RB * (D + 4) * 4 <= LDS, "what else LDS holds");
-    static constexpr int RESIDENT = WAVES == 4 && LDS <= 80 * 1024 && RB * D <= 128 ? 2 : 1;   // blocks of a CU
+    static constexpr int JOIN = (WK - 1) * WM * 32 * (D + 4) * 4;        // parts of waves that share rows
+    static constexpr int FLAGS = std::max({4 * TILE, 2 * TILE + SCRATCH, JOIN}), LDS = FLAGS + 64;       // two steps of K, two of V, or one of each and the scratch, or the parts
+    static constexpr int RESIDENT = WAVES <= 4 && DEPTH == 1 && LDS <= 80 * 1024 && D <= 128 ? 2 : 1;       // blocks of a CU
+    static_assert(PB <= 2 && LDS <= 160 * 1024 && LDS >= kMostShared * 4 + 64, "LDS");
     // floats of a part: [ROWS][D] O, [ROWS] m, [ROWS] l
     static constexpr int64_t PART = (int64_t)ROWS * (D + 2);
 };
@@ -108,23 +111,31 @@ struct Span {
 
 __device__ __forceinline__ int table_row(const ChunkArgs& p, int b) { return p.row_of ? p.row_of[b] : b; }
 
-// Steps of a sequence's items of one key head.
+// Tiles of rows are numbered through: sequence b's have the places from floor(first[b] * group / ROWS) + b on, which is room enough for them; some places
+// in between have none.
 template <class S>
-__device__ __forceinline__ int64_t steps_of(const ChunkArgs& p, int b)
+__device__ __forceinline__ int place_of(const ChunkArgs& p, int b) { return (int)((int64_t)min(max(p.first[b], 0), p.T) * p.group / S::ROWS) + b; }
+
+// Steps of a tile; 0 where there is none.
+template <class S>
+__device__ __forceinline__ int steps_of(const ChunkArgs& p, int b, int tile)
 {
     const Seq s(p, b);
-    const bool there = (unsigned)table_row(p, b) < (unsigned)p.n_rows;
-    const int tiles = s.row_tiles(p, S::ROWS);
-    if (tiles == 0) return 0;
-    if (p.seen) return (int64_t)tiles * Span(p, s, 0, S::ROWS, there).template steps<S::STEP>();
-    int64_t n = 0;
-    for (int i = 0; i < tiles; ++i) n += Span(p, s, i, S::ROWS, there).template steps<S::STEP>();
-    return n;
+    if (tile >= s.row_tiles(p, S::ROWS)) return 0;
+    return Span(p, s, tile, S::ROWS, (unsigned)table_row(p, b) < (unsigned)p.n_rows).template steps<S::STEP>();
 }
 
-// Where a block begins in the line of steps, and how many it has.
+// Length of an item of the tile in the line that shares are cut from: its steps, behind kBetween that stand for what it costs besides.
+template <class S>
+__device__ __forceinline__ int units_of(const ChunkArgs& p, int b, int tile)
+{
+    const int n = steps_of<S>(p, b, tile);
+    return n > 0 ? n + kBetween : 0;
+}
+
+// Where a block begins in the line, and how much of it it has.
 struct Begin {
-    int b, tile, hk, step;
+    int b, tile, hk, unit;                        // unit: of the item
     int64_t at, end, per;
 };
 
@@ -140,15 +151,40 @@ __device__ __forceinline__ int64_t sum_before(int64_t v, int lane, int64_t& tota
     return x - v;
 }
 
+// The share's first step: every thread adds up the steps of its part of the places.  LDS: [n_seqs] places, then 8 numbers of 64 bits behind kMostShared of them.
 template <class S>
-__device__ __forceinline__ bool find_share(const ChunkArgs& p, int64_t* lds, Begin& o)
+__device__ __forceinline__ bool find_share(const ChunkArgs& p, char* smem, Begin& o)
 {
+    int* place = reinterpret_cast<int*>(smem);
+    int64_t* lds = reinterpret_cast<int64_t*>(smem + kMostShared * sizeof(int));
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int each = (p.n_seqs + S::THREADS - 1) / S::THREADS, b0 = min(p.n_seqs, tid * each), b1 = min(p.n_seqs, b0 + each);
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) mine += steps_of<S>(p, b) * p.Hk;
+    for (int b = tid; b < p.n_seqs; b += S::THREADS) place[b] = place_of<S>(p, b);
+    __syncthreads();
+    const int slots = (int)((int64_t)p.T * p.group / S::ROWS) + p.n_seqs, each = (slots + S::THREADS - 1) / S::THREADS;
+    const int u0 = min(slots, tid * each), u1 = min(slots, u0 + each);
+    int b0 = 0;                                   // the last sequence whose place is not beyond u0
+    for (int n = p.n_seqs; n > 1;) {
+        const int half = n / 2;
+        if (place[b0 + half] <= u0) {
+            b0 += half;
+            n -= half;
+        } else n = half;
+    }
+    // f(place in the order, sequence, tile) for the thread's places
+    auto mine = [&](auto&& f) {
+        int b = b0;
+        for (int u = u0; u < u1; ++u) {
+            while (b + 1 < p.n_seqs && place[b + 1] <= u) ++b;
+            if (u >= place[b] && f(b, u - place[b])) return;
+        }
+    };
+    int64_t sum = 0;
+    mine([&](int b, int tile) {
+        sum += units_of<S>(p, b, tile) * p.Hk;
+        return false;
+    });
     int64_t total;
-    int64_t before = sum_before(mine, lane, total);
+    int64_t before = sum_before(sum, lane, total);
     if (lane == 0) lds[wave] = total;
     __syncthreads();
     int64_t all = 0;
@@ -157,52 +193,46 @@ __device__ __forceinline__ bool find_share(const ChunkArgs& p, int64_t* lds, Beg
         if (w < wave) before += lds[w];
         all += lds[w];
     }
+    __syncthreads();
     o.per = (all + gridDim.x - 1) / gridDim.x;
     o.at = min(all, o.per * (int64_t)blockIdx.x);
     o.end = min(all, o.at + o.per);
     if (o.at >= o.end) return false;
-    // the one thread whose sequences hold the first step looks for it
-    if (before <= o.at && o.at < before + mine) {
-        int b = b0;
-        for (;; ++b) {
-            const int64_t n = steps_of<S>(p, b) * p.Hk;
-            if (o.at < before + n) break;
-            before += n;
-        }
-        const Seq s(p, b);
-        const bool there = (unsigned)table_row(p, b) < (unsigned)p.n_rows;
-        int tile = 0, n = 0;
-        for (;; ++tile) {
-            n = Span(p, s, tile, S::ROWS, there).template steps<S::STEP>();
-            if (o.at < before + (int64_t)n * p.Hk) break;
-            before += (int64_t)n * p.Hk;
-        }
-        lds[S::WAVES] = b;
-        lds[S::WAVES + 1] = tile;
-        lds[S::WAVES + 2] = (o.at - before) / n;
-        lds[S::WAVES + 3] = (o.at - before) % n;
-    }
+    // the one thread whose tiles hold the first step looks for it
+    if (before <= o.at && o.at < before + sum)
+        mine([&](int b, int tile) {
+            const int n = units_of<S>(p, b, tile);
+            if (o.at >= before + (int64_t)n * p.Hk) {
+                before += (int64_t)n * p.Hk;
+                return false;
+            }
+            int hk = 0;
+            for (; o.at >= before + n; ++hk) before += n;
+            lds[0] = b;
+            lds[1] = tile;
+            lds[2] = hk;
+            lds[3] = o.at - before;
+            return true;
+        });
     __syncthreads();
-    o.b = __builtin_amdgcn_readfirstlane((int)lds[S::WAVES]);
-    o.tile = __builtin_amdgcn_readfirstlane((int)lds[S::WAVES + 1]);
-    o.hk = __builtin_amdgcn_readfirstlane((int)lds[S::WAVES + 2]);
-    o.step = __builtin_amdgcn_readfirstlane((int)lds[S::WAVES + 3]);
+    o.b = __builtin_amdgcn_readfirstlane((int)lds[0]);
+    o.tile = __builtin_amdgcn_readfirstlane((int)lds[1]);
+    o.hk = __builtin_amdgcn_readfirstlane((int)lds[2]);
+    o.unit = __builtin_amdgcn_readfirstlane((int)lds[3]);
     __syncthreads();
     return true;
 }
 
-// One block for each item.  Sequence b's tiles have the places from floor(first[b] * group / ROWS) + b on, which is room enough for them; the blocks
-// in between have none.  Late tiles of a chunk, which see the most, come first.
+// One block for each place and key head.  Late tiles of a chunk, which see the most, come first.
 template <class S>
 __device__ __forceinline__ bool find_item(const ChunkArgs& p, Begin& o)
 {
     const int lane = threadIdx.x & 63, slots = gridDim.x / p.Hk, u = slots - 1 - (int)(blockIdx.x / p.Hk);
-    auto place = [&](int b) { return (int)((int64_t)min(max(p.first[b], 0), p.T) * p.group / S::ROWS) + b; };
     // the last sequence whose place is not beyond u, 64 of a stride at a time
     int lo = 0, n = p.n_seqs;
     while (n > 1) {
         const int stride = (n + 63) / 64, b = lo + lane * stride;
-        const bool is = lane * stride < n && place(b) <= u;
+        const bool is = lane * stride < n && place_of<S>(p, b) <= u;
         const uint64_t m = __ballot(is);
         const int k = m ? 63 - __builtin_clzll(m) : 0;
         lo = __builtin_amdgcn_readfirstlane(lo + k * stride);
@@ -210,9 +240,9 @@ __device__ __forceinline__ bool find_item(const ChunkArgs& p, Begin& o)
     }
     o.b = lo;
     const Seq s(p, lo);
-    o.tile = u - place(lo);
+    o.tile = u - place_of<S>(p, lo);
     o.hk = blockIdx.x % p.Hk;
-    o.step = 0;
+    o.unit = 0;
     return o.tile >= 0 && o.tile < s.row_tiles(p, S::ROWS);
 }
 
@@ -253,9 +283,9 @@ __device__ __forceinline__ void unrolled(F&& body)
 __device__ __forceinline__ unsigned below(int n) { return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1; }
 
 template <class S>
-__global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArgs p)
+__global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 1) chunk_kernel(ChunkArgs p)
 {
-    constexpr int D = S::D, RB = S::RB, WM = S::WM, WK = S::WK, PB = S::PB, STEP = S::STEP, POS = STEP / 64;
+    constexpr int D = S::D, WM = S::WM, WK = S::WK, PB = S::PB, STEP = S::STEP, POS = STEP / 64;
     constexpr bool E4M3 = S::E4M3;
     using Half = pv8<E4M3>;
     // e4m3: probabilities as fp16, exactly enough for V's 4 bits; 2^kUp of them, so that small ones are not lost below fp16's range
@@ -264,14 +294,13 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 31, g = lane >> 5, wm = wave % WM, wk = wave / WM;
     char *const kbuf = smem, *const vbuf = smem + 2 * S::TILE;
-    int64_t* found = reinterpret_cast<int64_t*>(smem);    // while no step is there
 
     Begin at;
     if (p.whole) {
         if (!find_item<S>(p, at)) return;
     } else {
         if (tid == 0) p.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
-        if (!find_share<S>(p, found, at)) return;
+        if (!find_share<S>(p, smem, at)) return;
     }
 
     for (;;) {
@@ -280,8 +309,26 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
         const int row = table_row(p, at.b);
         const Span span(p, seq, at.tile, S::ROWS, (unsigned)row < (unsigned)p.n_rows);
         const int32_t* pages = p.pages + (span.n > 0 ? (int64_t)row * p.row_stride : 0);          // where there is nothing to see, any row will do
-        const int steps = span.template steps<STEP>(), begin = at.step;
-        const int end = p.whole ? steps : (int)min((int64_t)steps, at.step + (at.end - at.at));
+        const int steps = span.template steps<STEP>(), begin = p.whole ? 0 : max(at.unit - kBetween, 0);
+        const int ends_at = p.whole ? steps + kBetween : (int)min((int64_t)steps + kBetween, at.unit + (at.end - at.at)), end = max(ends_at - kBetween, 0);
+        // on by so much of the line; false at the share's end
+        auto advance = [&](int units) {
+            at.at += units;
+            if (at.at >= at.end) return false;
+            at.unit = 0;
+            if (++at.hk < p.Hk) return true;
+            at.hk = 0;
+            ++at.tile;
+            while (at.tile >= Seq(p, at.b).row_tiles(p, S::ROWS)) {   // ends: the share's steps belong to sequences that have some
+                at.tile = 0;
+                ++at.b;
+            }
+            return true;
+        };
+        if (begin >= end) {                               // no step of it
+            if (!advance(ends_at - at.unit)) return;
+            continue;
+        }
         const int n_rows = seq.n * p.group;
         const char *kbase = p.kc + (int64_t)at.hk * p.head_stride, *vbase = p.vc + (int64_t)at.hk * p.head_stride;
         float to_log2 = p.scale * 1.4426950408889634f * (E4M3 ? p.k_scale[at.hk] : 1.0f);
@@ -293,23 +340,19 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
             bool real;
             int token, head, nth;                         // nth: the token's number in the sequence
         };
-        auto row_of = [&](int r) {
-            const int i = at.tile * S::ROWS + (wm * RB + r) * 32 + c, j = min(i, n_rows - 1) / p.group;
+        auto row_of = [&]() {
+            const int i = at.tile * S::ROWS + wm * 32 + c, j = min(i, n_rows - 1) / p.group;
             return Row{i < n_rows, seq.t0 + j, at.hk * p.group + (i < n_rows ? i - j * p.group : 0), j};
         };
-        const bool idle = at.tile * S::ROWS + wm * RB * 32 >= n_rows;         // a wave without rows only brings K and V
-        int last[RB], from[RB];
-        bf16x8 q[RB][S::KS];
-#pragma unroll
-        for (int r = 0; r < RB; ++r) {
-            const Row o = row_of(r);
-            int pos = seq.context + o.nth;
-            if (p.positions) pos = max(seq.context, p.positions[o.token]);
-            last[r] = p.seen ? seq.context - 1 : pos;
-            from[r] = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
-            if (!o.real) {                                // whatever it sees, nobody looks at it
-                last[r] = 0x7FFFFFFF;
-                from[r] = 0;
+        const bool idle = at.tile * S::ROWS + wm * 32 >= n_rows;         // a wave without rows only brings K and V
+        int last = 0x7FFFFFFF, from = 0;                  // of a lane without a row: nobody looks at what it sees
+        bf16x8 q[S::KS];
+        {
+            const Row o = row_of();
+            if (o.real) {
+                const int pos = p.positions ? max(seq.context, p.positions[o.token]) : seq.context + o.nth;
+                last = p.seen ? seq.context - 1 : pos;
+                from = p.window > 0 ? max(pos - p.window + 1, 0) : 0;
             }
             const bf16_t* src = p.q + (int64_t)o.token * p.q_stride + (int64_t)o.head * D;
 #pragma unroll
@@ -317,8 +360,8 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
                 uint4 v = make_uint4(0, 0, 0, 0);
                 if (o.real) v = *reinterpret_cast<const uint4*>(src + 16 * k + 8 * g);
                 v.x ^= flip; v.y ^= flip; v.z ^= flip; v.w ^= flip;
-                q[r][k] = __builtin_bit_cast(bf16x8, v);
-                if constexpr (S::WAVES == 4 && S::RESIDENT == 1) asm volatile("" : "+a"(q[r][k]));      // operands may stay in accumulation registers
+                q[k] = __builtin_bit_cast(bf16x8, v);
+                if constexpr (S::RESIDENT * S::WAVES < 8) asm volatile("" : "+a"(q[k]));     // operands may stay in accumulation registers
             }
         }
 
@@ -327,8 +370,8 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
         const int kat = rk * 128 + ((g ^ turn64(c)) << 4), kat32 = S::N64 * STEP * 128 + rk * 64 + ((g ^ turn32(c)) << 4);
         const int vat = rv * 128 + ((piece ^ turn64(sub)) << 4) + in, vat32 = S::N64 * STEP * 128 + rv * 64 + ((piece ^ turn32(sub)) << 4) + in;
 
-        f32x16 acc[RB][S::VS];
-        float m[RB], l[RB];
+        f32x16 acc[S::VS];
+        float m, l;
 
         // ---------------- where a step's positions are: lane i has those of positions i, 64 + i, ...  Places behind the last position are read from that one.
         struct Look {
@@ -414,91 +457,68 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
         constexpr std::false_type of_k{};
         constexpr std::true_type of_v{};
         // ---------------- what each row sees of it: a bit for each of the 32 positions
-        auto cover = [&](int step, int b, const uint64_t (&there)[POS], f32x16 (&s)[RB]) {
+        auto cover = [&](int step, int b, const uint64_t (&there)[POS], f32x16& s) {
             const int in_step = (wk * PB + b) * 32, vb = step * STEP + in_step;
             const uint64_t word = POS > 1 && in_step >= 64 ? there[POS - 1] : there[0];
             const unsigned is = (unsigned)(word >> (in_step & 63));
             // the first k of them are among the sinks, at positions vb on; the others at positions at on
             const int k = min(max(span.sinks - vb, 0), 32), at = vb - span.sinks + span.lo;
-            bool all = is == 0xFFFFFFFFu && k == 0;
-#pragma unroll
-            for (int r = 0; r < RB; ++r) all = all && at + 31 <= last[r] && at >= from[r];
-            if (__all(all)) return;
+            if (__all(is == 0xFFFFFFFFu && k == 0 && at + 31 <= last && at >= from)) return;
             const unsigned sink = below(k);
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                unsigned on = below(last[r] - at + 1) & (~below(from[r] - at) | below(p.sinks - at));
-                const int nth = at - seq.context;         // of the new tokens, the one at position `at`
-                if (p.seen && nth > -32) {
-                    const uint32_t* w = p.seen + (int64_t)row_of(r).token * p.seen_stride;
-                    const int i = nth >> 5;
-                    const uint64_t lo = i >= 0 && i < p.words ? w[i] : 0, hi = i + 1 < p.words ? w[i + 1] : 0;
-                    on |= (unsigned)((lo | hi << 32) >> (nth & 31)) & ~below(-nth);
-                }
-                on = ((sink & below(last[r] - vb + 1)) | (~sink & on)) & is;
-                on >>= 4 * g;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (!(on >> (8 * (i / 4) + i % 4) & 1)) s[r][i] = -__builtin_inff();
+            unsigned on = below(last - at + 1) & (~below(from - at) | below(p.sinks - at));
+            const int nth = at - seq.context;         // of the new tokens, the one at position `at`
+            if (p.seen && nth > -32) {
+                const uint32_t* w = p.seen + (int64_t)row_of().token * p.seen_stride;
+                const int i = nth >> 5;
+                const uint64_t lo = i >= 0 && i < p.words ? w[i] : 0, hi = i + 1 < p.words ? w[i + 1] : 0;
+                on |= (unsigned)((lo | hi << 32) >> (nth & 31)) & ~below(-nth);
             }
+            on = ((sink & below(last - vb + 1)) | (~sink & on)) & is;
+            on >>= 4 * g;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (!(on >> (8 * (i / 4) + i % 4) & 1)) s[i] = -__builtin_inff();
         };
         // ---------------- probabilities in place of scores, in three steps: the maximum, what it changes, the exponentials.
-        auto largest = [&](const f32x16 (&s)[RB], float (&top)[RB], int i) {
-            const int r = i / 16;
-            top[r] = i % 16 ? fmaxf(top[r], s[r][i % 16]) : s[r][0];
-        };
+        auto largest = [&](const f32x16& s, float& top, int i) { top = i ? fmaxf(top, s[i]) : s[0]; };
         // f: what earlier sums are to be multiplied by.  Returns whether any of them are; no branch, so that products go on around it.
-        auto refer = [&](float (&top)[RB], float (&f)[RB], float (&ref)[RB]) {
-            bool moves = false;
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(top[r]), __float_as_uint(top[r]), false, false);
-                top[r] = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * to_log2;
-                moves = moves || top[r] > m[r] + kSlack;
-            }
-            moves = __any(moves);
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                const float m_new = moves ? fmaxf(m[r], top[r]) : m[r];
-                f[r] = m[r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[r] - m_new);
-                l[r] *= f[r];
-                m[r] = m_new;
-                ref[r] = (m_new == -__builtin_inff() ? 0.0f : m_new) - kUp;
-            }
+        auto refer = [&](float& top, float& f, float& ref) {
+            const auto two = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+            top = fmaxf(__uint_as_float(two[0]), __uint_as_float(two[1])) * to_log2;
+            const bool moves = __any(top > m + kSlack);
+            const float m_new = moves ? fmaxf(m, top) : m;
+            f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - m_new);
+            l *= f;
+            m = m_new;
+            ref = (m_new == -__builtin_inff() ? 0.0f : m_new) - kUp;
             return moves;
         };
-        auto exponent = [&](f32x16 (&s)[RB], const float (&ref)[RB], int i) {
-            const int r = i / 16;
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r][i % 16], to_log2, -ref[r]));
-            l[r] += e;
-            s[r][i % 16] = e;
+        auto exponent = [&](f32x16& s, float ref, int i) {
+            s[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i], to_log2, -ref));
+            l += s[i];
         };
-        auto exponents = [&](f32x16 (&s)[RB], float (&f)[RB]) {
-            float top[RB], ref[RB];
+        auto exponents = [&](f32x16& s, float& f) {
+            float top, ref;
 #pragma unroll
-            for (int i = 0; i < 16 * RB; ++i) largest(s, top, i);
+            for (int i = 0; i < 16; ++i) largest(s, top, i);
             const bool moves = refer(top, f, ref);
 #pragma unroll
-            for (int i = 0; i < 16 * RB; ++i) exponent(s, ref, i);
+            for (int i = 0; i < 16; ++i) exponent(s, ref, i);
             return moves;
         };
-        auto rescale = [&](const float (&f)[RB]) {
+        auto rescale = [&](float f) {
 #pragma unroll
-            for (int r = 0; r < RB; ++r)
+            for (int j = 0; j < S::VS; ++j)
 #pragma unroll
-                for (int j = 0; j < S::VS; ++j)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[r][j][i] *= f[r];
+                for (int i = 0; i < 16; ++i) acc[j][i] *= f;
         };
-        auto rounded = [&](const f32x16 (&s)[RB], Half (&pr)[RB][2]) {
+        auto rounded = [&](const f32x16& s, Half (&pr)[2]) {
 #pragma unroll
-            for (int r = 0; r < RB; ++r)
+            for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) pr[r][t][i] = s[r][8 * t + i];
+                for (int i = 0; i < 8; ++i) pr[t][i] = s[8 * t + i];
         };
-        // ---------------- a block's products in slots of RB: KS of S = K Q^T, then 2 * VS of O^T += V^T P^T; their operand from K or V
+        // ---------------- a block's products, in slots: KS of S = K Q^T, then 2 * VS of O^T += V^T P^T; their operand from K or V
         union Operand {
             bf16x8 k;
             s16x4 h[2];
@@ -524,17 +544,14 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
             const unsigned k = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)kt, v = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)vt;
             return Lds{k + kat, k + kat32, v + vat, v + vat32};
         };
-        auto product = [&](auto slot, const Operand& a, f32x16 (&s)[RB], const Half (&pr)[RB][2]) {
+        auto product = [&](auto slot, const Operand& a, f32x16& s, const Half (&pr)[2]) {
             constexpr int k = decltype(slot)::value, t = (k - S::KS) / S::VS, j = (k - S::KS) % S::VS;
-#pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                if constexpr (k < S::KS) s[r] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.k, q[r][k], k == 0 ? f32x16{} : s[r], 0, 0, 0);
-                else if constexpr (E4M3) acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
-                else acc[r][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[r][t], acc[r][j], 0, 0, 0);
-            }
+            if constexpr (k < S::KS) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.k, q[k], k == 0 ? f32x16{} : s, 0, 0, 0);
+            else if constexpr (E4M3) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[t], acc[j], 0, 0, 0);
+            else acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[t], acc[j], 0, 0, 0);
         };
-        auto scores = [&](const Lds& o, int b, f32x16 (&s)[RB]) {
-            const Half none[RB][2] = {};
+        auto scores = [&](const Lds& o, int b, f32x16& s) {
+            const Half none[2] = {};
             unrolled<S::KS>([&](auto k) {
                 Operand a;
                 operand(k, o, b, a);
@@ -547,64 +564,65 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
             lds_barrier();
         };
         auto clear = [&]() {
+            m = -__builtin_inff();
+            l = 0.0f;
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                m[r] = -__builtin_inff();
-                l[r] = 0.0f;
-#pragma unroll
-                for (int j = 0; j < S::VS; ++j) acc[r][j] = f32x16{};
-            }
+            for (int j = 0; j < S::VS; ++j) acc[j] = f32x16{};
         };
 
         // ---------------- the pipeline: block n of a wave is weighed while n + 1 has its exponentials taken and n + 2 its scores.  In step j V of step j and K
         // of step j + LEAD are in LDS, the next ones in registers, those after them on their way to there.
         {
-            constexpr int LEAD = S::LEAD;
-            Raw kraw, vraw;
-            unsigned spots[LEAD][PIECES];                 // where the thread reads, of steps j + 2 .. j + LEAD + 1
-            uint64_t there[LEAD + 3][POS];                // of steps j ..
+            constexpr int LEAD = S::LEAD, DEPTH = S::DEPTH;
+            Raw kraw[DEPTH], vraw[DEPTH];
+            unsigned spots[LEAD][PIECES];                 // where the thread reads, of steps j + DEPTH + 1 .. j + DEPTH + LEAD
+            uint64_t there[LEAD + DEPTH + 2][POS];        // of steps j ..
             Look asked;
-            f32x16 s0[RB], s1[RB];
-            Half p0[RB][2], p1[RB][2];
-            float f[RB];
+            f32x16 s0, s1;
+            Half p0[2], p1[2];
+            float f;
             {
-                Look first[LEAD + 2];
-                Where w[LEAD + 2];
-                Raw kr[LEAD];
+                constexpr int N = LEAD + DEPTH + 1;
+                Look first[N];
+                Where w[N];
+                Raw kr[LEAD + 1], vr;
 #pragma unroll
-                for (int i = 0; i < LEAD + 2; ++i) first[i] = look(begin + i);
-                asked = look(begin + LEAD + 2);
+                for (int i = 0; i < N; ++i) first[i] = look(begin + i);
+                asked = look(begin + N);
 #pragma unroll
-                for (int i = 0; i < LEAD + 2; ++i) {
+                for (int i = 0; i < N; ++i) {
                     w[i] = resolve(first[i]);
 #pragma unroll
                     for (int k = 0; k < POS; ++k) there[i][k] = w[i].there[k];
-                    if (i < LEAD) fetch(kbase, w[i].off, kr[i]);
-                    if (i == 0) fetch(vbase, w[0].off, vraw);
+                    if (i <= LEAD) fetch(kbase, w[i].off, kr[i]);
+                    if (i == 0) fetch(vbase, w[0].off, vr);
                 }
-                fetch(kbase, w[LEAD].off, kraw);
 #pragma unroll
-                for (int i = 0; i < LEAD; ++i) store(kbuf + i * S::TILE, kr[i], of_k);
-                store(vbuf, vraw, of_v);
-                if constexpr (LEAD == 1) store(kbuf + S::TILE, kraw, of_k);
-                __syncthreads();
+                for (int i = 0; i < DEPTH; ++i) {
+                    fetch(kbase, w[LEAD + 1 + i].off, kraw[i]);
+                    fetch(vbase, w[1 + i].off, vraw[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) store(kbuf + i * S::TILE, kr[i], of_k);
+                store(vbuf, vr, of_v);
+                lds_sync();
                 clear();
                 scores(lds_of(kbuf, vbuf), 0, s0);
                 scores(lds_of(LEAD == 1 ? kbuf : kbuf + S::TILE, vbuf), LEAD == 1 ? 1 : 0, s1);
                 if constexpr (LEAD == 2) {
-                    __syncthreads();
-                    store(kbuf, kraw, of_k);
+                    lds_sync();
+                    store(kbuf, kr[2], of_k);
                 }
-                fetch(kbase, w[LEAD + 1].off, kraw);
-                fetch(vbase, w[1].off, vraw);
                 cover(begin, 0, there[0], s0);
                 exponents(s0, f);
                 rounded(s0, p0);
 #pragma unroll
-                for (int i = 0; i < LEAD; ++i) spread(w[i + 2].off, spots[i]);
+                for (int i = 0; i < LEAD; ++i) spread(w[1 + DEPTH + i].off, spots[i]);
             }
-            for (int step = begin; step < end; ++step) {
-                const int odd = (step - begin) & 1;
+            for (int step0 = begin; step0 < end; step0 += DEPTH) unrolled<DEPTH>([&](auto turn) {
+                constexpr int set = decltype(turn)::value;
+                const int step = step0 + set, odd = (step - begin) & 1;
+                if (set > 0 && step >= end) return;
                 lds_sync();                               // V of this step and K of step + LEAD are there, and nobody reads the other buffers any more
                 unsigned vo[PIECES];
 #pragma unroll
@@ -617,24 +635,24 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
                 // what a step has to do besides, one thing behind each of the first slots
                 auto beside = [&](auto slot) {
                     constexpr int k = decltype(slot)::value;
-                    if constexpr (k == 0) store(kbuf + ((odd + LEAD + 1) & 1) * S::TILE, kraw, of_k);
-                    if constexpr (k == 1) store(vbuf + (odd ^ 1) * S::TILE, vraw, of_v);
+                    if constexpr (k == 0) store(kbuf + ((odd + LEAD + 1) & 1) * S::TILE, kraw[set], of_k);
+                    if constexpr (k == 1) store(vbuf + (odd ^ 1) * S::TILE, vraw[set], of_v);
                     if constexpr (k == 2) {
                         const Where w = resolve(asked);
 #pragma unroll
-                        for (int i = 0; i < POS; ++i) there[LEAD + 2][i] = w.there[i];
+                        for (int i = 0; i < POS; ++i) there[LEAD + DEPTH + 1][i] = w.there[i];
                         spread(w.off, spots[LEAD - 1]);
                     }
-                    if constexpr (k == 3) read(vbase, vo, vraw);
-                    if constexpr (k == 4) read(kbase, spots[LEAD - 1], kraw);
-                    if constexpr (k == 5) asked = look(step + LEAD + 3);
+                    if constexpr (k == 3) read(vbase, vo, vraw[set]);
+                    if constexpr (k == 4) read(kbase, spots[LEAD - 1], kraw[set]);
+                    if constexpr (k == 5) asked = look(step + LEAD + DEPTH + 2);
                 };
-                auto part = [&](auto b_, f32x16 (&cur)[RB], f32x16 (&next)[RB], Half (&pr)[RB][2], Half (&pn)[RB][2]) {
-                    constexpr int b = decltype(b_)::value, SLOTS = S::KS + 2 * S::VS, FIRST = SLOTS / 4, AHEAD = S::AHEAD, ALL = 16 * RB;
+                auto part = [&](auto b_, f32x16& cur, f32x16& next, Half (&pr)[2], Half (&pn)[2]) {
+                    constexpr int b = decltype(b_)::value, SLOTS = S::KS + 2 * S::VS, FIRST = SLOTS / 4, AHEAD = S::AHEAD;
                     Operand a[AHEAD + 1];
                     unrolled<AHEAD>([&](auto i) { operand(i, tiles, b, a[i]); });
                     cover(step + (b + 1) / PB, (b + 1) % PB, there[(b + 1) / PB], cur);
-                    float top[RB], ref[RB];
+                    float top, ref;
                     bool moves = false;
                     unrolled<SLOTS>([&](auto i) {
                         constexpr int k = decltype(i)::value;
@@ -642,21 +660,20 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
                         product(i, a[k % (AHEAD + 1)], next, pr);
                         if constexpr (k < FIRST) {
 #pragma unroll
-                            for (int e = ALL * k / FIRST; e < ALL * (k + 1) / FIRST; ++e) largest(cur, top, e);
+                            for (int e = 16 * k / FIRST; e < 16 * (k + 1) / FIRST; ++e) largest(cur, top, e);
                             if constexpr (k == FIRST - 1) moves = refer(top, f, ref);
                         } else {
-                            constexpr int N = SLOTS - FIRST, e0 = ALL * (k - FIRST) / N / 2 * 2, e1 = k == SLOTS - 1 ? ALL : ALL * (k - FIRST + 1) / N / 2 * 2;
+                            constexpr int N = SLOTS - FIRST, e0 = 16 * (k - FIRST) / N / 2 * 2, e1 = k == SLOTS - 1 ? 16 : 16 * (k - FIRST + 1) / N / 2 * 2;
 #pragma unroll
                             for (int e = e0; e < e1; ++e) {
                                 exponent(cur, ref, e);
-                                pn[e / 16][e % 16 / 8][e % 8] = cur[e / 16][e % 16];
+                                pn[e / 8][e % 8] = cur[e];
                             }
                         }
                         if constexpr (b == 0) beside(i);
                         __builtin_amdgcn_sched_barrier(0);
                     });
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) asm volatile("" : "+v"(pn[r][0]), "+v"(pn[r][1]), "+v"(l[r]), "+v"(next[r]));        // here, and not where they are needed
+                    asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(l), "+v"(next));        // here, and not where they are needed
                     if (__builtin_expect(moves, 0)) {
                         asm volatile("");                 // seldom: a branch, not a product with one
                         rescale(f);
@@ -669,37 +686,30 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
                     part(std::integral_constant<int, 1>{}, s0, s1, p1, p0);
                 } else {
                     part(std::integral_constant<int, 0>{}, s1, s0, p0, p1);
-#pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        s1[r] = s0[r];
-                        p0[r][0] = p1[r][0];
-                        p0[r][1] = p1[r][1];
-                    }
+                    s1 = s0;
+                    p0[0] = p1[0];
+                    p0[1] = p1[1];
                 }
 #pragma unroll
-                for (int i = 0; i < LEAD + 2; ++i)
+                for (int i = 0; i < LEAD + DEPTH + 1; ++i)
 #pragma unroll
                     for (int k = 0; k < POS; ++k) there[i][k] = there[i + 1][k];
-            }
-            __syncthreads();                              // all have read their last step
+            });
         }
 
         bool bad = false;
+        if (row_of().real)
 #pragma unroll
-        for (int r = 0; r < RB; ++r)
-            if (row_of(r).real)
+            for (int j = 0; j < S::VS; ++j)
 #pragma unroll
-                for (int j = 0; j < S::VS; ++j)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) bad = bad || !(fabsf(acc[r][j][i]) < __builtin_inff());
-        int* flags = reinterpret_cast<int*>(smem);
-        const bool any = __any(bad);
-        if (lane == 0) flags[wave] = any ? 1 : 0;
-        __syncthreads();
+                for (int i = 0; i < 16; ++i) bad = bad || !(fabsf(acc[j][i]) < __builtin_inff());
+        int* flags = reinterpret_cast<int*>(smem + S::FLAGS);
+        bad = __any(bad);
+        if (lane == 0) flags[wave] = bad ? 1 : 0;
+        lds_sync();                                       // all have read their last step
         bad = false;
 #pragma unroll
         for (int w = 0; w < S::WAVES; ++w) bad = bad || flags[w] != 0;
-        __syncthreads();
         if (bad) {                                        // once more, with care and no haste
             float* scratch = reinterpret_cast<float*>(smem + S::TILE) + wave * 32 * 32;      // one step of K before it, of V behind
             char* vt = smem + S::TILE + S::SCRATCH;
@@ -713,36 +723,33 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
                 store(vt, raw, of_v);
                 __syncthreads();
                 for (int b = 0; b < PB; ++b) {
-                    f32x16 s[RB];
-                    float f[RB];
+                    f32x16 s;
+                    float f;
                     scores(lds_of(kbuf, vt), b, s);
                     cover(step, b, w.there, s);
                     if (exponents(s, f)) rescale(f);
+                    wave_lds_order();
 #pragma unroll
-                    for (int r = 0; r < RB; ++r) {
-                        wave_lds_order();
+                    for (int i = 0; i < 16; ++i) scratch[(8 * (i / 4) + 4 * g + i % 4) * 32 + c] = s[i];
+                    wave_lds_order();
+                    for (int e = 0; e < 32; ++e) {
+                        const float weight = scratch[e * 32 + c];
+                        if (weight == 0.0f) continue;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) scratch[(8 * (i / 4) + 4 * g + i % 4) * 32 + c] = s[r][i];
-                        wave_lds_order();
-                        for (int e = 0; e < 32; ++e) {
-                            const float weight = scratch[e * 32 + c];
-                            if (weight == 0.0f) continue;
+                        for (int j = 0; j < S::VS; ++j)
 #pragma unroll
-                            for (int j = 0; j < S::VS; ++j)
+                            for (int i4 = 0; i4 < 4; ++i4) {
+                                const uint2 raw2 = *reinterpret_cast<const uint2*>(vt + piece_at<S>((wk * PB + b) * 32 + e, 4 * j + i4) + 8 * g);
+                                const unsigned u[2] = {raw2.x, raw2.y};
 #pragma unroll
-                                for (int i4 = 0; i4 < 4; ++i4) {
-                                    const uint2 raw2 = *reinterpret_cast<const uint2*>(vt + piece_at<S>((wk * PB + b) * 32 + e, 4 * j + i4) + 8 * g);
-                                    const unsigned u[2] = {raw2.x, raw2.y};
-#pragma unroll
-                                    for (int i = 0; i < 4; ++i) {
-                                        const unsigned short h = (unsigned short)(u[i / 2] >> 16 * (i & 1));
-                                        float val;
-                                        if constexpr (E4M3) val = (float)__builtin_bit_cast(_Float16, h);
-                                        else val = __uint_as_float((unsigned)h << 16);
-                                        acc[r][j][4 * i4 + i] = __builtin_fmaf(weight, val, acc[r][j][4 * i4 + i]);
-                                    }
+                                for (int i = 0; i < 4; ++i) {
+                                    const unsigned short h = (unsigned short)(u[i / 2] >> 16 * (i & 1));
+                                    float val;
+                                    if constexpr (E4M3) val = (float)__builtin_bit_cast(_Float16, h);
+                                    else val = __uint_as_float((unsigned)h << 16);
+                                    acc[j][4 * i4 + i] = __builtin_fmaf(weight, val, acc[j][4 * i4 + i]);
                                 }
-                        }
+                            }
                     }
                 }
                 __syncthreads();
@@ -750,103 +757,85 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
         }
 
         // ---------------- the end of the item, or of the share's part of it
-#pragma unroll
-        for (int r = 0; r < RB; ++r) l[r] += __shfl_xor(l[r], 32);
+        l += __shfl_xor(l, 32);
         if constexpr (WK > 1) {
-            float* joined = reinterpret_cast<float*>(smem);   // [WK - 1][WM][32 RB][D + 4]: O, then m, l
-            auto slot = [&](int k, int r) { return joined + ((((k - 1) * WM + wm) * RB + r) * 32 + c) * (D + 4); };
-            if (wk > 0)
+            float* joined = reinterpret_cast<float*>(smem);   // [WK - 1][WM][32][D + 4]: O, then m, l
+            auto slot = [&](int k) { return joined + (((k - 1) * WM + wm) * 32 + c) * (D + 4); };
+            if (wk > 0) {
+                float* dst = slot(wk);
 #pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    float* dst = slot(wk, r);
+                for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4)
+                        *reinterpret_cast<float4*>(dst + 32 * j + 8 * i4 + 4 * g) =
+                            make_float4(acc[j][4 * i4], acc[j][4 * i4 + 1], acc[j][4 * i4 + 2], acc[j][4 * i4 + 3]);
+                if (g == 0) {
+                    dst[D] = m;
+                    dst[D + 1] = l;
+                }
+            }
+            lds_sync();
+            if (wk == 0) {
+                float top = m;
+                for (int k = 1; k < WK; ++k) top = fmaxf(top, slot(k)[D]);
+                const float ref = top == -__builtin_inff() ? 0.0f : top;
+                float f = __builtin_amdgcn_exp2f(m - ref);
+                l *= f;
+#pragma unroll
+                for (int j = 0; j < S::VS; ++j)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[j][i] *= f;
+                for (int k = 1; k < WK; ++k) {
+                    const float* src = slot(k);
+                    f = __builtin_amdgcn_exp2f(src[D] - ref);
+                    l += f * src[D + 1];
 #pragma unroll
                     for (int j = 0; j < S::VS; ++j)
 #pragma unroll
-                        for (int i4 = 0; i4 < 4; ++i4)
-                            *reinterpret_cast<float4*>(dst + 32 * j + 8 * i4 + 4 * g) =
-                                make_float4(acc[r][j][4 * i4], acc[r][j][4 * i4 + 1], acc[r][j][4 * i4 + 2], acc[r][j][4 * i4 + 3]);
-                    if (g == 0) {
-                        dst[D] = m[r];
-                        dst[D + 1] = l[r];
-                    }
+                        for (int i4 = 0; i4 < 4; ++i4) {
+                            const float4 v = *reinterpret_cast<const float4*>(src + 32 * j + 8 * i4 + 4 * g);
+                            acc[j][4 * i4] += f * v.x;
+                            acc[j][4 * i4 + 1] += f * v.y;
+                            acc[j][4 * i4 + 2] += f * v.z;
+                            acc[j][4 * i4 + 3] += f * v.w;
+                        }
                 }
-            __syncthreads();
-            if (wk == 0)
-#pragma unroll
-                for (int r = 0; r < RB; ++r) {
-                    float top = m[r];
-                    for (int k = 1; k < WK; ++k) top = fmaxf(top, slot(k, r)[D]);
-                    const float ref = top == -__builtin_inff() ? 0.0f : top;
-                    float f = __builtin_amdgcn_exp2f(m[r] - ref);
-                    l[r] *= f;
-#pragma unroll
-                    for (int j = 0; j < S::VS; ++j)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[r][j][i] *= f;
-                    for (int k = 1; k < WK; ++k) {
-                        const float* src = slot(k, r);
-                        f = __builtin_amdgcn_exp2f(src[D] - ref);
-                        l[r] += f * src[D + 1];
-#pragma unroll
-                        for (int j = 0; j < S::VS; ++j)
-#pragma unroll
-                            for (int i4 = 0; i4 < 4; ++i4) {
-                                const float4 v = *reinterpret_cast<const float4*>(src + 32 * j + 8 * i4 + 4 * g);
-                                acc[r][j][4 * i4] += f * v.x;
-                                acc[r][j][4 * i4 + 1] += f * v.y;
-                                acc[r][j][4 * i4 + 2] += f * v.z;
-                                acc[r][j][4 * i4 + 3] += f * v.w;
-                            }
-                    }
-                    m[r] = top;
-                }
-            __syncthreads();                                  // LDS is free for the next item
+                m = top;
+            }
+            lds_sync();                                       // LDS is free for the next item
         }
         const bool begins = begin == 0, ends = end == steps;
         if (!p.whole && begins && !ends && tid == 0)
-            p.cuts[blockIdx.x] = make_int4(at.b, at.tile, at.hk, (int)((at.at + steps - 1) / at.per - blockIdx.x) + 1);
-        if (wk == 0)
+            p.cuts[blockIdx.x] = make_int4(at.b, at.tile, at.hk, (int)((at.at - at.unit + steps + kBetween - 1) / at.per - blockIdx.x) + 1);
+        const Row o = row_of();
+        if (wk == 0 && o.real) {
+            if (begins && ends) {
+                const float k = l > 0.0f || l != l ? (E4M3 ? p.v_scale[at.hk] : 1.0f) / l : 0.0f;
+                bf16_t* dst = p.out + (int64_t)o.token * p.out_stride + (int64_t)o.head * D;
 #pragma unroll
-            for (int r = 0; r < RB; ++r) {
-                if (begins && ends) {
-                    const Row o = row_of(r);
-                    if (!o.real) continue;
-                    const float k = l[r] > 0.0f || l[r] != l[r] ? (E4M3 ? p.v_scale[at.hk] : 1.0f) / l[r] : 0.0f;
-                    bf16_t* dst = p.out + (int64_t)o.token * p.out_stride + (int64_t)o.head * D;
+                for (int j = 0; j < S::VS; ++j)
 #pragma unroll
-                    for (int j = 0; j < S::VS; ++j)
+                    for (int i4 = 0; i4 < 4; ++i4)
+                        *reinterpret_cast<uint2*>(dst + 32 * j + 8 * i4 + 4 * g) =
+                            make_uint2(pack_bf16(acc[j][4 * i4] * k, acc[j][4 * i4 + 1] * k), pack_bf16(acc[j][4 * i4 + 2] * k, acc[j][4 * i4 + 3] * k));
+                if (p.lse && g == 0) p.lse[(int64_t)o.token * p.H + o.head] = (m - kUp + __log2f(l)) * 0.6931471805599453f;
+            } else {
+                float* part = p.parts + (2 * (int64_t)blockIdx.x + (begins ? 1 : 0)) * S::PART;
+                const int i = wm * 32 + c;
 #pragma unroll
-                        for (int i4 = 0; i4 < 4; ++i4)
-                            *reinterpret_cast<uint2*>(dst + 32 * j + 8 * i4 + 4 * g) =
-                                make_uint2(pack_bf16(acc[r][j][4 * i4] * k, acc[r][j][4 * i4 + 1] * k), pack_bf16(acc[r][j][4 * i4 + 2] * k, acc[r][j][4 * i4 + 3] * k));
-                    if (p.lse && g == 0) p.lse[(int64_t)o.token * p.H + o.head] = (m[r] - kUp + __log2f(l[r])) * 0.6931471805599453f;
-                } else {
-                    float* part = p.parts + (2 * (int64_t)blockIdx.x + (begins ? 1 : 0)) * S::PART;
-                    const int i = (wm * RB + r) * 32 + c;
+                for (int j = 0; j < S::VS; ++j)
 #pragma unroll
-                    for (int j = 0; j < S::VS; ++j)
-#pragma unroll
-                        for (int i4 = 0; i4 < 4; ++i4)
-                            *reinterpret_cast<float4*>(part + (int64_t)i * D + 32 * j + 8 * i4 + 4 * g) =
-                                make_float4(acc[r][j][4 * i4], acc[r][j][4 * i4 + 1], acc[r][j][4 * i4 + 2], acc[r][j][4 * i4 + 3]);
-                    if (g == 0) {
-                        part[S::ROWS * D + i] = m[r];
-                        part[S::ROWS * D + S::ROWS + i] = l[r];
-                    }
+                    for (int i4 = 0; i4 < 4; ++i4)
+                        *reinterpret_cast<float4*>(part + (int64_t)i * D + 32 * j + 8 * i4 + 4 * g) =
+                            make_float4(acc[j][4 * i4], acc[j][4 * i4 + 1], acc[j][4 * i4 + 2], acc[j][4 * i4 + 3]);
+                if (g == 0) {
+                    part[S::ROWS * D + i] = m;
+                    part[S::ROWS * D + S::ROWS + i] = l;
                 }
             }
-        if (p.whole) return;
-        // ---------------- on to the next item of the share
-        at.at += end - begin;
-        if (at.at >= at.end) return;
-        at.step = 0;
-        if (++at.hk < p.Hk) continue;
-        at.hk = 0;
-        ++at.tile;
-        while (at.tile >= Seq(p, at.b).row_tiles(p, S::ROWS)) {       // ends: the share's steps belong to sequences that have some
-            at.tile = 0;
-            ++at.b;
         }
+        if (p.whole) return;
+        if (!advance(ends_at - at.unit)) return;
     }
 }
 
@@ -854,7 +843,7 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT) chunk_kernel(ChunkArg
 template <int D>
 __global__ void __launch_bounds__(256) chunk_join(ChunkArgs p, int rows, float up)
 {
-    constexpr int LANES = D / 4;                          // lanes of a row of O, four columns each
+    constexpr int LANES = D / 4, SETS = 64 / LANES;       // lanes of a row of O, four columns each; sets of lanes that take turns at the parts
     const int4 cut = p.cuts[blockIdx.x];
     const int n = cut.w, lane = threadIdx.x & 63, i = blockIdx.y * 4 + (threadIdx.x >> 6);
     if (n == 0 || i >= rows) return;
@@ -868,21 +857,33 @@ __global__ void __launch_bounds__(256) chunk_join(ChunkArgs p, int rows, float u
 #pragma unroll
     for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     const float ref = top == -__builtin_inff() ? 0.0f : top;
+    const int set = lane / LANES, col = 4 * (lane - set * LANES);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     float sum = 0.0f;
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) {
-        const float* src = part(k);
-        const float f = __builtin_amdgcn_exp2f(src[rows * D + i] - ref);
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (lane < LANES) v = *reinterpret_cast<const float4*>(src + (int64_t)i * D + 4 * lane);
-        o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
-        sum += f * src[rows * D + rows + i];
+    if (set < SETS) {
+#pragma unroll 8
+        for (int k = set; k < n; k += SETS) {
+            const float* src = part(k);
+            const float f = __builtin_amdgcn_exp2f(src[rows * D + i] - ref);
+            const float4 v = *reinterpret_cast<const float4*>(src + (int64_t)i * D + col);
+            o.x += f * v.x; o.y += f * v.y; o.z += f * v.z; o.w += f * v.w;
+            sum += f * src[rows * D + rows + i];
+        }
+    }
+#pragma unroll
+    for (int s = 1; s < SETS; ++s) {                      // in this order in every lane of the first set
+        const int from = (lane + s * LANES) & 63;
+        const float4 v = make_float4(__shfl(o.x, from), __shfl(o.y, from), __shfl(o.z, from), __shfl(o.w, from));
+        const float l = __shfl(sum, from);
+        if (set == 0) {
+            o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+            sum += l;
+        }
     }
     const int j = at / p.group, head = cut.z * p.group + at - j * p.group, t = seq.t0 + j;
     const float k = sum > 0.0f || sum != sum ? (p.v_scale ? p.v_scale[cut.z] : 1.0f) / sum : 0.0f;
-    if (lane < LANES)
-        *reinterpret_cast<uint2*>(p.out + (int64_t)t * p.out_stride + (int64_t)head * D + 4 * lane) = make_uint2(pack_bf16(o.x * k, o.y * k), pack_bf16(o.z * k, o.w * k));
+    if (set == 0)
+        *reinterpret_cast<uint2*>(p.out + (int64_t)t * p.out_stride + (int64_t)head * D + col) = make_uint2(pack_bf16(o.x * k, o.y * k), pack_bf16(o.z * k, o.w * k));
     if (p.lse && lane == 0) p.lse[(int64_t)t * p.H + head] = (top - up + __log2f(sum)) * 0.6931471805599453f;
 }
 
@@ -891,13 +892,13 @@ template <int D, bool E4M3, typename F>
 auto pick(double rows, F&& body)
 {
     if constexpr (D <= 128) {
-        if (rows <= 32) return body(Shape<D, E4M3, 1, 1, 4, 1>{});
-        if (rows <= 64) return body(Shape<D, E4M3, 1, 2, 2, 1>{});
-        if (rows <= 128) return body(Shape<D, E4M3, 1, 4, 1, 2>{});
-        return body(Shape<D, E4M3, 1, 8, 1, 2>{});
+        if (rows <= 32) return body(Shape<D, E4M3, 1, D == 64 ? 4 : 2, 1, 1>{});
+        if (rows <= 64) return body(Shape<D, E4M3, 2, 2, 1, 2>{});
+        if (rows <= 128) return body(Shape<D, E4M3, 4, 2, 1, 1>{});
+        return body(Shape<D, E4M3, 8, 1, 2, 1>{});
     } else {
-        if (rows <= 64) return body(Shape<D, E4M3, 1, 2, 2, 1>{});
-        return body(Shape<D, E4M3, 1, 4, 1, 2>{});
+        if (rows <= 64) return body(Shape<D, E4M3, 2, 2, 1, 1>{});
+        return body(Shape<D, E4M3, 4, 1, 2, 1>{});
     }
 }
 template <typename F>
@@ -982,7 +983,7 @@ hipError_t launch_chunk(const moe_kv_cache& c, const moe_block_table& t, const m
     return pick(c.head_dim, e4m3, rows, [&](auto shape) {
         using S = decltype(shape);
         const int64_t slots = (int64_t)ch.T * p.group / S::ROWS + ch.n_seqs, items = slots * p.Hk;
-        p.whole = ch.n_seqs > 1024 || items >= 8 * 256 * S::RESIDENT;
+        p.whole = ch.n_seqs > kMostShared || items >= 8 * 256 * S::RESIDENT;
         if (p.whole) {
             hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)items), dim3(S::THREADS), S::LDS, s, p);
             return hipGetLastError();

@@ -54,8 +54,8 @@ def test_chunk_attention(dim, tmp_path):
     for c, r in zip(calls, out):
         assert r["status"] == 0, c
         first = r["launches"][0]
-        D, e4m3, RB, WM, WK, PB = first["args"]
-        rows = 32 * RB * WM
+        D, e4m3, WM, WK, PB, depth = first["args"]
+        rows = 32 * WM
         assert first["name"] == "chunk_kernel" and D == dim and bool(e4m3) == c["e4m3"] and first["block"] == 64 * WM * WK and first["lds"] <= 160 * 1024
         if len(r["launches"]) == 1 and first["grid"][0] > 1:      # a block for each item: room for all tiles of rows, however the tokens are dealt out
             group = c["heads"] // c["kv_heads"]
