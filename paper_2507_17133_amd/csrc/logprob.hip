@@ -3,7 +3,7 @@
 //   m = max x,  S = sum e^(x - m),  U = sum e^(x - m) (x - m):      lse = m + log S,  log p_g = (x_g - m) - log S,  H = log S - U / S
 //   rank of g = #{x > x_g} + #{x = x_g, lower number};      the n_top first entries of the order (falling x, rising number)
 //
-// Both terms of H are at least 0, so nothing cancels.  A row is read once: a block takes a slice of it into registers, where the passes that follow
+// Both terms of H are at least 0, so nothing cancels.  A row is read once: a wave takes a slice of it into registers, where the passes that follow
 // (maximum, sums, ranks, the best) find it; join_rows puts the slices of a row together by the same formulas.
 #include "draft.h"
 
@@ -12,11 +12,13 @@
 namespace bmoe {
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kEnough = 768;                      // blocks from which longer slices are taken: three for each CU
+// A slice has one wave, with nobody to wait for (2112 rows of 131072 entries, four given tokens and eight alternatives: slices of one, two, four and eight
+// waves 242, 247, 256 and 371 us).
+constexpr int kThreads = 64;
+constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
+constexpr int kEnough = 1536;                     // slices from which longer ones are taken: six for each CU
 constexpr int kCandidates = 512;                  // entries that a block sorts
-constexpr int kLongest = 32;                      // entries of a thread at most: slices of 8192
-constexpr int kJoinEach = 36, kJoinMost = kJoinEach * kThreads;        // entries that join_rows chooses from
+constexpr int kLongest = 32;                      // entries of a thread at most: slices of 2048
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 struct LogprobArgs {
@@ -135,18 +137,19 @@ __device__ __forceinline__ float reached_by(float v, int n)
 }
 
 // LDS of the choice of a block's best entries.
+template <int WAVES>
 struct Choice {
-    float bound[kWaves];
+    float bound[WAVES];
     int found;
     Entry list[kCandidates];
-    Entry won[kWaves];
+    Entry won[WAVES];
 };
 
 // The first n of the block's entries in order, to put(place, entry); a place that has none gets (-infinity, none).  `most`: the thread's largest value;
 // each(bound, f): f(entry) for every entry of the thread that reaches bound.  Entries that reach a bound that n of them are known to reach hold the first n; where too many
 // do, as where all are alike, the entries are taken out one by one.
-template <typename Each, typename Put>
-__device__ __forceinline__ void choose(Choice& c, int n, float most, Each&& each, Put&& put)
+template <int WAVES, typename Each, typename Put>
+__device__ __forceinline__ void choose(Choice<WAVES>& c, int n, float most, Each&& each, Put&& put)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const float mine = reached_by(most, n);
@@ -155,7 +158,7 @@ __device__ __forceinline__ void choose(Choice& c, int n, float most, Each&& each
     __syncthreads();
     float bound = c.bound[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) bound = fmaxf(bound, c.bound[w]);
+    for (int w = 1; w < WAVES; ++w) bound = fmaxf(bound, c.bound[w]);
     each(bound, [&](const Entry e) {
         const int at = atomicAdd(&c.found, 1);
         if (at < kCandidates) c.list[at] = e;
@@ -164,7 +167,7 @@ __device__ __forceinline__ void choose(Choice& c, int n, float most, Each&& each
     const int found = c.found;
     if (found <= kCandidates) {
         // an entry's place: how many of the others precede it, counted by four neighbouring lanes
-        for (int i0 = 0; i0 < max(found, n); i0 += kThreads / 4) {
+        for (int i0 = 0; i0 < max(found, n); i0 += (64 * WAVES) / 4) {
             const int i = i0 + tid / 4;
             const Entry e = i < found ? c.list[i] : Entry{-__builtin_inff(), 0x7FFFFFFF};
             int at = 0;
@@ -190,7 +193,7 @@ __device__ __forceinline__ void choose(Choice& c, int n, float most, Each&& each
         if (lane == 0) c.won[wave] = top;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
+        for (int w = 0; w < WAVES; ++w)
             if (precedes(c.won[w], top)) top = c.won[w];
         __syncthreads();
         if (tid == 0) put(i, top);
@@ -213,17 +216,16 @@ __device__ __forceinline__ Entry given_token(const LogprobArgs& p, const char* r
     return Entry{real ? logit<FP32>(row, id) : 0.0f, real ? id : -1};
 }
 
-// One slice of a row, EACH entries a thread.  HBM bounds it in large calls, beside the vector instructions (about 9 per entry, an exponential counts as 4, and one
-// more for each given token); the launches in small ones.
+// One slice of a row, EACH entries a thread.  Large calls are bound by HBM as long as sums are all that is asked for (2112 rows of 131072 entries 95 us, 5.8 TB/s),
+// by vector instructions with ranks (two per entry and given token: four tokens 178 us) and alternatives (eight 146 us, both 242); small ones by their launches.
 template <bool FP32, int EACH>
 __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
 {
     constexpr int PER = FP32 ? 4 : 8, VECS = EACH / PER;          // entries of a 16-byte load
-    __shared__ Stats stats[kWaves];
-    __shared__ int counts[kWaves][MOE_MAX_GIVEN + 1];      // given tokens come in twos
+    __shared__ int counts[MOE_MAX_GIVEN + 1];             // given tokens come in twos
     __shared__ Entry given[MOE_MAX_GIVEN];
-    __shared__ Choice choice;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    __shared__ Choice<1> choice;
+    const int tid = threadIdx.x;
     const int t = blockIdx.x / p.slices, slice = blockIdx.x - t * p.slices;
     const char* row = p.logits + (int64_t)t * p.stride * (FP32 ? 4 : 2);
     // slices begin on 16-byte lines, the first of them before the row where that begins inside one
@@ -298,10 +300,9 @@ __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
     }
     a.s = wave_sum(a.s);
     a.u = wave_sum(a.u);
-    if (lane == 0) stats[wave] = a;
-    __syncthreads();                              // given tokens, sums
+    __syncthreads();                              // given tokens
     // ranks, two given tokens at a time (a lane's two counts in one number)
-    const Entry held = p.G ? given[min(lane, p.G - 1)] : Entry{0.0f, -1};
+    const Entry held = p.G ? given[min(tid, p.G - 1)] : Entry{0.0f, -1};
     for (int k = 0; k < p.G; k += 2) {
         int n[2] = {0, 0};
         unsigned mine = 0;
@@ -332,7 +333,7 @@ __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
             }
         }
         mine = wave_sum(mine);
-        if (lane < 2) counts[wave][k + lane] = (lane ? n[1] + (mine >> 16) : n[0] + (mine & 0xFFFFu));
+        if (tid < 2) counts[k + tid] = tid ? n[1] + (mine >> 16) : n[0] + (mine & 0xFFFFu);
     }
     auto each = [&](float bound, auto&& f) {
 #pragma unroll
@@ -346,14 +347,11 @@ __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
                     }
             }
     };
-    a = stats[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) a.join(stats[w]);
     if (p.slices > 1) {
         if (tid == 0) p.stats[blockIdx.x] = make_float4(a.m, a.s, a.u, 0.0f);
         if (p.N) choose(choice, p.N, most, each, [&](int i, const Entry e) { p.best[(int64_t)blockIdx.x * p.N + i] = make_float2(e.x, __int_as_float(e.id)); });
         if (p.G) __syncthreads();
-        if (tid < p.G) p.before[(int64_t)blockIdx.x * p.G + tid] = counts[0][tid] + counts[1][tid] + counts[2][tid] + counts[3][tid];
+        if (tid < p.G) p.before[(int64_t)blockIdx.x * p.G + tid] = counts[tid];
         return;
     }
     const Row r(a);
@@ -370,32 +368,25 @@ __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
     if (tid < p.G) {
         const Entry e = given[tid];
         if (p.logprob) p.logprob[(int64_t)t * p.G + tid] = e.id < 0 ? 0.0f : r.of(e.x);
-        if (p.rank) p.rank[(int64_t)t * p.G + tid] = e.id < 0 || r.none ? -1 : counts[0][tid] + counts[1][tid] + counts[2][tid] + counts[3][tid];
+        if (p.rank) p.rank[(int64_t)t * p.G + tid] = e.id < 0 || r.none ? -1 : counts[tid];
     }
 }
 
-// A block for each row whose slices are joined; EACH of their best entries a thread.
-template <bool FP32, int EACH>
-__global__ void __launch_bounds__(kThreads) join_rows(LogprobArgs p)
+// A block for each row whose slices are joined.  Their best entries are read a second time where they are chosen from: they are many only in rows of many slices.
+template <bool FP32>
+__global__ void __launch_bounds__(kJoinThreads) join_rows(LogprobArgs p)
 {
-    __shared__ Stats stats[kWaves];
-    __shared__ Choice choice;
+    __shared__ Stats stats[kJoinWaves];
+    __shared__ Choice<kJoinWaves> choice;
     const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t first = (int64_t)t * p.slices;
-    Entry entry[EACH];
+    const float2* best = p.best + first * p.N;
+    const int n_best = p.slices * p.N;
     float most = -__builtin_inff();
-#pragma unroll
-    for (int i = 0; i < EACH; ++i) {
-        const int at = i * kThreads + tid;
-        entry[i] = Entry{-__builtin_inff(), 0x7FFFFFFF};
-        if (at < p.slices * p.N) {
-            const float2 v = p.best[first * p.N + at];
-            entry[i] = Entry{v.x, __float_as_int(v.y)};
-        }
-        most = fmaxf(most, entry[i].x);
-    }
+#pragma unroll 4
+    for (int i = tid; i < n_best; i += kJoinThreads) most = fmaxf(most, best[i].x);
     Stats a{-__builtin_inff(), 0.0f, 0.0f};
-    for (int i = tid; i < p.slices; i += kThreads) {
+    for (int i = tid; i < p.slices; i += kJoinThreads) {
         const float4 v = p.stats[first + i];
         a.join(Stats{v.x, v.y, v.z});
     }
@@ -408,7 +399,7 @@ __global__ void __launch_bounds__(kThreads) join_rows(LogprobArgs p)
     __syncthreads();
     a = stats[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) a.join(stats[w]);
+    for (int w = 1; w < kJoinWaves; ++w) a.join(stats[w]);
     const Row r(a);
     if (tid == 0) {
         if (p.lse) p.lse[t] = r.lse;
@@ -428,9 +419,11 @@ __global__ void __launch_bounds__(kThreads) join_rows(LogprobArgs p)
     if (p.N)
         choose(choice, p.N, most,
                [&](float bound, auto&& f) {
-#pragma unroll
-                   for (int i = 0; i < EACH; ++i)
-                       if (entry[i].x >= bound && entry[i].id != 0x7FFFFFFF) f(entry[i]);
+#pragma unroll 4
+                   for (int i = tid; i < n_best; i += kJoinThreads) {
+                       const float2 v = best[i];
+                       if (v.x >= bound && __float_as_int(v.y) != 0x7FFFFFFF) f(Entry{v.x, __float_as_int(v.y)});
+                   }
                },
                [&](int i, const Entry e) {
                    if (p.top_id) p.top_id[(int64_t)t * p.N + i] = r.none ? -1 : e.id;
@@ -440,13 +433,11 @@ __global__ void __launch_bounds__(kThreads) join_rows(LogprobArgs p)
 
 constexpr int slices_of(int V, int each, int ahead = 7) { return (V + ahead + each * kThreads - 1) / (each * kThreads); }      // up to 7 places before a row that begins inside a line
 
-static_assert(slices_of(MOE_MAX_ENTRIES, kLongest) * MOE_MAX_TOP <= kJoinMost, "the best of all slices of a row");
-
 // Entries of a thread: the longest slices that still make enough blocks, or the shortest ones.
-int entries_each(int64_t T, int V, int n_top)
+int entries_each(int64_t T, int V)
 {
     int each = kLongest;
-    while (each > 8 && T * slices_of(V, each) < kEnough && (int64_t)slices_of(V, each / 2) * n_top <= kJoinMost) each /= 2;
+    while (each > 8 && T * slices_of(V, each) < kEnough) each /= 2;
     return each;
 }
 
@@ -461,8 +452,7 @@ hipError_t go(const LogprobArgs& p, int each, hipStream_t s)
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.slices == 1) return e;
-    if (p.slices * p.N <= 4 * kThreads) hipLaunchKernelGGL((join_rows<FP32, 4>), dim3(p.T), threads, 0, s, p);
-    else hipLaunchKernelGGL((join_rows<FP32, kJoinEach>), dim3(p.T), threads, 0, s, p);
+    hipLaunchKernelGGL((join_rows<FP32>), dim3(p.T), dim3(kJoinThreads), 0, s, p);
     return hipGetLastError();
 }
 
@@ -485,7 +475,7 @@ hipError_t launch_logprobs(const moe_logprob_args& a, void* ws, hipStream_t s)
     p.T = a.T; p.V = a.V;
     p.G = a.logprob || a.rank ? a.n_given : 0;
     p.N = a.top_id || a.top_logprob ? a.n_top : 0;
-    const int each = entries_each(a.T, a.V, p.N), size = a.type == MOE_LOGITS_FP32 ? 4 : 2;
+    const int each = entries_each(a.T, a.V), size = a.type == MOE_LOGITS_FP32 ? 4 : 2;
     const bool aligned = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && (a.T == 1 || a.stride * size % 16 == 0);
     p.slices = slices_of(a.V, each, aligned ? 0 : 16 / size - 1);
     const size_t parts = (size_t)p.T * p.slices;
