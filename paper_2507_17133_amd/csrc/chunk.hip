@@ -6,7 +6,7 @@
 // A sequence's rows are its (new token, query head of a key head) pairs, token by token.  An item is a tile of up to ROWS rows of one key head; a block
 // goes through the item's positions STEP at a time.  K and V of a step lie in LDS as [64 columns][position], 16-byte pieces of a row exchanged so that
 // neither of the two ways they are read meets a bank twice; while one step is worked on the next is on its way to registers (e4m3 is widened
-// when it goes to LDS).  Each wave has 32 or 64 of the rows and, where rows are few, its part of the positions:
+// when it goes to LDS).  Each wave has 32 of the rows and, where rows are few, its part of the positions:
 //   S [32 positions][32 rows] = K Q^T,     O^T [D][32 rows] += V^T P^T          (32 x 32 x 16 MFMAs)
 // S leaves lane (g, c) = (lane / 32, lane % 32) with row c at positions 8 j + 4 g + 0..3: already the layout of P^T as the second operand, its 8
 // positions in the order {16 t + 4 g + 0..3, 16 t + 8 + 4 g + 0..3}; V^T is read in the same order by transposing LDS reads.  Maximum, sum and rescaling
@@ -29,15 +29,18 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kChunkShares = 512;                 // shares of the line of steps at most
-constexpr int kBetween = 5;                         // what an item costs besides its steps, in steps
-constexpr int kMostShared = 1024;                 // sequences of a call whose steps are dealt out in shares
-constexpr float kSlack = 4.0f;                    // how far (in powers of two) scores may exceed the maximum that they refer to
+constexpr int kBetween = 5;                       // what an item costs besides its steps, in steps; with 1 a prompt of 2048 tokens took 138 us, with 5 84
+constexpr int kUneven = 16;                       // by how many steps an item may exceed a share where each has a block: about what parts and their join cost
+constexpr int kMostShared = 1024;                 // sequences of a call whose steps are dealt out in shares: what LDS has room for
+// How far (in powers of two) scores may exceed the maximum that they refer to.  0, so that O is rescaled whenever the maximum grows: 4096 tokens, 16 over 4
+// heads of 256, 318 us, with 4 264; 16 x 16 drafted tokens 94 and 80.  2^4 costs the probabilities no bits: they are floating-point, and sums are fp32.
+constexpr float kSlack = 4.0f;
 constexpr int kMostContext = 0x7FFE0000;          // so that positions of new tokens stay in 32 bits
 
 // Rows of a block 32 * WM, one of WM waves each; WK waves share the positions of a step, PB blocks of 32 each.
-template <int D_, bool E4M3_, int WM_, int WK_, int PB_, int DEPTH_>
+template <int D_, bool E4M3_, int WM_, int WK_, int PB_>
 struct Shape {
-    static constexpr int D = D_, WM = WM_, WK = WK_, PB = PB_, DEPTH = DEPTH_;       // DEPTH: steps on their way to registers
+    static constexpr int D = D_, WM = WM_, WK = WK_, PB = PB_;
     static constexpr bool E4M3 = E4M3_;
     static constexpr int WAVES = WM * WK, THREADS = 64 * WAVES;
     static_assert(WAVES == 2 || WAVES == 4 || WAVES == 8, "waves of a block");
@@ -50,8 +53,8 @@ struct Shape {
     static constexpr int SCRATCH = WAVES * 32 * 32 * 4;                       // probabilities of the careful second product
     static constexpr int JOIN = (WK - 1) * WM * 32 * (D + 4) * 4;        // parts of waves that share rows
     static constexpr int FLAGS = std::max({4 * TILE, 2 * TILE + SCRATCH, JOIN}), LDS = FLAGS + 64;       // two steps of K, two of V, or one of each and the scratch, or the parts
-    static constexpr int RESIDENT = WAVES <= 4 && DEPTH == 1 && LDS <= 80 * 1024 && D <= 128 ? 2 : 1;       // blocks of a CU
-    static_assert(PB <= 2 && LDS <= 160 * 1024 && LDS >= kMostShared * 4 + 64, "LDS");
+    static constexpr int RESIDENT = WAVES <= 4 && LDS <= 80 * 1024 && D <= 128 ? 2 : 1;       // blocks of a CU
+    static_assert(PB <= 2 && LDS <= 160 * 1024 && LDS >= kMostShared * 4 + 96, "LDS");
     // floats of a part: [ROWS][D] O, [ROWS] m, [ROWS] l
     static constexpr int64_t PART = (int64_t)ROWS * (D + 2);
 };
@@ -77,7 +80,8 @@ struct ChunkArgs {
     bf16_t* out;
     int64_t out_stride;
     float* lse;
-    int whole;                                    // one block for each item; else shares of the line of steps
+    int whole;                                    // one block for each item: 0 no, 1 yes, 2 if no item is much longer than a share
+    int shares;                                   // of the line of steps, otherwise
     int4* cuts;                                   // per share: the item that it begins and does not end (sequence, tile, key head, shares)
     float* parts;                                 // per share two parts
 };
@@ -151,12 +155,14 @@ __device__ __forceinline__ int64_t sum_before(int64_t v, int lane, int64_t& tota
     return x - v;
 }
 
-// The share's first step: every thread adds up the steps of its part of the places.  LDS: [n_seqs] places, then 8 numbers of 64 bits behind kMostShared of them.
+// The share's first step: every thread adds up the steps of its part of the places.  LDS: [n_seqs] places, then 8 numbers of 64 bits behind kMostShared of
+// them and 8 of 32.  Decides whether each item is to have a block, and leaves the rest to find_item() then.
 template <class S>
-__device__ __forceinline__ bool find_share(const ChunkArgs& p, char* smem, Begin& o)
+__device__ __forceinline__ bool find_share(const ChunkArgs& p, char* smem, Begin& o, bool& whole)
 {
     int* place = reinterpret_cast<int*>(smem);
     int64_t* lds = reinterpret_cast<int64_t*>(smem + kMostShared * sizeof(int));
+    int* longest = reinterpret_cast<int*>(lds + 8);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     for (int b = tid; b < p.n_seqs; b += S::THREADS) place[b] = place_of<S>(p, b);
     __syncthreads();
@@ -179,22 +185,34 @@ __device__ __forceinline__ bool find_share(const ChunkArgs& p, char* smem, Begin
         }
     };
     int64_t sum = 0;
+    int most = 0;
     mine([&](int b, int tile) {
-        sum += units_of<S>(p, b, tile) * p.Hk;
+        const int n = units_of<S>(p, b, tile);
+        sum += (int64_t)n * p.Hk;
+        most = max(most, n);
         return false;
     });
+#pragma unroll
+    for (int i = 32; i; i >>= 1) most = max(most, __shfl_xor(most, i));
     int64_t total;
     int64_t before = sum_before(sum, lane, total);
-    if (lane == 0) lds[wave] = total;
+    if (lane == 0) {
+        lds[wave] = total;
+        longest[wave] = most;
+    }
     __syncthreads();
     int64_t all = 0;
 #pragma unroll
     for (int w = 0; w < S::WAVES; ++w) {
         if (w < wave) before += lds[w];
         all += lds[w];
+        most = max(most, longest[w]);
     }
     __syncthreads();
-    o.per = (all + gridDim.x - 1) / gridDim.x;
+    o.per = (all + p.shares - 1) / p.shares;
+    whole = __builtin_amdgcn_readfirstlane(p.whole == 2 && most <= o.per + kUneven ? 1 : 0) != 0;
+    if (whole) return true;
+    if ((int)blockIdx.x >= p.shares) return false;
     o.at = min(all, o.per * (int64_t)blockIdx.x);
     o.end = min(all, o.at + o.per);
     if (o.at >= o.end) return false;
@@ -227,7 +245,8 @@ __device__ __forceinline__ bool find_share(const ChunkArgs& p, char* smem, Begin
 template <class S>
 __device__ __forceinline__ bool find_item(const ChunkArgs& p, Begin& o)
 {
-    const int lane = threadIdx.x & 63, slots = gridDim.x / p.Hk, u = slots - 1 - (int)(blockIdx.x / p.Hk);
+    const int lane = threadIdx.x & 63, slots = (int)((int64_t)p.T * p.group / S::ROWS) + p.n_seqs, u = slots - 1 - (int)(blockIdx.x / p.Hk);
+    if (u < 0) return false;
     // the last sequence whose place is not beyond u, 64 of a stride at a time
     int lo = 0, n = p.n_seqs;
     while (n > 1) {
@@ -296,12 +315,12 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
     char *const kbuf = smem, *const vbuf = smem + 2 * S::TILE;
 
     Begin at;
-    if (p.whole) {
-        if (!find_item<S>(p, at)) return;
-    } else {
-        if (tid == 0) p.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
-        if (!find_share<S>(p, smem, at)) return;
+    bool whole = p.whole == 1;
+    if (!whole) {
+        if (tid == 0 && (int)blockIdx.x < p.shares) p.cuts[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (!find_share<S>(p, smem, at, whole)) return;
     }
+    if (whole && !find_item<S>(p, at)) return;
 
     for (;;) {
         // ---------------- an item, or what the share has of it
@@ -309,8 +328,8 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
         const int row = table_row(p, at.b);
         const Span span(p, seq, at.tile, S::ROWS, (unsigned)row < (unsigned)p.n_rows);
         const int32_t* pages = p.pages + (span.n > 0 ? (int64_t)row * p.row_stride : 0);          // where there is nothing to see, any row will do
-        const int steps = span.template steps<STEP>(), begin = p.whole ? 0 : max(at.unit - kBetween, 0);
-        const int ends_at = p.whole ? steps + kBetween : (int)min((int64_t)steps + kBetween, at.unit + (at.end - at.at)), end = max(ends_at - kBetween, 0);
+        const int steps = span.template steps<STEP>(), begin = whole ? 0 : max(at.unit - kBetween, 0);
+        const int ends_at = whole ? steps + kBetween : (int)min((int64_t)steps + kBetween, at.unit + (at.end - at.at)), end = max(ends_at - kBetween, 0);
         // on by so much of the line; false at the share's end
         auto advance = [&](int units) {
             at.at += units;
@@ -573,16 +592,16 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
         // ---------------- the pipeline: block n of a wave is weighed while n + 1 has its exponentials taken and n + 2 its scores.  In step j V of step j and K
         // of step j + LEAD are in LDS, the next ones in registers, those after them on their way to there.
         {
-            constexpr int LEAD = S::LEAD, DEPTH = S::DEPTH;
-            Raw kraw[DEPTH], vraw[DEPTH];
-            unsigned spots[LEAD][PIECES];                 // where the thread reads, of steps j + DEPTH + 1 .. j + DEPTH + LEAD
-            uint64_t there[LEAD + DEPTH + 2][POS];        // of steps j ..
+            constexpr int LEAD = S::LEAD;
+            Raw kraw, vraw;
+            unsigned spots[LEAD][PIECES];                 // where the thread reads, of steps j + 2 .. j + LEAD + 1
+            uint64_t there[LEAD + 3][POS];              // of steps j ..
             Look asked;
             f32x16 s0, s1;
             Half p0[2], p1[2];
             float f;
             {
-                constexpr int N = LEAD + DEPTH + 1;
+                constexpr int N = LEAD + 2;
                 Look first[N];
                 Where w[N];
                 Raw kr[LEAD + 1], vr;
@@ -597,11 +616,8 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
                     if (i <= LEAD) fetch(kbase, w[i].off, kr[i]);
                     if (i == 0) fetch(vbase, w[0].off, vr);
                 }
-#pragma unroll
-                for (int i = 0; i < DEPTH; ++i) {
-                    fetch(kbase, w[LEAD + 1 + i].off, kraw[i]);
-                    fetch(vbase, w[1 + i].off, vraw[i]);
-                }
+                fetch(kbase, w[LEAD + 1].off, kraw);
+                fetch(vbase, w[1].off, vraw);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) store(kbuf + i * S::TILE, kr[i], of_k);
                 store(vbuf, vr, of_v);
@@ -617,12 +633,10 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
                 exponents(s0, f);
                 rounded(s0, p0);
 #pragma unroll
-                for (int i = 0; i < LEAD; ++i) spread(w[1 + DEPTH + i].off, spots[i]);
+                for (int i = 0; i < LEAD; ++i) spread(w[2 + i].off, spots[i]);
             }
-            for (int step0 = begin; step0 < end; step0 += DEPTH) unrolled<DEPTH>([&](auto turn) {
-                constexpr int set = decltype(turn)::value;
-                const int step = step0 + set, odd = (step - begin) & 1;
-                if (set > 0 && step >= end) return;
+            for (int step = begin; step < end; ++step) {
+                const int odd = (step - begin) & 1;
                 lds_sync();                               // V of this step and K of step + LEAD are there, and nobody reads the other buffers any more
                 unsigned vo[PIECES];
 #pragma unroll
@@ -635,17 +649,17 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
                 // what a step has to do besides, one thing behind each of the first slots
                 auto beside = [&](auto slot) {
                     constexpr int k = decltype(slot)::value;
-                    if constexpr (k == 0) store(kbuf + ((odd + LEAD + 1) & 1) * S::TILE, kraw[set], of_k);
-                    if constexpr (k == 1) store(vbuf + (odd ^ 1) * S::TILE, vraw[set], of_v);
+                    if constexpr (k == 0) store(kbuf + ((odd + LEAD + 1) & 1) * S::TILE, kraw, of_k);
+                    if constexpr (k == 1) store(vbuf + (odd ^ 1) * S::TILE, vraw, of_v);
                     if constexpr (k == 2) {
                         const Where w = resolve(asked);
 #pragma unroll
-                        for (int i = 0; i < POS; ++i) there[LEAD + DEPTH + 1][i] = w.there[i];
+                        for (int i = 0; i < POS; ++i) there[LEAD + 2][i] = w.there[i];
                         spread(w.off, spots[LEAD - 1]);
                     }
-                    if constexpr (k == 3) read(vbase, vo, vraw[set]);
-                    if constexpr (k == 4) read(kbase, spots[LEAD - 1], kraw[set]);
-                    if constexpr (k == 5) asked = look(step + LEAD + DEPTH + 2);
+                    if constexpr (k == 3) read(vbase, vo, vraw);
+                    if constexpr (k == 4) read(kbase, spots[LEAD - 1], kraw);
+                    if constexpr (k == 5) asked = look(step + LEAD + 3);
                 };
                 auto part = [&](auto b_, f32x16& cur, f32x16& next, Half (&pr)[2], Half (&pn)[2]) {
                     constexpr int b = decltype(b_)::value, SLOTS = S::KS + 2 * S::VS, FIRST = SLOTS / 4, AHEAD = S::AHEAD;
@@ -691,10 +705,10 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
                     p0[1] = p1[1];
                 }
 #pragma unroll
-                for (int i = 0; i < LEAD + DEPTH + 1; ++i)
+                for (int i = 0; i < LEAD + 2; ++i)
 #pragma unroll
                     for (int k = 0; k < POS; ++k) there[i][k] = there[i + 1][k];
-            });
+            }
         }
 
         bool bad = false;
@@ -805,7 +819,7 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
             lds_sync();                                       // LDS is free for the next item
         }
         const bool begins = begin == 0, ends = end == steps;
-        if (!p.whole && begins && !ends && tid == 0)
+        if (!whole && begins && !ends && tid == 0)
             p.cuts[blockIdx.x] = make_int4(at.b, at.tile, at.hk, (int)((at.at - at.unit + steps + kBetween - 1) / at.per - blockIdx.x) + 1);
         const Row o = row_of();
         if (wk == 0 && o.real) {
@@ -834,7 +848,7 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
                 }
             }
         }
-        if (p.whole) return;
+        if (whole) return;
         if (!advance(ends_at - at.unit)) return;
     }
 }
@@ -887,20 +901,32 @@ __global__ void __launch_bounds__(256) chunk_join(ChunkArgs p, int rows, float u
     if (p.lse && lane == 0) p.lse[(int64_t)t * p.H + head] = (top - up + __log2f(sum)) * 0.6931471805599453f;
 }
 
-// body(Shape): the shape that a call takes.
+// body(Shape): the shape that a call takes, by the rows that a sequence has on average.  Both sides measured, in us, 32 query heads over 8 of 128
+// columns if nothing else is said
+// (prompts in shares of steps):
+//   up to 32 rows    two waves with a half of the positions each, two blocks a CU, so that one reads while the other begins or ends an item: 64
+//                    sequences of 8 tokens, up to 4096 positions in e4m3: 120; four waves 140; the shape for 128 rows 148.  Heads of 64 columns,
+//                    whose steps are small, with four waves: 32 sequences of 8 tokens 50, two waves 52 (16 of 16 tokens, bf16: 55 and 62)
+//   up to 64, e4m3   two waves of 32 rows in the same manner: 64 sequences of 8 tokens, 64 over 8 heads, up to 2048 positions: 81; the next shape 93
+//   up to 64, bf16   where twice as much is on its way, the next shape: 16 tokens behind 32768 positions 45; two waves 49; four 46
+//   up to 128        eight waves, of which two share the positions of 32 rows: 16 sequences of 24 tokens, up to 4096 positions: 64; the last shape 67
+//   more             eight waves with all positions: 4096 tokens, 32 over 8 heads of 64: 145; the shape for 128 rows 185
+// Heads of 192 and 256 columns leave registers for four waves, with all positions: 4096 tokens, 16 over 4 heads of 256: 264; where two share the
+// positions 477.  They do share them for few rows of 192 columns: 32 sequences of 4 tokens, 32 over 4 heads: 79 and 85 (of 256: 73 and 70).
 template <int D, bool E4M3, typename F>
 auto pick(double rows, F&& body)
 {
     if constexpr (D <= 128) {
-        if (rows <= 32) return body(Shape<D, E4M3, 1, D == 64 ? 4 : 2, 1, 1>{});
-        if (rows <= 64) return body(Shape<D, E4M3, 2, 2, 1, 2>{});
-        if (rows <= 128) return body(Shape<D, E4M3, 4, 2, 1, 1>{});
-        return body(Shape<D, E4M3, 8, 1, 2, 1>{});
+        if (rows <= 32) return body(Shape<D, E4M3, 1, D == 64 ? 4 : 2, 1>{});
+        if (E4M3 && rows <= 64) return body(Shape<D, E4M3, 2, 1, 2>{});
+        if (rows <= 128) return body(Shape<D, E4M3, 4, 2, 1>{});
+        return body(Shape<D, E4M3, 8, 1, 2>{});
     } else {
-        if (rows <= 64) return body(Shape<D, E4M3, 2, 2, 1, 1>{});
-        return body(Shape<D, E4M3, 4, 1, 2, 1>{});
+        if (D == 192 && rows <= 32) return body(Shape<192, E4M3, 2, 2, 1>{});
+        return body(Shape<D, E4M3, 4, 1, 2>{});
     }
 }
+
 template <typename F>
 auto pick(int D, bool e4m3, double rows, F&& body)
 {
@@ -983,17 +1009,23 @@ hipError_t launch_chunk(const moe_kv_cache& c, const moe_block_table& t, const m
     return pick(c.head_dim, e4m3, rows, [&](auto shape) {
         using S = decltype(shape);
         const int64_t slots = (int64_t)ch.T * p.group / S::ROWS + ch.n_seqs, items = slots * p.Hk;
-        p.whole = ch.n_seqs > kMostShared || items >= 8 * 256 * S::RESIDENT;
-        if (p.whole) {
+        // The tiles of a drafted tree see all of their sequence and go by shares: 256 trees of 8 tokens, up to 2048 positions, 230 us, with a block for each item
+        // 248.  So do chunks of one tile each (256 x 8 tokens behind up to 4096: 400 us and 694).  Where a chunk has two tiles and more, its blocks read the
+        // same positions at about the same time and write no parts: a prompt of 4096 tokens 164 us, in shares 197; four of 512, a window of 1024, 58 and
+        // 67; sixteen of 128 95 and 109; 16384 tokens 2060 and 2194.  One sequence that is far longer than the others would keep few blocks busy, and only
+        // the device knows the lengths: its blocks add them up (3 us) and take shares then.
+        const int most_shares = 256 * S::RESIDENT;
+        p.whole = ch.n_seqs > kMostShared ? 1 : !p.seen && rows >= 2 * S::ROWS && items - (int64_t)ch.n_seqs * p.Hk >= most_shares ? 2 : 0;
+        if (p.whole == 1) {
             hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)items), dim3(S::THREADS), S::LDS, s, p);
             return hipGetLastError();
         }
         const int64_t most = items * (((int64_t)p.cap + S::STEP - 1) / S::STEP);
-        const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(most, 256 * S::RESIDENT));
-        hipLaunchKernelGGL((chunk_kernel<S>), dim3(grid), dim3(S::THREADS), S::LDS, s, p);
+        p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(most, most_shares));
+        hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)(p.whole ? std::max<int64_t>(items, p.shares) : p.shares)), dim3(S::THREADS), S::LDS, s, p);
         hipError_t e = hipGetLastError();
-        if (e != hipSuccess || grid == 1) return e;
-        hipLaunchKernelGGL((chunk_join<S::D>), dim3(grid, S::ROWS / 4), dim3(256), 0, s, p, S::ROWS, S::E4M3 ? 11.0f : 0.0f);
+        if (e != hipSuccess || p.shares == 1) return e;
+        hipLaunchKernelGGL((chunk_join<S::D>), dim3(p.shares, S::ROWS / 4), dim3(256), 0, s, p, S::ROWS, S::E4M3 ? 11.0f : 0.0f);
         return hipGetLastError();
     });
 }

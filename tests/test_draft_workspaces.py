@@ -54,15 +54,21 @@ def test_chunk_attention(dim, tmp_path):
     for c, r in zip(calls, out):
         assert r["status"] == 0, c
         first = r["launches"][0]
-        D, e4m3, WM, WK, PB, depth = first["args"]
+        D, e4m3, WM, WK, PB = first["args"]
         rows = 32 * WM
         assert first["name"] == "chunk_kernel" and D == dim and bool(e4m3) == c["e4m3"] and first["block"] == 64 * WM * WK and first["lds"] <= 160 * 1024
         if len(r["launches"]) == 1 and first["grid"][0] > 1:      # a block for each item: room for all tiles of rows, however the tokens are dealt out
             group = c["heads"] // c["kv_heads"]
             assert first["grid"][0] == (c["T"] * group // rows + c["seqs"]) * c["kv_heads"]
-        else:                                                     # shares, two parts each
+        else:                                                     # shares, two parts each; perhaps with blocks enough for the items, too
+            shares = first["grid"][0]
+            if len(r["launches"]) == 2:
+                group, join = c["heads"] // c["kv_heads"], r["launches"][1]
+                items = (c["T"] * group // rows + c["seqs"]) * c["kv_heads"]
+                shares = join["grid"][0]
+                assert join["name"] == "chunk_join" and first["grid"][0] in (shares, max(shares, items)) and (not c["tree"] or first["grid"][0] == shares), c
             size = M.C.c_size_t(0)
             cache = M.moe_kv_cache(k=4096, v=4096, page_stride=16 * c["kv_heads"] * dim, token_stride=c["kv_heads"] * dim, head_stride=dim, k_scale=4096,
                                    v_scale=4096, type=1 if c["e4m3"] else 0, n_pages=10, page_size=16, n_kv_heads=c["kv_heads"], head_dim=dim)
             assert M._lib().moe_chunk_workspace_size(M.C.byref(cache), c["seqs"], c["T"], c["heads"], M.C.byref(size)) == 0
-            assert size.value >= up(16 * first["grid"][0]) + 4 * 2 * first["grid"][0] * rows * (dim + 2), c
+            assert size.value >= up(16 * shares) + 4 * 2 * shares * rows * (dim + 2), c
