@@ -338,9 +338,9 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
             if (++at.hk < p.Hk) return true;
             at.hk = 0;
             ++at.tile;
-            while (at.tile >= Seq(p, at.b).row_tiles(p, S::ROWS)) {   // ends: the share's steps belong to sequences that have some
+            while (at.tile >= Seq(p, at.b).row_tiles(p, S::ROWS)) {
                 at.tile = 0;
-                ++at.b;
+                if (++at.b >= p.n_seqs) return false;             // only where `first` decreases
             }
             return true;
         };
@@ -859,7 +859,7 @@ __global__ void __launch_bounds__(256) chunk_join(ChunkArgs p, int rows, float u
 {
     constexpr int LANES = D / 4, SETS = 64 / LANES;       // lanes of a row of O, four columns each; sets of lanes that take turns at the parts
     const int4 cut = p.cuts[blockIdx.x];
-    const int n = cut.w, lane = threadIdx.x & 63, i = blockIdx.y * 4 + (threadIdx.x >> 6);
+    const int n = min(cut.w, (int)(gridDim.x - blockIdx.x)), lane = threadIdx.x & 63, i = blockIdx.y * 4 + (threadIdx.x >> 6);
     if (n == 0 || i >= rows) return;
     const Seq seq(p, cut.x);
     const int at = cut.y * rows + i;
