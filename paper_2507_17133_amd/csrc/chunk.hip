@@ -15,6 +15,17 @@
 //
 // A position counts for some rows of an item and not for others; its probability is then 0 for these, but 0 times a NaN or an infinity of V is NaN.  A
 // part whose result is not finite is computed once more with the second product in fp32 lane by lane, which skips such places.
+//
+// A probability is rounded once for the second product: to bf16 beside a bf16 V (half a step, 2^-8 of it: 0.0020 to 0.0023 of the result's norm against 64 bits, 0.0017
+// of that the result's own rounding), to fp16 beside an e4m3 V, which fp16 holds exactly (2^-11: 0.0017 in all).  Two bf16 for each would take half as many
+// products again where these are a half of the time.
+//
+// What bounds it: a CU's matrix and vector instructions, which hardly overlap.  (Beside a step of 32 x 32 x 16 MFMAs that takes 16.6 ns alone, fused multiply-adds
+// of 10.1 ns alone make 22.4.)  So the loop has its products, LDS reads and the softmax of the neighbouring blocks in slots of a fixed order: block n is
+// weighed, n + 1 has its exponentials taken, n + 2 its scores computed.  Measured, join included: 16384 tokens of four prompts, a window of
+// 4096, 56 over 8 heads of 128, bf16 2060 to 2120 us, 918 TFLOP/s (matrix pipe 0.43 of the cycles, vector 0.52 of the issue); 64 trees of 33 tokens behind up
+// to 8192 positions, 64 over 8 heads, e4m3 450 to 478 us, 1.8 TB/s and 650 TFLOP/s (0.34 and 0.44: 27 us are the join, and items begin and end); a tree of 26 tokens behind
+// 2048 positions 25 us, latency.  Without that order, or with LDS rows that were not turned, the first took 2614.
 #include "draft.h"
 
 #include <algorithm>
@@ -307,7 +318,7 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
     constexpr int D = S::D, WM = S::WM, WK = S::WK, PB = S::PB, STEP = S::STEP, POS = STEP / 64;
     constexpr bool E4M3 = S::E4M3;
     using Half = pv8<E4M3>;
-    // e4m3: probabilities as fp16, exactly enough for V's 4 bits; 2^kUp of them, so that small ones are not lost below fp16's range
+    // e4m3: probabilities as fp16, 2^kUp of them, so that small ones are not lost below fp16's range (2^(kUp + kSlack) is within it)
     constexpr float kUp = E4M3 ? 11.0f : 0.0f;
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);

@@ -5,6 +5,7 @@
 // Whole turns are taken off in fp64, where position times frequency is exact to 1e-16 of the turns made; the sine and cosine of what is
 // left are fp32.  They are computed once per token and shared by its heads through LDS.  HBM bound: each input is read once, each
 // output written once.  1021 tokens of 16 + 2 * 16 heads into e4m3 7.0 us, one token 2.6 us: latency.
+// Tokens of a tree go to places apart from their positions: 2112 tokens of 32 + 2 * 8 heads into e4m3 8.2 us.
 #include "layer.h"
 
 #include <type_traits>
