@@ -215,11 +215,14 @@ def moe_token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = No
         new = logits.new_empty
         out = Logprobs(new((T, G), dtype=f32) if G else None, new((T, G), dtype=i32) if G else None, new(T, dtype=f32), new(T, dtype=f32),
                        new((T, top), dtype=i32) if top else None, new((T, top), dtype=f32) if top else None)
+        to = [None if t is None else t.data_ptr() for t in out]
+    else:
+        to = [_dense(out.logprob, f32, T, G), _dense(out.rank, i32, T, G), _dense(out.lse, f32, T), _dense(out.entropy, f32, T),
+              _dense(out.top_id, i32, T, top), _dense(out.top_logprob, f32, T, top)]
     if workspace is None:
         workspace = alloc_logprob_workspace(T, V, G, top, logits.device)
     a = moe_logprob_args(logits.data_ptr(), _rows(logits, f32 if fp32 else torch.bfloat16, T, V), tokens.data_ptr() if G else None, tokens_stride,
-                         _dense(out.logprob, f32, T, G), _dense(out.rank, i32, T, G), _dense(out.lse, f32, T), _dense(out.entropy, f32, T),
-                         _dense(out.top_id, i32, T, top), _dense(out.top_logprob, f32, T, top), T, V, MOE_LOGITS_FP32 if fp32 else MOE_LOGITS_BF16, G, top)
+                         *to, T, V, MOE_LOGITS_FP32 if fp32 else MOE_LOGITS_BF16, G, top)
     st = (_ready or _lib()).moe_token_logprobs(C.byref(a), *_bytes(workspace), _on(logits))
     if st != MOE_OK:
         _check(st, "moe_token_logprobs")
