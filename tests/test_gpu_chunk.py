@@ -165,6 +165,28 @@ def test_long_chunks_of_very_different_contexts(lengths, e4m3):
     assert bool(torch.isfinite(lse).all())
 
 
+def test_captured_chunks_whose_contexts_change():
+    """One graph and one workspace: a block for each item, then shares, then blocks again, as the lengths of the replay say."""
+    new, lengths = [400, 401, 399], [(0, 0, 0), (9000, 0, 70), (30, 60, 0), (0, 9000, 1000), (0, 0, 0)]
+    cache, table, first, _, q, _, _ = _setup(24, new, [9000, 9000, 9000], 64, 32, 64)
+    first, context = _dev(first), _dev([0, 0, 0])
+    ws = A.alloc_chunk_workspace(cache, 3, q.shape[0], 64)
+    call = lambda workspace: A.moe_chunk_attention(cache, q, table, first, context, want_lse=True, workspace=workspace)
+    eager = []
+    for n in lengths:
+        context.copy_(torch.tensor(n, dtype=torch.int32))
+        eager.append(call(A.alloc_chunk_workspace(cache, 3, q.shape[0], 64)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = call(ws)
+    for n, (want, want_lse) in zip(lengths, eager):
+        context.copy_(torch.tensor(n, dtype=torch.int32))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), n
+
+
 def test_one_long_sequence_among_short_ones():
     _check(_setup(8, [5, 5, 5, 5], [20000, 3, 50, 0], 8, 2, 64, 64, tree=True))
     _check(_setup(9, [30, 1], [30000, 9], 8, 2, 128, 16, e4m3=True), window=25000, sinks=5)
