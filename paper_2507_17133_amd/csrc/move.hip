@@ -3,7 +3,7 @@
 // Sources increase and none lies before its target, so a thread that takes its 16 bytes of a head through the list, eight entries read before any of
 // them is written, moves them as if all had been read first.  Each entry is two dependent loads (list, block table) of one address for the whole block, then
 // the row: latency, of a few accepted tokens (5 of one request, 8 heads of 128, bf16: 4.5 us) as of many (9 of each of 256, e4m3: 9.9 us, 9.4 MB
-// read and written; two trips of 8 entries each).
+// read and written; two trips of up to 8 entries.  With 4 at a time 20.6 us, with 12 9.4, with 16 10.1, the one request 0.1 and 0.6 us more).
 #include "draft.h"
 
 namespace bmoe {
