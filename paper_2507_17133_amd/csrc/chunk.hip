@@ -27,6 +27,7 @@
 // to 8192 positions, 64 over 8 heads, e4m3 450 to 478 us, 1.8 TB/s and 650 TFLOP/s (0.34 and 0.44: 27 us are the join, and items begin and end); a tree of 26 tokens behind
 // 2048 positions 25 us, latency.  Without that order, or with LDS rows that were not turned, the first took 2614.
 #include "draft.h"
+#include "chunk_span.h"
 
 #include <algorithm>
 #include <type_traits>
@@ -109,20 +110,14 @@ struct Seq {
     __device__ __forceinline__ int row_tiles(const ChunkArgs& p, int rows) const { return (n * p.group + rows - 1) / rows; }
 };
 
-// The positions of a tile of rows: the first `sinks`, then those from lo on, n in all.
-struct Span {
-    int sinks, lo, n;
-    __device__ __forceinline__ Span(const ChunkArgs& p, const Seq& s, int tile, int rows, bool there)
-    {
-        const int j0 = tile * rows / p.group, j1 = min(s.n - 1, (tile * rows + rows - 1) / p.group);
-        const int hi = there ? min(s.context + (p.seen ? s.n : j1 + 1), p.cap) : 0;
-        lo = p.window > 0 ? min(max(s.context + (p.seen ? 0 : j0) + 1 - p.window, 0), hi) : 0;
-        sinks = min(p.sinks, lo);
-        n = hi - lo + sinks;
-    }
-    template <int STEP>
-    __device__ __forceinline__ int steps() const { return max(1, (n + STEP - 1) / STEP); }       // an item with nothing to see has its rows cleared
-};
+// The positions of a sequence's tile of rows; `there`: whether the block table has a row for it.
+__device__ __forceinline__ Span span_of(const ChunkArgs& p, const Seq& s, int tile, int rows, bool there)
+{
+    const int j0 = tile * rows / p.group, j1 = min(s.n - 1, (tile * rows + rows - 1) / p.group);
+    return Span(s.context, s.n, j0, j1, p.seen != nullptr, p.window, p.sinks, there ? p.cap : 0);
+}
+template <int STEP>
+__device__ __forceinline__ int steps_in(const Span& s) { return max(1, (s.n + STEP - 1) / STEP); }       // an item with nothing to see has its rows cleared
 
 __device__ __forceinline__ int table_row(const ChunkArgs& p, int b) { return p.row_of ? p.row_of[b] : b; }
 
@@ -137,7 +132,7 @@ __device__ __forceinline__ int steps_of(const ChunkArgs& p, int b, int tile)
 {
     const Seq s(p, b);
     if (tile >= s.row_tiles(p, S::ROWS)) return 0;
-    return Span(p, s, tile, S::ROWS, (unsigned)table_row(p, b) < (unsigned)p.n_rows).template steps<S::STEP>();
+    return steps_in<S::STEP>(span_of(p, s, tile, S::ROWS, (unsigned)table_row(p, b) < (unsigned)p.n_rows));
 }
 
 // Length of an item of the tile in the line that shares are cut from: its steps, behind kBetween that stand for what it costs besides.
@@ -337,9 +332,9 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
         // ---------------- an item, or what the share has of it
         const Seq seq(p, at.b);
         const int row = table_row(p, at.b);
-        const Span span(p, seq, at.tile, S::ROWS, (unsigned)row < (unsigned)p.n_rows);
+        const Span span = span_of(p, seq, at.tile, S::ROWS, (unsigned)row < (unsigned)p.n_rows);
         const int32_t* pages = p.pages + (span.n > 0 ? (int64_t)row * p.row_stride : 0);          // where there is nothing to see, any row will do
-        const int steps = span.template steps<STEP>(), begin = whole ? 0 : max(at.unit - kBetween, 0);
+        const int steps = steps_in<STEP>(span), begin = whole ? 0 : max(at.unit - kBetween, 0);
         const int ends_at = whole ? steps + kBetween : (int)min((int64_t)steps + kBetween, at.unit + (at.end - at.at)), end = max(ends_at - kBetween, 0);
         // on by so much of the line; false at the share's end
         auto advance = [&](int units) {
@@ -418,9 +413,9 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
             Look o;
 #pragma unroll
             for (int k = 0; k < POS; ++k) {
-                const int v = step * STEP + 64 * k + lane, in = max(min(v, most - 1), 0);
+                const int v = step * STEP + 64 * k + lane;
                 o.counts[k] = __ballot(v < most);
-                const unsigned pos = in < span.sinks ? in : in - span.sinks + span.lo;
+                const unsigned pos = span.read(v, most);
                 const unsigned pg = (unsigned)((uint64_t)pos * p.page_magic >> p.page_shift);
                 o.in_page[k] = pos - pg * (unsigned)p.page_size;
                 o.page[k] = pages[pg];
