@@ -16,9 +16,9 @@
 // A position counts for some rows of an item and not for others; its probability is then 0 for these, but 0 times a NaN or an infinity of V is NaN.  A
 // part whose result is not finite is computed once more with the second product in fp32 lane by lane, which skips such places.
 //
-// A probability is rounded once for the second product: to bf16 beside a bf16 V (half a step, 2^-8 of it: 0.0020 to 0.0023 of the result's norm against 64 bits, 0.0017
-// of that the result's own rounding), to fp16 beside an e4m3 V, which fp16 holds exactly (2^-11: 0.0017 in all).  Two bf16 for each would take half as many
-// products again where these are a half of the time.
+// A probability's rounding for the second product: beside an e4m3 V to fp16, which fp16 holds exactly (2^-11 of it: error of a result against 64 bits 0.0017 of the norm, which is
+// the result's own rounding).  Beside a bf16 V, sequences of up to 128 rows have it as two bf16, cut off at bf16's bits and the rest, which add up to it within 2^-15 (0.0017);
+// longer ones as one (half a step, 2^-8 of it: 0.0023), where a second product costs a quarter of the time (see pick).
 //
 // What bounds it: a CU's matrix and vector instructions, which hardly overlap.  (Beside a step of 32 x 32 x 16 MFMAs that takes 16.6 ns alone, fused multiply-adds
 // of 10.1 ns alone make 22.4.)  So the loop has its products, LDS reads and the softmax of the neighbouring blocks in slots of a fixed order: block n is
@@ -53,7 +53,7 @@ constexpr int kMostContext = 0x7FFE0000;          // so that positions of new to
 template <int D_, bool E4M3_, int WM_, int WK_, int PB_>
 struct Shape {
     static constexpr int D = D_, WM = WM_, WK = WK_, PB = PB_;
-    static constexpr bool E4M3 = E4M3_;
+    static constexpr bool E4M3 = E4M3_, TWO = false;
     static constexpr int WAVES = WM * WK, THREADS = 64 * WAVES;
     static_assert(WAVES == 2 || WAVES == 4 || WAVES == 8, "waves of a block");
     static constexpr int ROWS = 32 * WM, STEP = 32 * PB * WK;
@@ -69,6 +69,12 @@ struct Shape {
     static_assert(PB <= 2 && LDS <= 160 * 1024 && LDS >= kMostShared * 4 + 96, "LDS");
     // floats of a part: [ROWS][D] O, [ROWS] m, [ROWS] l
     static constexpr int64_t PART = (int64_t)ROWS * (D + 2);
+};
+// The same with two bf16 for a probability.
+template <class S>
+struct Fine : S {
+    static_assert(!S::E4M3, "fp16 holds them well enough");
+    static constexpr bool TWO = true;
 };
 
 struct ChunkArgs {
@@ -313,6 +319,9 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
     constexpr int D = S::D, WM = S::WM, WK = S::WK, PB = S::PB, STEP = S::STEP, POS = STEP / 64;
     constexpr bool E4M3 = S::E4M3;
     using Half = pv8<E4M3>;
+    struct Weights {                                      // a block's probabilities; what their rounding leaves, where that is kept
+        Half of[2], rest[S::TWO ? 2 : 1];
+    };
     // e4m3: probabilities as fp16, 2^kUp of them, so that small ones are not lost below fp16's range (2^(kUp + kSlack) is within it)
     constexpr float kUp = E4M3 ? 11.0f : 0.0f;
     extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -537,11 +546,17 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[j][i] *= f;
         };
-        auto rounded = [&](const f32x16& s, Half (&pr)[2]) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) pr[t][i] = s[8 * t + i];
+        // probabilities e and e + 1 of a block, as they go to the second product
+        auto rounded = [&](const f32x16& s, Weights& pr, int e) {
+            if constexpr (S::TWO) {
+                const unsigned a = __float_as_uint(s[e]), b = __float_as_uint(s[e + 1]);
+                reinterpret_cast<unsigned(&)[4]>(pr.of[e / 8])[e % 8 / 2] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+                pr.rest[e / 8][e % 8] = s[e] - __uint_as_float(a & 0xFFFF0000u);
+                pr.rest[e / 8][e % 8 + 1] = s[e + 1] - __uint_as_float(b & 0xFFFF0000u);
+            } else {
+                pr.of[e / 8][e % 8] = s[e];
+                pr.of[e / 8][e % 8 + 1] = s[e + 1];
+            }
         };
         // ---------------- a block's products, in slots: KS of S = K Q^T, then 2 * VS of O^T += V^T P^T; their operand from K or V
         union Operand {
@@ -569,14 +584,17 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
             const unsigned k = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)kt, v = (unsigned)(uintptr_t)(__attribute__((address_space(3))) const char*)vt;
             return Lds{k + kat, k + kat32, v + vat, v + vat32};
         };
-        auto product = [&](auto slot, const Operand& a, f32x16& s, const Half (&pr)[2]) {
+        auto product = [&](auto slot, const Operand& a, f32x16& s, const Weights& pr) {
             constexpr int k = decltype(slot)::value, t = (k - S::KS) / S::VS, j = (k - S::KS) % S::VS;
             if constexpr (k < S::KS) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.k, q[k], k == 0 ? f32x16{} : s, 0, 0, 0);
-            else if constexpr (E4M3) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr[t], acc[j], 0, 0, 0);
-            else acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr[t], acc[j], 0, 0, 0);
+            else if constexpr (E4M3) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a.v, pr.of[t], acc[j], 0, 0, 0);
+            else {
+                acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr.of[t], acc[j], 0, 0, 0);
+                if constexpr (S::TWO) acc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.v, pr.rest[t], acc[j], 0, 0, 0);
+            }
         };
         auto scores = [&](const Lds& o, int b, f32x16& s) {
-            const Half none[2] = {};
+            const Weights none = {};
             unrolled<S::KS>([&](auto k) {
                 Operand a;
                 operand(k, o, b, a);
@@ -604,7 +622,7 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
             uint64_t there[LEAD + 3][POS];              // of steps j ..
             Look asked;
             f32x16 s0, s1;
-            Half p0[2], p1[2];
+            Weights p0, p1;
             float f;
             {
                 constexpr int N = LEAD + 2;
@@ -637,7 +655,8 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
                 }
                 cover(begin, 0, there[0], s0);
                 exponents(s0, f);
-                rounded(s0, p0);
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) rounded(s0, p0, e);
 #pragma unroll
                 for (int i = 0; i < LEAD; ++i) spread(w[2 + i].off, spots[i]);
             }
@@ -667,7 +686,7 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
                     if constexpr (k == 4) read(kbase, spots[LEAD - 1], kraw);
                     if constexpr (k == 5) asked = look(step + LEAD + 3);
                 };
-                auto part = [&](auto b_, f32x16& cur, f32x16& next, Half (&pr)[2], Half (&pn)[2]) {
+                auto part = [&](auto b_, f32x16& cur, f32x16& next, const Weights& pr, Weights& pn) {
                     constexpr int b = decltype(b_)::value, SLOTS = S::KS + 2 * S::VS, FIRST = SLOTS / 4, AHEAD = S::AHEAD;
                     Operand a[AHEAD + 1];
                     unrolled<AHEAD>([&](auto i) { operand(i, tiles, b, a[i]); });
@@ -687,13 +706,14 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
 #pragma unroll
                             for (int e = e0; e < e1; ++e) {
                                 exponent(cur, ref, e);
-                                pn[e / 8][e % 8] = cur[e];
+                                if (e & 1) rounded(cur, pn, e - 1);
                             }
                         }
                         if constexpr (b == 0) beside(i);
                         __builtin_amdgcn_sched_barrier(0);
                     });
-                    asm volatile("" : "+v"(pn[0]), "+v"(pn[1]), "+v"(l), "+v"(next));        // here, and not where they are needed
+                    asm volatile("" : "+v"(pn.of[0]), "+v"(pn.of[1]), "+v"(l), "+v"(next));  // here, and not where they are needed
+                    if constexpr (S::TWO) asm volatile("" : "+v"(pn.rest[0]), "+v"(pn.rest[1]));
                     if (__builtin_expect(moves, 0)) {
                         asm volatile("");                 // seldom: a branch, not a product with one
                         rescale(f);
@@ -707,8 +727,7 @@ __global__ void __launch_bounds__(S::THREADS, S::RESIDENT * S::WAVES >= 8 ? 2 : 
                 } else {
                     part(std::integral_constant<int, 0>{}, s1, s0, p0, p1);
                     s1 = s0;
-                    p0[0] = p1[0];
-                    p0[1] = p1[1];
+                    p0 = p1;
                 }
 #pragma unroll
                 for (int i = 0; i < LEAD + 2; ++i)
@@ -919,16 +938,25 @@ __global__ void __launch_bounds__(256) chunk_join(ChunkArgs p, int rows, float u
 //   more             eight waves with all positions: 4096 tokens, 32 over 8 heads of 64: 145; the shape for 128 rows 185
 // Heads of 192 and 256 columns leave registers for four waves, with all positions: 4096 tokens, 16 over 4 heads of 256: 264; where two share the
 // positions 477.  They do share them for few rows of 192 columns: 32 sequences of 4 tokens, 32 over 4 heads: 79 and 85 (of 256: 73 and 70).
+// Up to 128 rows a bf16 cache has two bf16 for a probability.  These calls wait for memory more than for products: a tree of 26 tokens 25.5 us with one and 26.2 with two, 64
+// sequences of 4 tokens 61.1 and 61.9, 32 of 33 120.5 and 127.3, 16 of 24 63.5 and 68.2; heads of 192 columns 88.7 and 94.1, of 256, which leave too few registers, 79.5
+// and 89.0.  Longer ones are bound by the products and by the making of their operands: a prompt of 2048 tokens 77.2 and 93.3, 16384 tokens 2065 and 2655.
 template <int D, bool E4M3, typename F>
 auto pick(double rows, F&& body)
 {
+    auto few = [&](auto shape) {
+        using S = decltype(shape);
+        if constexpr (E4M3) return body(S{});
+        else return body(Fine<S>{});
+    };
     if constexpr (D <= 128) {
-        if (rows <= 32) return body(Shape<D, E4M3, 1, D == 64 ? 4 : 2, 1>{});
-        if (E4M3 && rows <= 64) return body(Shape<D, E4M3, 2, 1, 2>{});
-        if (rows <= 128) return body(Shape<D, E4M3, 4, 2, 1>{});
+        if (rows <= 32) return few(Shape<D, E4M3, 1, D == 64 ? 4 : 2, 1>{});
+        if (E4M3 && rows <= 64) return few(Shape<D, E4M3, 2, 1, 2>{});
+        if (rows <= 128) return few(Shape<D, E4M3, 4, 2, 1>{});
         return body(Shape<D, E4M3, 8, 1, 2>{});
     } else {
-        if (D == 192 && rows <= 32) return body(Shape<192, E4M3, 2, 2, 1>{});
+        if (D == 192 && rows <= 32) return few(Shape<192, E4M3, 2, 2, 1>{});
+        if (rows <= 128) return few(Shape<D, E4M3, 4, 1, 2>{});
         return body(Shape<D, E4M3, 4, 1, 2>{});
     }
 }
