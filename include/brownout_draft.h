@@ -71,7 +71,8 @@ moe_status moe_tree_masks(const int32_t *parents, int32_t n, int32_t words, uint
  * Scores, softmax and sums are fp32.  For the product with v a probability is rounded to fp16 (2^-11 of it) beside an 8-bit cache.  Beside a bf16 cache it is held as two
  * bf16 (2^-15), as in moe_paged_attention, in calls with T * n_heads / n_kv_heads <= 128 * n_seqs, and rounded to one (2^-8) in those of more rows, where the second product costs a quarter of
  * the time.
- * The workspace (moe_chunk_workspace_size: for up to n_seqs sequences and T tokens, 256-byte aligned) needs no initialisation.
+ * The workspace (moe_chunk_workspace_size: for up to n_seqs sequences and T tokens, 256-byte aligned) needs no initialisation.  head_dim 128: 17 MB for up to 32 rows (tokens times
+ * n_heads / n_kv_heads), 34 for up to 128, 68 beyond.
  * Limits: head_dim 64, 96, 128, 192 or 256; n_heads a multiple of n_kv_heads, at most MOE_MAX_HEADS; T <= 65536, n_seqs <= 65536, seen_words <= 128.
  */
 typedef struct moe_chunk {

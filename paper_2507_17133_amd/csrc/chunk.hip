@@ -976,6 +976,14 @@ auto pick(int D, bool e4m3, double rows, F&& body)
     }
 }
 
+// Shares of the line of steps at most: as many blocks as there is room for.
+template <class S>
+constexpr int64_t most_shares()
+{
+    static_assert(256 * S::RESIDENT <= kChunkShares, "cuts");
+    return 256 * S::RESIDENT;
+}
+
 template <int D, bool E4M3>
 hipError_t init_of()
 {
@@ -1002,12 +1010,14 @@ hipError_t init_chunk_kernels()
     return init_of<256, true>();
 }
 
-// For every split of up to T tokens over up to n_seqs sequences: parts of the tallest tiles.
-size_t chunk_workspace_bytes(const moe_kv_cache& c, int n_seqs, int T, int n_heads)
+// For every split of up to T tokens over any number of sequences: the parts of the largest shape that it may take, which is one for at most as many rows as there are.
+size_t chunk_workspace_bytes(const moe_kv_cache& c, int T, int n_heads)
 {
-    (void)n_seqs; (void)T; (void)n_heads;
-    const int rows = c.head_dim <= 128 ? 256 : 128;
-    return align_up(kChunkShares * sizeof(int4), 256) + align_up((size_t)2 * kChunkShares * rows * (c.head_dim + 2) * sizeof(float), 256);
+    const double most = (double)T * (n_heads / c.n_kv_heads);
+    int64_t floats = 0;
+    for (double rows : {32.0, 64.0, 128.0, most})
+        floats = std::max(floats, pick(c.head_dim, c.type == MOE_KV_E4M3, std::min(rows, most), [](auto s) { return 2 * most_shares<decltype(s)>() * decltype(s)::PART; }));
+    return align_up(kChunkShares * sizeof(int4), 256) + align_up(floats * sizeof(float), 256);
 }
 
 hipError_t launch_chunk(const moe_kv_cache& c, const moe_block_table& t, const moe_chunk& ch, const bf16_t* q, int64_t q_stride, int n_heads, float scale,
@@ -1048,14 +1058,13 @@ hipError_t launch_chunk(const moe_kv_cache& c, const moe_block_table& t, const m
         // same positions at about the same time and write no parts: a prompt of 4096 tokens 164 us, in shares 197; four of 512, a window of 1024, 58 and
         // 67; sixteen of 128 95 and 109; 16384 tokens 2060 and 2194.  One sequence that is far longer than the others would keep few blocks busy, and only
         // the device knows the lengths: its blocks add them up (3 us) and take shares then.
-        const int most_shares = 256 * S::RESIDENT;
-        p.whole = ch.n_seqs > kMostShared ? 1 : !p.seen && rows >= 2 * S::ROWS && items - (int64_t)ch.n_seqs * p.Hk >= most_shares ? 2 : 0;
+        p.whole = ch.n_seqs > kMostShared ? 1 : !p.seen && rows >= 2 * S::ROWS && items - (int64_t)ch.n_seqs * p.Hk >= most_shares<S>() ? 2 : 0;
         if (p.whole == 1) {
             hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)items), dim3(S::THREADS), S::LDS, s, p);
             return hipGetLastError();
         }
         const int64_t most = items * (((int64_t)p.cap + S::STEP - 1) / S::STEP);
-        p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(most, most_shares));
+        p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(most, most_shares<S>()));
         hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)(p.whole ? std::max<int64_t>(items, p.shares) : p.shares)), dim3(S::THREADS), S::LDS, s, p);
         hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.shares == 1) return e;

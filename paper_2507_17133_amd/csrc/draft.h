@@ -29,7 +29,7 @@ moe_status rope_call(const moe_kv_cache* cache, const moe_block_table* table, co
                      bool apart, void* q_out, int64_t q_out_stride, void* stream, const char* name);
 
 hipError_t init_chunk_kernels();
-size_t chunk_workspace_bytes(const moe_kv_cache& c, int n_seqs, int T, int n_heads);
+size_t chunk_workspace_bytes(const moe_kv_cache& c, int T, int n_heads);
 hipError_t launch_chunk(const moe_kv_cache& c, const moe_block_table& t, const moe_chunk& ch, const bf16_t* q, int64_t q_stride, int n_heads, float scale,
                         bf16_t* out, int64_t out_stride, float* lse, void* ws, hipStream_t s);
 

@@ -67,7 +67,7 @@ moe_status moe_chunk_workspace_size(const moe_kv_cache* cache, int32_t n_seqs, i
     if (st != MOE_OK) return st;
     if (n_seqs < 0 || !bytes) return MOE_ERR_INVALID_ARG;
     if (n_seqs > kMostSeqs) return MOE_ERR_UNSUPPORTED;
-    *bytes = chunk_workspace_bytes(*cache, n_seqs, T, n_heads);
+    *bytes = chunk_workspace_bytes(*cache, T, n_heads);
     // a caller sizes its workspace before its first launch: the per-device set-up is done then, ahead of any stream capture
     if (ensure_device_init(nullptr) != hipSuccess) (void)hipGetLastError();
     return MOE_OK;
@@ -92,7 +92,7 @@ moe_status moe_chunk_attention(const moe_kv_cache* cache, const moe_block_table*
         bad_stride(q_stride, 8) || bad_stride(out_stride, 4))
         return MOE_ERR_ALIGNMENT;
     if ((T > 1 && out_stride < (int64_t)n_heads * cache->head_dim) || (chunk->seen && T > 1 && chunk->seen_stride < chunk->seen_words)) return MOE_ERR_SHAPE;
-    if (!workspace || workspace_bytes < chunk_workspace_bytes(*cache, n_seqs, T, n_heads)) return MOE_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < chunk_workspace_bytes(*cache, T, n_heads)) return MOE_ERR_WORKSPACE;
     if (off(workspace, 256)) return MOE_ERR_ALIGNMENT;
     // blocks read a token's q where others have written its out
     if (rows_meet(q, 2 * q_stride, out, 2 * out_stride, T, (int64_t)2 * n_heads * cache->head_dim)) return MOE_ERR_INVALID_ARG;
