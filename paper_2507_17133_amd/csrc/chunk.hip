@@ -99,6 +99,7 @@ struct ChunkArgs {
     int64_t out_stride;
     float* lse;
     int whole;                                    // one block for each item: 0 no, 1 yes, 2 if no item is much longer than a share
+    int first_block;                              // of the items' blocks, the first of this launch
     int shares;                                   // of the line of steps, otherwise
     int4* cuts;                                   // per share: the item that it begins and does not end (sequence, tile, key head, shares)
     float* parts;                                 // per share two parts
@@ -257,7 +258,8 @@ __device__ __forceinline__ bool find_share(const ChunkArgs& p, char* smem, Begin
 template <class S>
 __device__ __forceinline__ bool find_item(const ChunkArgs& p, Begin& o)
 {
-    const int lane = threadIdx.x & 63, slots = (int)((int64_t)p.T * p.group / S::ROWS) + p.n_seqs, u = slots - 1 - (int)(blockIdx.x / p.Hk);
+    const int lane = threadIdx.x & 63, slots = (int)((int64_t)p.T * p.group / S::ROWS) + p.n_seqs, block = p.first_block + (int)blockIdx.x,
+              u = slots - 1 - block / p.Hk;
     if (u < 0) return false;
     // the last sequence whose place is not beyond u, 64 of a stride at a time
     int lo = 0, n = p.n_seqs;
@@ -272,7 +274,7 @@ __device__ __forceinline__ bool find_item(const ChunkArgs& p, Begin& o)
     o.b = lo;
     const Seq s(p, lo);
     o.tile = u - place_of<S>(p, lo);
-    o.hk = blockIdx.x % p.Hk;
+    o.hk = block % p.Hk;
     o.unit = 0;
     return o.tile >= 0 && o.tile < s.row_tiles(p, S::ROWS);
 }
@@ -1059,9 +1061,16 @@ hipError_t launch_chunk(const moe_kv_cache& c, const moe_block_table& t, const m
         // 67; sixteen of 128 95 and 109; 16384 tokens 2060 and 2194.  One sequence that is far longer than the others would keep few blocks busy, and only
         // the device knows the lengths: its blocks add them up (3 us) and take shares then.
         p.whole = ch.n_seqs > kMostShared ? 1 : !p.seen && rows >= 2 * S::ROWS && items - (int64_t)ch.n_seqs * p.Hk >= most_shares<S>() ? 2 : 0;
+        p.first_block = 0;
         if (p.whole == 1) {
-            hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)items), dim3(S::THREADS), S::LDS, s, p);
-            return hipGetLastError();
+            constexpr int64_t kBlocks = ((int64_t)1 << 31) / S::THREADS;      // a launch takes less than 2^32 threads
+            for (int64_t at = 0; at < items; at += kBlocks) {
+                p.first_block = (int)at;
+                hipLaunchKernelGGL((chunk_kernel<S>), dim3((unsigned)std::min(kBlocks, items - at)), dim3(S::THREADS), S::LDS, s, p);
+                hipError_t e = hipGetLastError();
+                if (e != hipSuccess) return e;
+            }
+            return hipSuccess;
         }
         const int64_t most = items * (((int64_t)p.cap + S::STEP - 1) / S::STEP);
         p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(most, most_shares<S>()));
