@@ -478,17 +478,32 @@ hipError_t launch_logprobs(const moe_logprob_args& a, void* ws, hipStream_t s)
     p.tokens = a.tokens; p.tokens_stride = a.tokens_stride;
     p.logprob = a.logprob; p.rank = a.rank; p.lse = a.lse; p.entropy = a.entropy;
     p.top_id = a.top_id; p.top_logprob = a.top_logprob;
-    p.T = a.T; p.V = a.V;
+    p.V = a.V;
     p.G = a.logprob || a.rank ? a.n_given : 0;
     p.N = a.top_id || a.top_logprob ? a.n_top : 0;
     const int each = entries_each(a.T, a.V), size = a.type == MOE_LOGITS_FP32 ? 4 : 2;
     const bool aligned = reinterpret_cast<uintptr_t>(a.logits) % 16 == 0 && (a.T == 1 || a.stride * size % 16 == 0);
     p.slices = slices_of(a.V, each, aligned ? 0 : 16 / size - 1);
-    const size_t parts = (size_t)p.T * p.slices;
+    const size_t parts = (size_t)a.T * p.slices;
     p.stats = static_cast<float4*>(ws);
     p.before = reinterpret_cast<int*>(static_cast<char*>(ws) + align_up(parts * sizeof(float4), 256));
     p.best = reinterpret_cast<float2*>(reinterpret_cast<char*>(p.before) + align_up(parts * sizeof(int) * p.G, 256));
-    return a.type == MOE_LOGITS_FP32 ? go<true>(p, each, s) : go<false>(p, each, s);
+    // a launch takes less than 2^32 threads: rows that need more go in several
+    const int most = (int)(((int64_t)1 << 31) / kThreads / p.slices);
+    for (int t = 0; t < a.T; t += p.T) {
+        p.T = std::min(most, a.T - t);
+        const hipError_t e = a.type == MOE_LOGITS_FP32 ? go<true>(p, each, s) : go<false>(p, each, s);
+        if (e != hipSuccess) return e;
+        auto on = [&](auto*& q, int64_t n) {
+            if (q) q += n;
+        };
+        on(p.logits, (int64_t)p.T * a.stride * size);
+        on(p.tokens, (int64_t)p.T * a.tokens_stride);
+        on(p.logprob, (int64_t)p.T * a.n_given); on(p.rank, (int64_t)p.T * a.n_given);
+        on(p.lse, p.T); on(p.entropy, p.T);
+        on(p.top_id, (int64_t)p.T * a.n_top); on(p.top_logprob, (int64_t)p.T * a.n_top);
+    }
+    return hipSuccess;
 }
 
 }  // namespace bmoe
