@@ -54,14 +54,22 @@ moe_status moe_rope_append_at(const moe_kv_cache *cache, const moe_block_table *
 moe_status moe_tree_masks(const int32_t *parents, int32_t n, int32_t words, uint32_t *seen, int32_t *depth);
 
 /*
+ * The same for a model whose layers see a window: of a token's ancestors those that it and the sinks leave it, depth[i] - depth[j] < window or depth[j] < sinks (window 0: all).
+ * `sinks`: positions behind the context that are sinks yet, which is the model's number of them less the context's length if that is positive.  With these bits
+ * a token of a tree sees what it would see at its position of a sequence.  window or sinks < 0: MOE_ERR_INVALID_ARG.
+ */
+moe_status moe_tree_window_masks(const int32_t *parents, int32_t n, int32_t words, int32_t window, int32_t sinks, uint32_t *seen, int32_t *depth);
+
+/*
  * Attention of sequences' new tokens over the paged cache, each sequence's cache read once for all of them.  Sequence b has context[b] positions in the cache and
  * n_b = first[b+1] - first[b] new tokens, the rows first[b] .. of q; new token j's key and value are already at position context[b] + j.
  *   out[t][h] = sum_p softmax_p(scale * q[t][h] . k[p][h / group]) v[p][h / group]   over the positions p that token t sees:
  * A chunk (seen NULL): the j-th new token is at position P = context[b] + j and sees the positions p <= P with p > P - window or p < sinks
  *   (window 0: all p <= P).
  * A tree (seen not NULL): the token is at position P = positions[t] (NULL: context[b] + j) and sees of the context the positions p with p > P - window or
- *   p < sinks (window 0: all), and of the new tokens those whose bit is set in its row of `seen`, whatever the window.  Bits of tokens that the
- *   sequence does not have count for nothing, nor do tokens beyond 32 * seen_words.  P < context[b] counts as context[b].
+ *   p < sinks (window 0: all), and of the new tokens those whose bit is set in its row of `seen`: bits say what the window leaves of them, too (moe_tree_window_masks;
+ *   those of moe_tree_masks let a path longer than the window see all of itself).  Bits of tokens that the sequence does not have count for nothing, nor do
+ *   tokens beyond 32 * seen_words.  P < context[b] counts as context[b].
  * Positions whose page is not there (see moe_block_table) or that lie beyond max_pages * page_size are left out.  A token that sees nothing has
  * out = 0 and lse = -infinity.  What the cache holds in places that a token does not see does not matter to it, NaN included.
  *   first [n_seqs+1], context [n_seqs], positions [T] int32; seen [T][seen_words] uint32, rows seen_stride words apart; table's token_row [n_seqs]

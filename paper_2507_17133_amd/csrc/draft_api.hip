@@ -2,7 +2,6 @@
 #include "draft.h"
 
 #include <cmath>
-#include <vector>
 
 namespace bmoe {
 namespace {
@@ -43,7 +42,12 @@ moe_status moe_rope_append_at(const moe_kv_cache* cache, const moe_block_table* 
 
 moe_status moe_tree_masks(const int32_t* parents, int32_t n, int32_t words, uint32_t* seen, int32_t* depth)
 {
-    if (n < 0) return MOE_ERR_INVALID_ARG;
+    return moe_tree_window_masks(parents, n, words, 0, 0, seen, depth);
+}
+
+moe_status moe_tree_window_masks(const int32_t* parents, int32_t n, int32_t words, int32_t window, int32_t sinks, uint32_t* seen, int32_t* depth)
+{
+    if (n < 0 || window < 0 || sinks < 0) return MOE_ERR_INVALID_ARG;
     if (n > MOE_MAX_TREE) return MOE_ERR_UNSUPPORTED;
     if (n == 0) return MOE_OK;
     if (!parents) return MOE_ERR_INVALID_ARG;
@@ -55,8 +59,16 @@ moe_status moe_tree_masks(const int32_t* parents, int32_t n, int32_t words, uint
         if (depth) depth[i] = up < 0 ? 0 : depth[up] + 1;
         if (!seen) continue;
         uint32_t* row = seen + (int64_t)i * words;
+        // the parent's, and the token itself
         for (int32_t w = 0; w < words; ++w) row[w] = up < 0 ? 0 : seen[(int64_t)up * words + w];
         row[i / 32] |= 1u << (i % 32);
+        if (window == 0) continue;
+        // the ancestor that the parent sees and the token does not: `window` levels up, at level `of`
+        int32_t level = 0, at = i, of = 0;
+        for (; at >= 0 && level < window; ++level) at = parents[at];
+        if (at < 0) continue;
+        for (int32_t j = parents[at]; j >= 0; j = parents[j]) ++of;
+        if (of >= sinks) row[at / 32] &= ~(1u << (at % 32));
     }
     return MOE_OK;
 }

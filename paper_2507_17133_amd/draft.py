@@ -16,8 +16,8 @@ from .layer import (KvCache, Rope, _bytes, _heads, _ints, _like, _on, _rows, _ta
                     moe_block_table, moe_kv_cache, moe_rope)
 
 MOE_LOGITS_BF16, MOE_LOGITS_FP32 = 0, 1
-EXPORTS = ("moe_sink_attention", "moe_rope_append_at", "moe_tree_masks", "moe_chunk_workspace_size", "moe_chunk_attention", "moe_cache_move",
-           "moe_logprob_workspace_size", "moe_token_logprobs")
+EXPORTS = ("moe_sink_attention", "moe_rope_append_at", "moe_tree_masks", "moe_tree_window_masks", "moe_chunk_workspace_size", "moe_chunk_attention",
+           "moe_cache_move", "moe_logprob_workspace_size", "moe_token_logprobs")
 
 
 class moe_chunk(C.Structure):
@@ -43,6 +43,7 @@ def _lib():
             "moe_sink_attention": [cache, table, p, i64, i32, i32, p, C.c_float, i32, i32, p, i64, p, p, C.c_size_t, p],
             "moe_rope_append_at": [cache, table, C.POINTER(moe_rope), p, i64, p, i64, p, i64, i32, i32, p, p, p, i64, p],
             "moe_tree_masks": [p, i32, i32, p, p],
+            "moe_tree_window_masks": [p, i32, i32, i32, i32, p, p],
             "moe_chunk_workspace_size": [cache, i32, i32, i32, size],
             "moe_chunk_attention": [cache, table, C.POINTER(moe_chunk), p, i64, i32, C.c_float, p, i64, p, p, C.c_size_t, p],
             "moe_cache_move": [cache, table, p, i64, i32, p, p, i32, p],
@@ -97,13 +98,14 @@ def moe_rope_append_at(cache: KvCache, rope: Rope, q: torch.Tensor, k: torch.Ten
     return out
 
 
-def tree_masks(parents: Sequence[int], words: Optional[int] = None) -> Tuple[torch.Tensor, torch.Tensor]:
-    """(seen [n, words] int32, depth [n] int32) on the CPU of a tree of n tokens; parents[i] < i, or -1 for the context's last token."""
+def tree_masks(parents: Sequence[int], words: Optional[int] = None, window: int = 0, sinks: int = 0) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(seen [n, words] int32, depth [n] int32) on the CPU of a tree of n tokens; parents[i] < i, or -1 for the context's last token.  With a window, without the
+    ancestors that it leaves out; `sinks`: positions behind the context that are sinks yet."""
     n = len(parents)
     words = (n + 31) // 32 if words is None else words
     seen, depth = torch.empty((n, words), dtype=torch.int32), torch.empty(n, dtype=torch.int32)
     up = torch.tensor(list(parents), dtype=torch.int32)
-    _check(_lib().moe_tree_masks(up.data_ptr(), n, words, seen.data_ptr(), depth.data_ptr()), "moe_tree_masks")
+    _check(_lib().moe_tree_window_masks(up.data_ptr(), n, words, window, sinks, seen.data_ptr(), depth.data_ptr()), "moe_tree_window_masks")
     return seen, depth
 
 
@@ -124,7 +126,7 @@ def moe_chunk_attention(cache: KvCache, q: torch.Tensor, block_table: torch.Tens
                         workspace: Optional[torch.Tensor] = None, stream=None):
     """Attention of q [T, heads, dim], sequence b's new tokens first[b] .. first[b + 1] - 1 behind context[b] cached positions (theirs are in the cache
     already, from position context[b] on).  seen None: each token sees what is before it, with a window and sinks; seen [T, words] int32: bits of the
-    sequence's new tokens that it sees, as tree_masks gives them, at `positions` (None: context + its number).  table_row: each sequence's row."""
+    sequence's new tokens that it sees, as tree_masks gives them (for a window: with that), at `positions` (None: context + its number).  table_row: each sequence's row."""
     if stream is not None:
         return _under(stream, moe_chunk_attention, cache, q, block_table, first, context, table_row, seen, positions, scale, window, sinks, out, want_lse,
                       workspace)
