@@ -42,7 +42,9 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int kChunkShares = 512;                 // shares of the line of steps at most
 constexpr int kBetween = 5;                       // what an item costs besides its steps, in steps; with 1 a prompt of 2048 tokens took 138 us, with 5 84
-constexpr int kUneven = 16;                       // by how many steps an item may exceed a share where each has a block: about what parts and their join cost
+// By how many steps an item may exceed a share where each has a block.  8 chunks of 256 tokens behind up to 512 and up to 1792 positions: with 0 64 and 101 us, with 4 44 and 101, with 16 44 and
+// 82, with 64 the same; behind up to 4500, 8000 and 12000 with 16 171, 272 and 373, with 64 169, 260 and 375.
+constexpr int kUneven = 16;
 constexpr int kMostShared = 1024;                 // sequences of a call whose steps are dealt out in shares: what LDS has room for
 // How far (in powers of two) scores may exceed the maximum that they refer to.  0, so that O is rescaled whenever the maximum grows: 4096 tokens, 16 over 4
 // heads of 256, 318 us, with 4 264; 16 x 16 drafted tokens 94 and 80.  2^4 costs the probabilities no bits: they are floating-point, and sums are fp32.
@@ -929,17 +931,17 @@ __global__ void __launch_bounds__(256) chunk_join(ChunkArgs p, int rows, float u
 }
 
 // body(Shape): the shape that a call takes, by the rows that a sequence has on average.  Both sides measured, in us, 32 query heads over 8 of 128
-// columns if nothing else is said
-// (prompts in shares of steps):
+// columns if nothing else is said (prompts in shares of steps):
 //   up to 32 rows    two waves with a half of the positions each, two blocks a CU, so that one reads while the other begins or ends an item: 64
-//                    sequences of 8 tokens, up to 4096 positions in e4m3: 120; four waves 140; the shape for 128 rows 148.  Heads of 64 columns,
-//                    whose steps are small, with four waves: 32 sequences of 8 tokens 50, two waves 52 (16 of 16 tokens, bf16: 55 and 62)
+//                    sequences of 8 tokens, up to 4096 positions in e4m3: 120; four waves 138; the shape for 128 rows 149 (bf16, of 4 tokens over 4 heads: 62, 67, 66).  Heads of 64 columns,
+//                    whose steps are small, with four waves: 32 sequences of 8 tokens 50, two waves 53 (16 of 16 tokens, bf16: 55 and 60)
 //   up to 64, e4m3   two waves of 32 rows in the same manner: 64 sequences of 8 tokens, 64 over 8 heads, up to 2048 positions: 81; the next shape 93
-//   up to 64, bf16   where twice as much is on its way, the next shape: 16 tokens behind 32768 positions 45; two waves 49; four 46
-//   up to 128        eight waves, of which two share the positions of 32 rows: 16 sequences of 24 tokens, up to 4096 positions: 64; the last shape 67
+//   up to 64, bf16   where twice as much is on its way, the next shape: 16 tokens behind 32768 positions 47; two waves 50; four 56
+//   up to 128        eight waves, of which two share the positions of 32 rows: 32 sequences of 33 tokens, up to 4096 positions: 127; the last shape 150 (16 of 24 tokens: 68 and 71; one of
+//                    26 tokens behind 2048: 26 and 24)
 //   more             eight waves with all positions: 4096 tokens, 32 over 8 heads of 64: 145; the shape for 128 rows 185
 // Heads of 192 and 256 columns leave registers for four waves, with all positions: 4096 tokens, 16 over 4 heads of 256: 264; where two share the
-// positions 477.  They do share them for few rows of 192 columns: 32 sequences of 4 tokens, 32 over 4 heads: 79 and 85 (of 256: 73 and 70).
+// positions 477.  They do share them for few rows: 32 sequences of 4 tokens, 32 over 4 heads of 192 81 and 91, 16 of 4 tokens, heads of 256 74 and 79.
 // Up to 128 rows a bf16 cache has two bf16 for a probability.  These calls wait for memory more than for products: a tree of 26 tokens 25.5 us with one and 26.2 with two, 64
 // sequences of 4 tokens 61.1 and 61.9, 32 of 33 120.5 and 127.3, 16 of 24 63.5 and 68.2; heads of 192 columns 88.7 and 94.1, of 256, which leave too few registers, 79.5
 // and 89.0.  Longer ones are bound by the products and by the making of their operands: a prompt of 2048 tokens 77.2 and 93.3, 16384 tokens 2065 and 2655.
@@ -957,7 +959,7 @@ auto pick(double rows, F&& body)
         if (rows <= 128) return few(Shape<D, E4M3, 4, 2, 1>{});
         return body(Shape<D, E4M3, 8, 1, 2>{});
     } else {
-        if (D == 192 && rows <= 32) return few(Shape<192, E4M3, 2, 2, 1>{});
+        if (rows <= 32) return few(Shape<D, E4M3, 2, 2, 1>{});
         if (rows <= 128) return few(Shape<D, E4M3, 4, 1, 2>{});
         return body(Shape<D, E4M3, 4, 1, 2>{});
     }
