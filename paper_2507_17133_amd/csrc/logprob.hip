@@ -16,8 +16,11 @@ namespace {
 // waves 242, 247, 256 and 371 us).
 constexpr int kThreads = 64;
 constexpr int kJoinThreads = 256, kJoinWaves = kJoinThreads / 64;
-constexpr int kEnough = 1536;                     // slices from which longer ones are taken: six for each CU
-constexpr int kCandidates = 512;                  // entries that a block sorts
+// Slices from which longer ones are taken: six for each CU.  fp32, one given token and 20 alternatives, 50021 entries: 16 rows with 384 21.5 us, with 1536 19.9; 32 rows with 768 22.5, with 1536
+// 20.9; 67 rows with 1536 24.6, with 3072 22.6, with 6144 23.7; but 16 rows of 131072 23.0 with 1536 and 27.2 with 3072.
+constexpr int kEnough = 1536;
+// Entries that a block sorts.  With 256 the same; with 1024, whose LDS leaves room for fewer blocks, 2112 rows of 131072 entries 266 us instead of 229.
+constexpr int kCandidates = 512;
 constexpr int kLongest = 32;                      // entries of a thread at most: slices of 2048
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
@@ -338,14 +341,12 @@ __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
     auto each = [&](float bound, auto&& f) {
 #pragma unroll
         for (int j = 0; j < VECS; ++j)
-            {
 #pragma unroll
-                for (int i = PER * j; i < PER * j + PER; ++i)
-                    if (x[i] >= bound) {
-                        const int id = begin + (j * kThreads + tid) * PER + i % PER;
-                        if ((unsigned)id < (unsigned)p.V) f(Entry{x[i], id});
-                    }
-            }
+            for (int i = PER * j; i < PER * j + PER; ++i)
+                if (x[i] >= bound) {
+                    const int id = begin + (j * kThreads + tid) * PER + i % PER;
+                    if ((unsigned)id < (unsigned)p.V) f(Entry{x[i], id});
+                }
     };
     if (p.slices > 1) {
         if (tid == 0) p.stats[blockIdx.x] = make_float4(a.m, a.s, a.u, 0.0f);
