@@ -81,6 +81,8 @@ moe_status moe_tree_window_masks(const int32_t *parents, int32_t n, int32_t word
  * the time.
  * The workspace (moe_chunk_workspace_size: for up to n_seqs sequences and T tokens, 256-byte aligned) needs no initialisation.  head_dim 128: 17 MB for up to 32 rows (tokens times
  * n_heads / n_kv_heads), 34 for up to 128, 68 beyond.
+ * Tiles of rows go by the call's mean, T / n_seqs: a long chunk beside many single tokens is better a call of its own.  So is one sequence far longer than the others of a call of more than 1024: there
+ * each tile has one block per key head, and is not shared out.
  * Limits: head_dim 64, 96, 128, 192 or 256; n_heads a multiple of n_kv_heads, at most MOE_MAX_HEADS; T <= 65536, n_seqs <= 65536, seen_words <= 128.
  */
 typedef struct moe_chunk {

@@ -23,9 +23,9 @@
 // What bounds it: a CU's matrix and vector instructions, which hardly overlap.  (Beside a step of 32 x 32 x 16 MFMAs that takes 16.6 ns alone, fused multiply-adds
 // of 10.1 ns alone make 22.4.)  So the loop has its products, LDS reads and the softmax of the neighbouring blocks in slots of a fixed order: block n is
 // weighed, n + 1 has its exponentials taken, n + 2 its scores computed.  Measured, join included: 16384 tokens of four prompts, a window of
-// 4096, 56 over 8 heads of 128, bf16 2060 to 2120 us, 918 TFLOP/s (matrix pipe 0.43 of the cycles, vector 0.52 of the issue); 64 trees of 33 tokens behind up
-// to 8192 positions, 64 over 8 heads, e4m3 450 to 478 us, 1.8 TB/s and 650 TFLOP/s (0.34 and 0.44: 27 us are the join, and items begin and end); a tree of 26 tokens behind
-// 2048 positions 25 us, latency.  Without that order, or with LDS rows that were not turned, the first took 2614.
+// 4096, 56 over 8 heads of 128, bf16 2050 to 2150 us on different cards, 900 to 940 TFLOP/s (matrix pipe 0.43 of the cycles, vector 0.51 of the issue); 64 trees of 33 tokens behind up
+// to 8192 positions, 64 over 8 heads, e4m3 472 to 490 us, 1.8 TB/s and 650 TFLOP/s (0.34 and 0.44: 24 us are the join, and items begin and end); a tree of 26 tokens behind
+// 2048 positions 26 us, latency.  Without that order, or with LDS rows that were not turned, the first took 2614.
 #include "draft.h"
 #include "chunk_span.h"
 

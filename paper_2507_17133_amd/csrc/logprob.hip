@@ -220,7 +220,7 @@ __device__ __forceinline__ Entry given_token(const LogprobArgs& p, const char* r
 }
 
 // One slice of a row, EACH entries a thread.  Large calls are bound by HBM as long as sums are all that is asked for (2112 rows of 131072 entries 95 us, 5.8 TB/s),
-// by vector instructions with ranks (two per entry and given token: four tokens 168 us) and alternatives (eight 149 us, both 230); small ones by their launches.
+// by vector instructions with ranks (two per entry and given token: four tokens 168 us) and alternatives (eight 149 us, both 229 in a row of calls: 217 and the join's 12); small ones by their launches.
 template <bool FP32, int EACH>
 __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
 {
@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(kThreads) slice_kernel(LogprobArgs p)
 }
 
 // A block for each row whose slices are joined, in whole numbers or a fixed order.  What does not depend on the sums is asked for first, and counts are added up by all
-// threads (2112 rows of 64 slices, four given tokens: 14 us; a thread for each token 28).  The slices' best entries are read a second time where they are chosen from: they are many only in rows of many slices.
+// threads (2112 rows of 64 slices, four given tokens and eight alternatives: 12 to 14 us; a thread for each token 28).  The slices' best entries are read a second time where they are chosen from: they are many only in rows of many slices.
 template <bool FP32>
 __global__ void __launch_bounds__(kJoinThreads) join_rows(LogprobArgs p)
 {

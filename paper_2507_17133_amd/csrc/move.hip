@@ -2,7 +2,7 @@
 //
 // Sources increase and none lies before its target, so a thread that takes its 16 bytes of a head through the list, eight entries read before any of
 // them is written, moves them as if all had been read first.  Each entry is two dependent loads (list, block table) of one address for the whole block, then
-// the row: latency, of a few accepted tokens (5 of one request, 8 heads of 128, bf16: 4.5 us) as of many (up to 9 of each of 256, e4m3: 9.9 us, 9.4 MB
+// the row: latency, of a few accepted tokens (5 of one request, 8 heads of 128, bf16: 4.5 us) as of many (up to 9 of each of 256, e4m3: 9.7 us in a row of calls, 9.4 MB
 // read and written).  Every thread walks the list and divides for itself, and the time goes by the entries: up to 1, 2, 4, 8, 9 and 16 of each of 256 take 4.0, 4.7, 5.9, 8.4, 9.9 and 14.6 us.  Trips
 // cost little beside that from eight entries on: up to 9 with 4 at a time 20.6 us, with 12 9.4, with 16 10.1, the one request 0.1 and 0.6 us more.
 #include "draft.h"
